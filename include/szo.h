@@ -248,6 +248,157 @@ size_t szo_step_workspace_bytes(const szo_linear_desc* descs /* host */, int n, 
  * workspace; every loss-accumulating call leaves the workspace idle again when it completes. */
 int szo_workspace_init(void* workspace, void* stream);
 
+/* ---- between the linear layers of a decoder block, and behind its head -------------------------------------
+ * What a model of these layers needs to score answers and to serve tokens: norms of queries and keys with the
+ * position rotation, a key/value cache in 8 bits, attention over it, and log probabilities of given tokens (the
+ * scalar f of Definition 1 for a language model is their negative mean).  The same conventions as above: the
+ * calls enqueue on `stream`, allocate nothing, never synchronise, and can be captured into a HIP graph.  Strides count
+ * elements; the last axis of every tensor is contiguous. */
+
+/* Element types of these calls. */
+#define SZO_F32   0
+#define SZO_BF16  1
+#define SZO_F16   2
+
+/* Queries and keys of a batch of tokens: for each token and head
+ *   u = x * w / sqrt(mean(x^2) + eps)      (norm != 0; w = 1 where the weight is NULL; u = x without norm)
+ *   out = u, its first rot_dim features turned pairwise by the angles of the token's position:
+ *         (a, b) -> (a cos - b sin, b cos + a sin), pairs (i, i + rot_dim/2), or (2i, 2i+1) with `interleaved`.
+ * Sums and products in fp32, rounded once to out_type.  A token whose position lies outside the tables gets NaN in the rotated features.
+ * kv_heads 0: queries only.  Outputs may be the inputs' own buffers where type and strides are the same. */
+typedef struct szo_qk_desc {
+  int64_t tokens;
+  int32_t q_heads, kv_heads;
+  int32_t head_dim, rot_dim;    /* multiples of 8; head_dim <= 256; 0 <= rot_dim <= head_dim            */
+  int32_t in_type, out_type;    /* SZO_F32, SZO_BF16 or SZO_F16                                         */
+  int32_t norm, interleaved;    /* 0 or 1                                                                */
+  float   eps;
+  int32_t reserved;             /* 0                                                                     */
+  const void *q, *k;            /* device [tokens, heads, head_dim] of in_type                          */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  const float *q_weight, *k_weight;   /* device fp32 [head_dim], may be NULL                            */
+  const int32_t* positions;     /* device [tokens]; may be NULL if rot_dim == 0                         */
+  const float *cos_table, *sin_table; /* device fp32 [table_rows, rot_dim/2], contiguous                */
+  int64_t table_rows;
+  void *q_out, *k_out;          /* device [tokens, heads, head_dim] of out_type                          */
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} szo_qk_desc;
+
+/* Gradients of a scalar by the outputs (read), by the inputs and by the weights (overwritten). */
+typedef struct szo_qk_grads {
+  int32_t out_type, reserved;   /* type of q_out_grad, k_out_grad; q_grad, k_grad are of the descriptor's in_type */
+  const void *q_out_grad, *k_out_grad;
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+  void *q_grad, *k_grad;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  float *q_weight_grad, *k_weight_grad;   /* device fp32 [head_dim], or NULL: not wanted                */
+} szo_qk_grads;
+
+int szo_qk_norm_rope(const szo_qk_desc* desc /* host */, void* stream);
+/* Backward of it from the same inputs (q_out and k_out of the descriptor are not read).  The weights' gradients are sums
+ * over tokens and heads in a fixed order.  workspace: device, szo_qk_workspace_bytes(desc), 16-byte aligned, for this call
+ * alone while it runs; may be NULL if no weight gradient is wanted. */
+int szo_qk_norm_rope_bwd(const szo_qk_desc* desc /* host */, const szo_qk_grads* grads /* host */, void* workspace, void* stream);
+size_t szo_qk_workspace_bytes(const szo_qk_desc* desc /* host */);
+
+/* A key/value cache in 8 bits.  Tokens of a sequence lie in pages, named in order by a row of page_table; a page holds,
+ * head by head, blocks of SZO_KV_BLOCK tokens.  The keys of a block are e4m3 codes (4 significant bits, largest 448, no
+ * infinity) with one power of two, and so are its values: x = code * 2^(exp byte - 127).  The exponent is the smallest
+ * with max|x| <= 448 * 2^e, e in [-32, 120], over the block's 32 tokens: powers of two make both directions exact but for
+ * the rounding to the code, and let a block's exponent grow by moving the codes' own exponents.
+ * Order inside a block of 32 * head_dim bytes, token t = 16a + 8b + 4c + r, feature d:
+ *   keys    byte (d / 32) * 1024 + t * 32 + d % 32
+ *   values  byte d * 32 + 16c + 8a + 4b + r
+ * so that a wave's 16-byte loads of either are contiguous and already are operands of the matrix products. */
+#define SZO_KV_BLOCK 32
+typedef struct szo_kv_cache {
+  int32_t pages, page_tokens;   /* page_tokens a multiple of 32                                          */
+  int32_t kv_heads, head_dim;   /* head_dim 64, 96, 128 or 256                                           */
+  int32_t sequences, max_pages; /* shape of page_table                                                   */
+  uint8_t *k, *v;               /* device [pages, kv_heads, page_tokens/32, 32*head_dim], 16-byte aligned */
+  uint8_t *k_exp, *v_exp;       /* device [pages, kv_heads, page_tokens/32]                             */
+  const int32_t* page_table;    /* device [sequences, max_pages]; an entry outside [0, pages) holds nothing */
+  const int32_t* lengths;       /* device [sequences]: tokens of each sequence, new ones included        */
+} szo_kv_cache;
+
+/* The newest tokens of every sequence: sequence b has those from token_start[b] to token_start[b+1], which stand at the end of its
+ * lengths[b] positions. */
+typedef struct szo_kv_tokens {
+  int32_t type, reserved;       /* SZO_F32, SZO_BF16 or SZO_F16                                         */
+  int64_t max_new;              /* most new tokens of one sequence; blocks of further ones are left out   */
+  const int32_t* token_start;   /* device [sequences + 1], ascending from 0                              */
+  void *k, *v;                  /* device [tokens, kv_heads, head_dim]                                   */
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} szo_kv_tokens;
+
+/* Quantises new tokens into the cache.  A block whose first token is among them is written whole (codes behind the last
+ * token become 0); in another block the other codes stay, moved to the new exponent where it grew.  NaN and infinities
+ * become NaN and do not count for the exponent.  No two sequences may write one page. */
+int szo_kv_cache_write(const szo_kv_cache* cache /* host */, const szo_kv_tokens* tokens /* host */, void* stream);
+/* The same tokens back from the cache, exactly what the codes stand for, rounded to `type` (bf16 holds every one exactly).
+ * Tokens on pages outside the cache come back as 0. */
+int szo_kv_cache_read(const szo_kv_cache* cache /* host */, const szo_kv_tokens* tokens /* host */, void* stream);
+
+/* Attention of the newest tokens of every sequence over its cache (what szo_kv_cache_write left there, the new tokens' own
+ * keys and values among it):
+ *   out = softmax(scale q K^T) V over the positions that a query sees.  Query i of n of a sequence with `length` tokens
+ *   stands at position p = length - n + i and sees positions [0, length), with `causal` up to p, with window > 0 from
+ *   p - window + 1 on.  A query that sees nothing gives 0, and lse -inf.
+ * q_heads is a multiple of kv_heads; query head h reads key head h / (q_heads / kv_heads).  What lies behind the length, or
+ * in masked places, has no influence, NaN included.  Scores, statistics and sums are fp32; the weights of the values are
+ * rounded to fp16 (11 significant bits, relative to the largest of the row), the output once to `type`. */
+typedef struct szo_attn_desc {
+  szo_kv_cache cache;
+  int32_t q_heads, type;        /* type of q and out: SZO_BF16 or SZO_F16                                */
+  int32_t causal, window;
+  float   scale;
+  int32_t max_q;                /* most queries of one sequence; further ones are left out               */
+  int32_t max_len, reserved;    /* longest sequence: a hint that the split of the work goes by            */
+  int64_t tokens;               /* rows of q                                                             */
+  const void* q;                /* device [tokens, q_heads, head_dim]                                    */
+  int64_t q_token_stride, q_head_stride;
+  const int32_t* q_start;       /* device [sequences + 1], ascending from 0 to tokens                   */
+  void* out;                    /* device [tokens, q_heads, head_dim]                                    */
+  int64_t out_token_stride, out_head_stride;
+  float* lse;                   /* device [tokens, q_heads]: log of the sum of exp(scale q k), or NULL    */
+} szo_attn_desc;
+/* workspace: device, szo_attn_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs. */
+int szo_attn_cached(const szo_attn_desc* desc /* host */, void* workspace, void* stream);
+size_t szo_attn_workspace_bytes(const szo_attn_desc* desc /* host */);
+
+/* Log probabilities of given tokens under softmax(scale * logits), row by row, in one pass over the logits:
+ *   logp = scale x_target - log sum exp(scale x)      entropy = -sum p log p      alternatives: the `top` largest logits
+ * Alternatives are in descending order, ties to the lower index, NaN before everything.  A target outside [0, vocab) is
+ * ignored: logp 0, no loss, no gradient of logp.  A row of -inf alone has no probabilities: logp and top_logp -inf, entropy 0,
+ * gradient 0.  A row with a NaN or +inf gives NaN.  Outputs that are NULL are not computed. */
+#define SZO_LOGPROBS_MAX_TOP 32
+typedef struct szo_logprobs_desc {
+  int64_t rows, vocab, row_stride;
+  int32_t type, top;            /* type of the logits; 0 <= top <= 32, top <= vocab                      */
+  float   scale;                /* 1 / temperature, finite and > 0                                       */
+  int32_t reserved;             /* 0                                                                     */
+  const void* logits;           /* device [rows, vocab]                                                  */
+  const int32_t* targets;       /* device [rows]; NULL: every target ignored                             */
+  float* logp;                  /* device [rows]                                                         */
+  float* entropy;               /* device [rows]; read by the backward                                   */
+  float* stats;                 /* device [rows, 2]: largest logit, sum of exp(scale (x - largest)); read by the backward */
+  float* top_logp;              /* device [rows, top]                                                    */
+  int32_t* top_index;           /* device [rows, top]                                                    */
+  double* loss_acc;             /* device double or NULL: loss_acc += loss_scale * sum of -logp over the rows with a target,
+                                 * in fp64 and a fixed order (logp may then not be NULL)                  */
+  double loss_scale;
+} szo_logprobs_desc;
+/* workspace: device, szo_logprobs_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs. */
+int szo_token_logprobs(const szo_logprobs_desc* desc /* host */, void* workspace, void* stream);
+size_t szo_logprobs_workspace_bytes(const szo_logprobs_desc* desc /* host */);
+/* Gradient by the logits of a scalar whose gradients by logp and by entropy are grad_logp and grad_entropy (device fp32
+ * [rows], either may be NULL):
+ *   grad_logits = scale (grad_logp (1[v = target] - p) - grad_entropy p (log p + entropy))
+ * from the forward's stats (and entropy, if grad_entropy is not NULL).  grad_logits: device, type of the logits, rows
+ * grad_row_stride apart; may be the logits' own buffer.  The other outputs of the descriptor are not touched. */
+int szo_token_logprobs_bwd(const szo_logprobs_desc* desc /* host */, const float* grad_logp, const float* grad_entropy,
+                           void* grad_logits, int64_t grad_row_stride, void* stream);
+
 /* ---- one-time set-up on the host (no GPU needed; deterministic) ------------------------- */
 
 /* Number of TCSR tiles of an [N,K] matrix: ceil(N/64) * (K/64).  0 if K % 64 != 0. */

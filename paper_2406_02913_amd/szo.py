@@ -21,6 +21,9 @@ STEP_FUSED_LOSS = 1
 STEP_ONE_DENSE_PASS = 2
 STEP_SMALL_WORKSPACE = 4
 FORMAT_UNIFORM, FORMAT_LUT = 0, 1
+F32, BF16, F16 = 0, 1, 2                  # element types of the calls between the linear layers
+KV_BLOCK = 32                             # tokens that share an exponent in the cache
+LOGPROBS_MAX_TOP = 32
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -37,6 +40,46 @@ class LinearDesc(C.Structure):
                 ("y", C.c_void_p), ("target", C.c_void_p),
                 ("lut", C.c_void_p), ("format", C.c_int32), ("reserved", C.c_int32),
                 ("x_minus", C.c_void_p)]
+
+
+def _fields(kind, names):
+    return [(n, kind) for n in names.split()]
+
+
+_I32, _I64, _PTR = C.c_int32, C.c_int64, C.c_void_p
+
+
+class QkDesc(C.Structure):
+    _fields_ = (_fields(_I64, "tokens") + _fields(_I32, "q_heads kv_heads head_dim rot_dim in_type out_type norm interleaved") + _fields(C.c_float, "eps") +
+                _fields(_I32, "reserved") + _fields(_PTR, "q k") + _fields(_I64, "q_token_stride q_head_stride k_token_stride k_head_stride") +
+                _fields(_PTR, "q_weight k_weight positions cos_table sin_table") + _fields(_I64, "table_rows") + _fields(_PTR, "q_out k_out") +
+                _fields(_I64, "q_out_token_stride q_out_head_stride k_out_token_stride k_out_head_stride"))
+
+
+class QkGrads(C.Structure):
+    _fields_ = (_fields(_I32, "out_type reserved") + _fields(_PTR, "q_out_grad k_out_grad") +
+                _fields(_I64, "q_out_token_stride q_out_head_stride k_out_token_stride k_out_head_stride") + _fields(_PTR, "q_grad k_grad") +
+                _fields(_I64, "q_token_stride q_head_stride k_token_stride k_head_stride") + _fields(_PTR, "q_weight_grad k_weight_grad"))
+
+
+class KvCache(C.Structure):
+    _fields_ = _fields(_I32, "pages page_tokens kv_heads head_dim sequences max_pages") + _fields(_PTR, "k v k_exp v_exp page_table lengths")
+
+
+class KvTokens(C.Structure):
+    _fields_ = (_fields(_I32, "type reserved") + _fields(_I64, "max_new") + _fields(_PTR, "token_start k v") +
+                _fields(_I64, "k_token_stride k_head_stride v_token_stride v_head_stride"))
+
+
+class AttnDesc(C.Structure):
+    _fields_ = ([("cache", KvCache)] + _fields(_I32, "q_heads type causal window") + _fields(C.c_float, "scale") + _fields(_I32, "max_q max_len reserved") +
+                _fields(_I64, "tokens") + _fields(_PTR, "q") + _fields(_I64, "q_token_stride q_head_stride") + _fields(_PTR, "q_start out") +
+                _fields(_I64, "out_token_stride out_head_stride") + _fields(_PTR, "lse"))
+
+
+class LogprobsDesc(C.Structure):
+    _fields_ = (_fields(_I64, "rows vocab row_stride") + _fields(_I32, "type top") + _fields(C.c_float, "scale") + _fields(_I32, "reserved") +
+                _fields(_PTR, "logits targets logp entropy stats top_logp top_index loss_acc") + _fields(C.c_double, "loss_scale"))
 
 
 _P = C.POINTER
@@ -73,6 +116,16 @@ _SIGS = {
     "szo_kernel_timing": (C.c_int, [C.c_int]),
     "szo_kernel_timing_read": (C.c_int, [C.c_void_p, C.c_void_p]),
     "szo_kernel_timing_read2": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "szo_qk_norm_rope": (C.c_int, [_P(QkDesc), C.c_void_p]),
+    "szo_qk_norm_rope_bwd": (C.c_int, [_P(QkDesc), _P(QkGrads), C.c_void_p, C.c_void_p]),
+    "szo_qk_workspace_bytes": (C.c_size_t, [_P(QkDesc)]),
+    "szo_kv_cache_write": (C.c_int, [_P(KvCache), _P(KvTokens), C.c_void_p]),
+    "szo_kv_cache_read": (C.c_int, [_P(KvCache), _P(KvTokens), C.c_void_p]),
+    "szo_attn_cached": (C.c_int, [_P(AttnDesc), C.c_void_p, C.c_void_p]),
+    "szo_attn_workspace_bytes": (C.c_size_t, [_P(AttnDesc)]),
+    "szo_token_logprobs": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p]),
+    "szo_logprobs_workspace_bytes": (C.c_size_t, [_P(LogprobsDesc)]),
+    "szo_token_logprobs_bwd": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "szo_last_hip_error": (C.c_int, []),
     "szo_version": (C.c_int, []),
 }
@@ -196,6 +249,193 @@ def new_workspace(device="cuda", nbytes=None):
     ws = torch.empty(szo_workspace_bytes() if nbytes is None else nbytes, dtype=torch.uint8, device=device)
     szo_workspace_init(ws)
     return ws
+
+
+# ---- between the linear layers ------------------------------------------------------------------
+# A descriptor holds device pointers, so its tensors have to outlive it: it keeps them in `keep`.
+def _type(t):
+    import torch
+    try:
+        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[t.dtype]
+    except KeyError:
+        raise ValueError(f"expected fp32, bf16 or fp16, got {t.dtype}") from None
+
+
+def _strided(t, shape):
+    """Pointer and the strides of tokens and heads of [tokens, heads, head_dim]; the last axis has to be contiguous."""
+    if t is None:
+        return None, 0, 0
+    if not t.is_cuda or tuple(t.shape) != tuple(shape) or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"expected a device tensor {tuple(shape)} with a contiguous last axis, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _typed(t, dtype, shape):
+    """Pointer of a contiguous device tensor of the type and shape that a call reads or writes (None -> NULL)."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _dev(t)
+
+
+def make_qk_desc(q, k, positions, cos_table, sin_table, q_out=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, norm=None):
+    """q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (or None), any strides with a contiguous last axis; tables fp32
+    [rows, rot_dim / 2] (None: no rotation).  `norm` is on where a weight is given, unless said otherwise.  Without outputs: for the backward."""
+    import torch
+    T, heads, D = q.shape
+    kv = 0 if k is None else k.shape[1]
+    if k is not None and k.dtype != q.dtype or (q_out is not None and k_out is not None and q_out.dtype != k_out.dtype):
+        raise ValueError("queries and keys are of one type, and so are their outputs")
+    rows, rot = (0, 0) if cos_table is None else (cos_table.shape[0], 2 * cos_table.shape[1])
+    out = q_out if q_out is not None else q
+    d = QkDesc(T, heads, kv, D, rot, _type(q), _type(out), int((q_weight is not None or k_weight is not None) if norm is None else norm), int(interleaved), eps, 0)
+    d.q, d.q_token_stride, d.q_head_stride = _strided(q, (T, heads, D))
+    d.k, d.k_token_stride, d.k_head_stride = _strided(k, (T, kv, D))
+    d.q_weight, d.k_weight = _typed(q_weight, torch.float32, (D,)), _typed(k_weight, torch.float32, (D,))
+    d.positions = _typed(positions, torch.int32, (T,))
+    d.cos_table, d.sin_table = _typed(cos_table, torch.float32, (rows, rot // 2)), _typed(sin_table, torch.float32, (rows, rot // 2))
+    d.table_rows = rows
+    d.q_out, d.q_out_token_stride, d.q_out_head_stride = _strided(q_out, (T, heads, D))
+    d.k_out, d.k_out_token_stride, d.k_out_head_stride = _strided(k_out, (T, kv, D))
+    d.keep = (q, k, positions, cos_table, sin_table, q_out, k_out, q_weight, k_weight)
+    return d
+
+
+def make_qk_grads(q_out_grad, k_out_grad, q_grad, k_grad, q_weight_grad=None, k_weight_grad=None):
+    import torch
+    D = q_grad.shape[2]
+    if k_grad is not None and (k_grad.dtype != q_grad.dtype or k_out_grad.dtype != q_out_grad.dtype):
+        raise ValueError("gradients of queries and keys are of one type")
+    g = QkGrads(_type(q_out_grad), 0)
+    g.q_out_grad, g.q_out_token_stride, g.q_out_head_stride = _strided(q_out_grad, q_grad.shape)
+    g.q_grad, g.q_token_stride, g.q_head_stride = _strided(q_grad, q_grad.shape)
+    if k_grad is not None:
+        g.k_out_grad, g.k_out_token_stride, g.k_out_head_stride = _strided(k_out_grad, k_grad.shape)
+        g.k_grad, g.k_token_stride, g.k_head_stride = _strided(k_grad, k_grad.shape)
+    g.q_weight_grad, g.k_weight_grad = _typed(q_weight_grad, torch.float32, (D,)), _typed(k_weight_grad, torch.float32, (D,))
+    g.shapes = tuple(q_grad.shape), (0 if k_grad is None else k_grad.shape[1]), _type(q_grad)
+    g.keep = (q_out_grad, k_out_grad, q_grad, k_grad, q_weight_grad, k_weight_grad)
+    return g
+
+
+def szo_qk_norm_rope(desc, stream=None):
+    _check("szo_qk_norm_rope", lib.szo_qk_norm_rope(C.byref(desc), _stream(stream)))
+
+
+def szo_qk_norm_rope_bwd(desc, grads, workspace=None, stream=None):
+    if grads.shapes != ((desc.tokens, desc.q_heads, desc.head_dim), desc.kv_heads, desc.in_type):
+        raise ValueError("gradients of other shapes or another type than the inputs")
+    _check("szo_qk_norm_rope_bwd", lib.szo_qk_norm_rope_bwd(C.byref(desc), C.byref(grads), _dev(workspace), _stream(stream)))
+
+
+def szo_qk_workspace_bytes(desc):
+    return int(lib.szo_qk_workspace_bytes(C.byref(desc)))
+
+
+def new_kv_cache(pages, page_tokens, kv_heads, head_dim, device="cuda"):
+    """(k, v, k_exp, v_exp) of an empty cache."""
+    import torch
+    shape = (pages, kv_heads, page_tokens // KV_BLOCK, KV_BLOCK * head_dim)
+    return tuple(torch.zeros(s, dtype=torch.uint8, device=device) for s in (shape, shape, shape[:3], shape[:3]))
+
+
+def make_kv_cache(k, v, k_exp, v_exp, page_table, lengths):
+    """k, v u8 [pages, kv_heads, page_tokens / 32, 32 * head_dim]; exponents u8 without the last axis; page_table i32 [sequences, max_pages]; lengths i32
+    [sequences], which a program updates in place as sequences grow."""
+    import torch
+    pages, heads, blocks, size = k.shape
+    _typed(v, torch.uint8, k.shape)
+    c = KvCache(pages, blocks * KV_BLOCK, heads, size // KV_BLOCK, page_table.shape[0], page_table.shape[1], _typed(k, torch.uint8, k.shape), _dev(v),
+                _typed(k_exp, torch.uint8, k.shape[:3]), _typed(v_exp, torch.uint8, k.shape[:3]), _typed(page_table, torch.int32, page_table.shape),
+                _typed(lengths, torch.int32, (page_table.shape[0],)))
+    c.keep = (k, v, k_exp, v_exp, page_table, lengths)
+    return c
+
+
+def make_kv_tokens(k, v, token_start, max_new):
+    """k, v [tokens, kv_heads, head_dim]: read by szo_kv_cache_write, written by szo_kv_cache_read."""
+    import torch
+    if k.dtype != v.dtype:
+        raise ValueError("keys and values are of one type")
+    t = KvTokens(_type(k), 0, max_new, _typed(token_start, torch.int32, token_start.shape))
+    t.k, t.k_token_stride, t.k_head_stride = _strided(k, k.shape)
+    t.v, t.v_token_stride, t.v_head_stride = _strided(v, k.shape)
+    t.shape = tuple(k.shape[1:]), token_start.shape[0]
+    t.keep = (k, v, token_start)
+    return t
+
+
+def _same_cache(cache, tokens):
+    if tokens.shape != ((cache.kv_heads, cache.head_dim), cache.sequences + 1):
+        raise ValueError("tokens of other heads, another head_dim or another number of sequences than the cache")
+
+
+def szo_kv_cache_write(cache, tokens, stream=None):
+    _same_cache(cache, tokens)
+    _check("szo_kv_cache_write", lib.szo_kv_cache_write(C.byref(cache), C.byref(tokens), _stream(stream)))
+
+
+def szo_kv_cache_read(cache, tokens, stream=None):
+    _same_cache(cache, tokens)
+    _check("szo_kv_cache_read", lib.szo_kv_cache_read(C.byref(cache), C.byref(tokens), _stream(stream)))
+
+
+def make_attn_desc(cache, q, out, q_start, max_q, max_len, scale, causal=True, window=0, lse=None):
+    """cache from make_kv_cache(); q, out bf16 or fp16 [tokens, q_heads, head_dim]; lse fp32 [tokens, q_heads] or None."""
+    import torch
+    if out.dtype != q.dtype:
+        raise ValueError("queries and output are of one type")
+    T, heads, D = q.shape
+    if D != cache.head_dim:
+        raise ValueError(f"queries of head_dim {D}, a cache of {cache.head_dim}")
+    d = AttnDesc(cache, heads, _type(q), int(causal), window, scale, max_q, max_len, 0, T)
+    d.q, d.q_token_stride, d.q_head_stride = _strided(q, q.shape)
+    d.q_start = _typed(q_start, torch.int32, (cache.sequences + 1,))
+    d.out, d.out_token_stride, d.out_head_stride = _strided(out, q.shape)
+    d.lse = _typed(lse, torch.float32, (T, heads))
+    d.keep = (cache, q, out, q_start, lse)
+    return d
+
+
+def szo_attn_cached(desc, workspace=None, stream=None):
+    _check("szo_attn_cached", lib.szo_attn_cached(C.byref(desc), _dev(workspace), _stream(stream)))
+
+
+def szo_attn_workspace_bytes(desc):
+    return int(lib.szo_attn_workspace_bytes(C.byref(desc)))
+
+
+def make_logprobs_desc(logits, targets=None, logp=None, entropy=None, stats=None, top_logp=None, top_index=None, scale=1.0, loss_acc=None, loss_scale=1.0):
+    """logits [rows, vocab], rows any distance apart; targets i32 [rows]; outputs that are None are not computed."""
+    import torch
+    R, V = logits.shape
+    if not logits.is_cuda or (V > 1 and logits.stride(1) != 1):
+        raise ValueError("expected device logits with contiguous rows")
+    some = top_index if top_index is not None else top_logp
+    top = 0 if some is None else some.shape[1]
+    d = LogprobsDesc(R, V, logits.stride(0), _type(logits), top, scale, 0, logits.data_ptr(), _typed(targets, torch.int32, (R,)),
+                     _typed(logp, torch.float32, (R,)), _typed(entropy, torch.float32, (R,)), _typed(stats, torch.float32, (R, 2)),
+                     _typed(top_logp, torch.float32, (R, top)), _typed(top_index, torch.int32, (R, top)),
+                     None if loss_acc is None else _typed(loss_acc, torch.float64, loss_acc.shape), loss_scale)
+    d.keep = (logits, targets, logp, entropy, stats, top_logp, top_index, loss_acc)
+    return d
+
+
+def szo_token_logprobs(desc, workspace=None, stream=None):
+    _check("szo_token_logprobs", lib.szo_token_logprobs(C.byref(desc), _dev(workspace), _stream(stream)))
+
+
+def szo_logprobs_workspace_bytes(desc):
+    return int(lib.szo_logprobs_workspace_bytes(C.byref(desc)))
+
+
+def szo_token_logprobs_bwd(desc, grad_logp, grad_entropy, grad_logits, stream=None):
+    """grad_logp, grad_entropy fp32 [rows] or None; grad_logits like the logits, or the logits themselves."""
+    import torch
+    R, V = desc.rows, desc.vocab
+    if not grad_logits.is_cuda or tuple(grad_logits.shape) != (R, V) or _type(grad_logits) != desc.type or (V > 1 and grad_logits.stride(1) != 1):
+        raise ValueError("expected a gradient of the logits' shape and type")
+    _check("szo_token_logprobs_bwd", lib.szo_token_logprobs_bwd(C.byref(desc), _typed(grad_logp, torch.float32, (R,)), _typed(grad_entropy, torch.float32, (R,)),
+                                                                grad_logits.data_ptr(), grad_logits.stride(0), _stream(stream)))
 
 
 # ---- host set-up -----------------------------------------------------------------------------
