@@ -3,12 +3,15 @@
 //   s = scale q k,  p = exp(s) where the query sees the key,  out = sum p v / sum p,  in one pass with a running maximum.
 //
 // A wave takes 32 query rows (a token's query heads of one key head are rows too: they share its keys) and walks blocks of 32 cached
-// tokens.  It computes S^T = K Q^T and O^T = V^T P^T in products of 32x32x16: in the result of the first a lane has one query row and 16 of
+// tokens.  It computes S^T = K Q^T and O^T = V^T P^T in products of 32 x 32: in the result of the first a lane has one query row and 16 of
 // the 32 tokens, which is just what the second takes as an operand, so the weights never leave their lane, and the row's maximum is
-// one lane exchange away.  The cache is laid out as the two left operands: 16 bytes of a lane are its codes for two products.
-//   Numbers: codes are exact in bf16 and fp16.  Keys' exponents go into the factor of the scores.  Values' exponents go into the exponent of the
-// weights: with x = log2(e) s + v_exp the running maximum is over x, sum 2^(x - m) code is the output's numerator and
-// sum 2^(x - m) 2^-v_exp the denominator, so that the weights, rounded to fp16, are relative to the largest contribution of the row.
+// one lane exchange away.  The cache is laid out as the two left operands: 16 bytes of a lane are its codes.
+//   Scores: codes become bf16 or fp16, like the queries, exactly; the block's exponent goes into the factor of its scores.  (The matrix cores'
+// 8-bit products would take the codes as they are, with a query in two or three 8-bit parts; but they add up to fewer than fp32's bits:
+// scores of 20 were off by 1e-4.)
+//   Values: codes become fp16, exactly; weights are rounded to fp16.  A block's exponent goes into the exponent of its weights: with
+// x = log2(e) s + v_exp the running maximum is over x, sum 2^(x - m) code is the output's numerator and sum 2^(x - m) 2^-v_exp the
+// denominator, so that the weights are relative to the largest contribution of the row.
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_kv.h"
@@ -16,56 +19,95 @@
 namespace szo {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kThreads = 256;              // of the joining kernel
 constexpr float kNone = -1e30f;            // running maximum of a row that has seen nothing
-constexpr float kSlack = 8.f;              // the maximum may fall behind by this many binary places before sums are scaled: weights up to 2^8 fit fp16
+constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
+constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
 
 struct AttnArgs {
   szo_attn_desc d;
   int group, blocks_per_page;              // query heads per key head
   int tiles, splits, rows_cap;             // row tiles of a workgroup, parts of the cache, rows kept per wave tile in partial sums
-  float to_log2;                           // scale * log2(e)
+  float to_log2;                           // |scale| * log2(e)
+  bool negate;                             // scale < 0: queries change sign
   float* partial;                          // [sequence][key head][wave tile][split][rows_cap][head_dim + 2]
   bool vec_q, vec_out;
-};
-
-struct Rows {
-  int n, start, length, first;             // queries of the sequence, its first row of q, its length, first row of the wave's 32
-  int count;                               // rows of the sequence for this key head
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <int D> struct Raw { uint4 w[D / 32]; };
 
-template <int D>
-__device__ __forceinline__ Raw<D> load_block(const uint8_t* codes, int64_t block, int lane) {
+// ONCE: nobody else reads it, so it may pass the caches by.
+template <int D, bool ONCE>
+__device__ __forceinline__ Raw<D> load_block(const uint8_t* codes, int block, int lane) {
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
   Raw<D> r;
-  const uint4* p = reinterpret_cast<const uint4*>(codes + block * (D * kKvBlock)) + (lane % 32) * 2 + lane / 32;
+  const words* p = reinterpret_cast<const words*>(codes + (int64_t)block * (D * kKvBlock)) + (lane % 32) * 2 + lane / 32;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) r.w[i] = p[i * 64];
+  for (int i = 0; i < D / 32; ++i) {
+    words w;
+    if constexpr (ONCE) w = __builtin_nontemporal_load(p + i * 64);
+    else w = p[i * 64];
+    r.w[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
   return r;
 }
 
-template <int TYPE> struct Half;
-template <> struct Half<SZO_BF16> {
+// Eight codes as fp16.
+__device__ __forceinline__ f16x8 halves(uint32_t lo, uint32_t hi) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ f32x16 product(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Operands of the scores, in the queries' type.
+template <int TYPE> struct Score;
+template <> struct Score<SZO_BF16> {
   typedef bf16x8 vec;
   static __device__ __forceinline__ vec codes(uint32_t lo, uint32_t hi) {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
     return vec{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
-  static __device__ __forceinline__ f32x16 product(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 add(vec k, vec q, f32x16 s) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q, s, 0, 0, 0); }
 };
-template <> struct Half<SZO_F16> {
+template <> struct Score<SZO_F16> {
   typedef f16x8 vec;
-  static __device__ __forceinline__ vec codes(uint32_t lo, uint32_t hi) {
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
-    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-    return vec{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-  }
-  static __device__ __forceinline__ f32x16 product(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ vec codes(uint32_t lo, uint32_t hi) { return halves(lo, hi); }
+  static __device__ __forceinline__ f32x16 add(vec k, vec q, f32x16 s) { return product(k, q, s); }
 };
+
+// A lane's row of queries, in the order of the features that a block of keys has: 32 s + 16 half + 8 u .. + 7.
+template <int TYPE, int D> struct Query {
+  typename Score<TYPE>::vec part[D / 32][2];
+  __device__ __forceinline__ void load(const void* base, int64_t at, bool valid, bool aligned, bool negate, int half) {
+    typedef typename Score<TYPE>::vec vec;
+    const auto* p = static_cast<const typename TypeOf<TYPE>::type*>(base) + at + 16 * half;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        vec x = {};
+        if (valid) {
+          if (aligned) x = *reinterpret_cast<const vec*>(p + 32 * s + 8 * u);
+          else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[32 * s + 8 * u + i];
+        }
+        uint4 w = __builtin_bit_cast(uint4, x);
+        const uint32_t flip = negate ? 0x80008000u : 0u;
+        w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
+        part[s][u] = __builtin_bit_cast(vec, w);
+      }
+  }
+};
+
+// Factor of a block's scores, in powers of two; never 0, so that masked ones stay -inf.
+__device__ __forceinline__ float score_factor(float to_log2, int key_exp) {
+  return fmaxf(to_log2 * power_of_two(min(max(key_exp - kExpBias, kExpMin), kExpMax)), 1e-37f);
+}
 
 // max and sum of a value and its other half's (lane +- 32)
 __device__ __forceinline__ float halves_max(float v) {
@@ -86,12 +128,59 @@ __device__ __forceinline__ float halves_sum(float v) {
 // 0x80 in each byte of w that is the code of NaN
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
-// WR waves side by side over rows, WK = 4 / WR over the cache.
-template <int TYPE, int D, int WR>
-__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel(const AttnArgs a) {
-  typedef Half<TYPE> H;
-  typedef typename H::vec vec;
-  constexpr int WK = kWaves / WR, E = D / 32;
+// Where a sequence's blocks lie, walked forward: the page table is read one step before the block's codes are asked for.
+struct Walk {
+  int page_at, sub;
+  __device__ __forceinline__ Walk(int block, int blocks_per_page) : page_at(block / blocks_per_page), sub(block - page_at * blocks_per_page) {}
+  __device__ __forceinline__ void step(int by, int blocks_per_page) {
+    sub += by;
+    while (sub >= blocks_per_page) { sub -= blocks_per_page; ++page_at; }
+  }
+  // Number of the block in the cache; -1: no page.  Below the sequence's length, so inside the page table.
+  __device__ __forceinline__ int at(const szo_kv_cache& c, const int32_t* table, int head, int blocks_per_page) const {
+    const int page = table[page_at];
+    return (uint32_t)page >= (uint32_t)c.pages ? -1 : (page * c.kv_heads + head) * blocks_per_page + sub;
+  }
+};
+
+// A lane's half of a row: finished, or as this split's partial sum.
+template <int TYPE, int D>
+__device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
+                                        int token, int q_head, int column, int half) {
+  const szo_attn_desc& d = a.d;
+  if (a.splits > 1) {
+    float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * a.rows_cap * (D + 2);
+    float* mine = to + (int64_t)column * D;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
+    if (half == 0) {
+      to[(int64_t)a.rows_cap * D + 2 * column] = m;
+      to[(int64_t)a.rows_cap * D + 2 * column + 1] = l;
+    }
+    return;
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  const int64_t at = (int64_t)token * d.out_token_stride + (int64_t)q_head * d.out_head_stride;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float y[4] = {o[e][i] * by, o[e][i + 1] * by, o[e][i + 2] * by, o[e][i + 3] * by};
+      if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at + 32 * e + 2 * i + 4 * half, y);
+      else store_f32<TYPE, 4, false>(d.out, at + 32 * e + 2 * i + 4 * half, y);
+    }
+  if (d.lse && half == 0) d.lse[(int64_t)token * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
+}
+
+// WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
+//   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
+// one step do not depend on each other.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192, registers run out).
+template <int TYPE, int D, int WR, int WK, bool ONCE>
+__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const AttnArgs a) {
+  constexpr int E = D / 32;
   const szo_attn_desc& d = a.d;
   const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), column = lane % 32, half = lane / 32;
   // key heads vary fastest: workgroups are dealt out to the 8 XCDs in turn, so the row tiles of one key head share an L2
@@ -104,113 +193,91 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel
   const int wave_tile = tile * WR + wave % WR, walker = wave / WR;
   const int start = max(d.q_start[sequence], 0), stop = (int)min((int64_t)d.q_start[sequence + 1], d.tokens);
   const int n = max(0, min(stop - start, d.max_q));
-  const int length = (int)max((int64_t)0, min((int64_t)d.cache.lengths[sequence], (int64_t)d.cache.max_pages * d.cache.page_tokens));
-  const int whole = d.cache.lengths[sequence], rows = n * a.group, first_row = wave_tile * 32;
+  const int whole = d.cache.lengths[sequence];
+  const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)d.cache.max_pages * d.cache.page_tokens));
+  const int rows = n * a.group, first_row = wave_tile * 32;
   if (tile * WR * 32 >= rows) return;                    // the workgroup as a whole
-  const bool active = first_row < rows;
+  const int behind = whole - (stop - start);             // position of the sequence's first query
 
   // this lane's row
   const int row = first_row + column, query = row / a.group, q_head = head * a.group + row % a.group;
   const bool valid = row < rows;
-  const int behind = whole - (stop - start);             // position of the sequence's first query
-  const int position = behind + query;
-  const int see_to = !valid ? 0 : d.causal ? min(length, position + 1) : length;
-  const int see_from = d.window > 0 ? position - d.window + 1 : 0;
+  const int see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
+  const int see_from = d.window > 0 ? behind + query - d.window + 1 : 0;
+  Query<TYPE, D> q;
+  q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
 
-  vec q[E][2];
-  if (active) {
-    const int64_t at = (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride;
-#pragma unroll
-    for (int s = 0; s < E; ++s)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        vec x = {};
-        if (valid) {
-          const auto* p = static_cast<const typename TypeOf<TYPE>::type*>(d.q) + at + 32 * s + 16 * half + 8 * u;
-          if (a.vec_q) x = *reinterpret_cast<const vec*>(p);
-          else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[i];
-        }
-        q[s][u] = x;
-      }
-  }
-
-  // blocks that some row of the wave's tile sees, the part of them that is this split's, and this wave's share of that
+  // blocks that some row of the wave sees, the part of them that is this split's, and this wave's share of that
   const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
-  const int reach = d.causal ? min(length, pos_last + 1) : length;
-  const int lo = d.window > 0 ? max(0, pos_first - d.window + 1) / kKvBlock : 0, hi = active && reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
+  const int reach = first_row >= rows || d.cache.pages == 0 ? 0 : d.causal ? min(length, pos_last + 1) : length;
+  const int lo = d.window > 0 ? max(0, pos_first - d.window + 1) / kKvBlock : 0, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
   const int share = (max(hi - lo, 0) + a.splits - 1) / a.splits;
   const int j0 = lo + split * share + walker, j1 = min(hi, lo + (split + 1) * share);
   const int see_all = d.causal ? min(length, pos_first + 1) : length;     // tokens before this one are seen by every row, but for the window
   const int see_all_from = d.window > 0 ? pos_last - d.window + 1 : 0;
 
-  f32x16 o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = f32x16{};
+  f32x16 o[E], s = {};
   float m = kNone, l = 0.f;
+  uint32_t poison[(E + 1) / 2];            // one bit for each of the lane's sums: it is NaN
+#pragma unroll
+  for (int e = 0; e < E; ++e) { o[e] = f32x16{}; poison[e / 2] = 0; }
 
-  int64_t block = j0 < j1 ? block_of(d.cache, sequence, j0, head, a.blocks_per_page) : -1;
-  Raw<D> k;
-  if (block >= 0) k = load_block<D>(d.cache.k, block, lane);
-  for (int j = j0; j < j1; j += WK) {
-    const int64_t next = j + WK < j1 ? block_of(d.cache, sequence, j + WK, head, a.blocks_per_page) : -1;
-    if (block >= 0) {
-      Raw<D> v = load_block<D>(d.cache.v, block, lane);
-      const int ke = (int)d.cache.k_exp[block] - kExpBias, ve = (int)d.cache.v_exp[block] - kExpBias;
-      f32x16 s = {};
+  if (j0 < j1) {
+    // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
+    const int bpp = a.blocks_per_page;
+    const int32_t* table = d.cache.page_table + (int64_t)sequence * d.cache.max_pages;
+    Walk walk(j0, bpp);
+    int now = walk.at(d.cache, table, head, bpp), next = now;
+    if (j0 + WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+    auto known = [](int b) { return max(b, 0); };
+    auto scores = [&](const Raw<D>& k) {
+      s = f32x16{};
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        s = H::product(H::codes(k.w[i].x, k.w[i].y), q[i][0], s);
-        s = H::product(H::codes(k.w[i].z, k.w[i].w), q[i][1], s);
+        s = Score<TYPE>::add(Score<TYPE>::codes(k.w[i].x, k.w[i].y), q.part[i][0], s);
+        s = Score<TYPE>::add(Score<TYPE>::codes(k.w[i].z, k.w[i].w), q.part[i][1], s);
       }
-      if (next >= 0) k = load_block<D>(d.cache.k, next, lane);
-      const float factor = a.to_log2 * power_of_two(min(max(ke, kExpMin), kExpMax)), shift = (float)min(max(ve, kExpMin), kExpMax);
-      const float unshift = power_of_two(-min(max(ve, kExpMin), kExpMax));
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], factor, shift);
-      const int token = j * kKvBlock + 4 * half;           // of x[0]; x[i] is 8 (i / 4) + i % 4 further
-      const bool all = (j + 1) * kKvBlock <= see_all && j * kKvBlock >= see_all_from;
+    };
+    Raw<D> k = load_block<D, ONCE>(d.cache.k, known(now), lane), v = load_block<D, ONCE>(d.cache.v, known(now), lane);
+    int ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)];
+    scores(k);
+    k = load_block<D, ONCE>(d.cache.k, known(next), lane);
+    for (int j = j0; j < j1; j += WK) {        // k: keys of the next step, v: values of this one
+      const bool there = now >= 0;
+      now = next;
+      if (j + 2 * WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+      const float factor = score_factor(a.to_log2, ke);
+      const int vexp = min(max(ve - kExpBias, kExpMin), kExpMax);
+      const float shift = (float)vexp, unshift = power_of_two(-vexp);
+      ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)];
+      const int token = j * kKvBlock + 4 * half, to = there ? see_to - token : 0, from = see_from - token;      // of s[0]; s[i] is 8 (i / 4) + i % 4 further
+      const bool all = there && (j + 1) * kKvBlock <= see_all && j * kKvBlock >= see_all_from;
       if (!all) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int t = token + 8 * (i / 4) + i % 4;
-          x[i] = t < see_to && t >= see_from ? x[i] : -__builtin_inff();
+          const int at = 8 * (i / 4) + i % 4;
+          s[i] = at < to && at >= from ? s[i] : -__builtin_inff();
         }
       }
-      float most = x[0];
+      float most = s[0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) most = fmaxf(most, x[i]);
-      most = halves_max(most);
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+      most = fmaf(halves_max(most), factor, shift);
       if (__any(most > m + kSlack)) {
-        const float to = fmaxf(m, most), scale = exp2f(m - to);
-        m = to;
+        const float top = fmaxf(m, most), scale = __builtin_amdgcn_exp2f(m - top);
+        m = top;
         l *= scale;
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[e][i] *= scale;
       }
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) { x[i] = __builtin_amdgcn_exp2f(x[i] - m); sum += x[i]; }
-      l = fmaf(sum, unshift, l);
-      f16x8 p[2];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = (_Float16)x[i];
       if (!all) {
         // A masked token's weight is 0, and 0 times NaN would be NaN: such codes are taken out, and the rows that do see them get their NaN
         uint32_t bad = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) bad |= nan_codes(v.w[e].x) | nan_codes(v.w[e].y) | nan_codes(v.w[e].z) | nan_codes(v.w[e].w);
         if (__any(bad != 0)) {
-          f16x8 seen[2];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = token + 8 * (i / 4) + i % 4;
-            seen[i / 8][i % 8] = t < see_to && t >= see_from ? (_Float16)1.f : (_Float16)0.f;
-          }
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             uint32_t w[4] = {v.w[e].x, v.w[e].y, v.w[e].z, v.w[e].w}, mark[4];
@@ -221,25 +288,58 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel
               mark[c] = ones * 0x38u;                      // the code of 1
             }
             v.w[e] = make_uint4(w[0], w[1], w[2], w[3]);
-            f32x16 hits = {};
-            hits = Half<SZO_F16>::product(Half<SZO_F16>::codes(mark[0], mark[1]), seen[0], hits);
-            hits = Half<SZO_F16>::product(Half<SZO_F16>::codes(mark[2], mark[3]), seen[1], hits);
+            f16x8 seen[2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[e][i] = hits[i] > 0.f ? __builtin_nanf("") : o[e][i];
+            for (int i = 0; i < 16; ++i) {
+              const int at = 8 * (i / 4) + i % 4;
+              seen[i / 8][i % 8] = at < to && at >= from ? (_Float16)1.f : (_Float16)0.f;
+            }
+            f32x16 hits = {};
+            hits = product(halves(mark[0], mark[1]), seen[0], hits);
+            hits = product(halves(mark[2], mark[3]), seen[1], hits);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) poison[e / 2] |= hits[i] > 0.f ? 1u << (e % 2 * 16 + i) : 0u;
           }
         }
       }
+      // Half of the weights beside the scores, the other half beside the first half of the output: there are vector instructions for every product to run beside
+      // (all of them first: 576 us instead of 556 for a prompt of 8192).
+      f16x8 p[2];
+      const float base = shift - m + kLift;
+      float sum = 0.f;
+      const f32x16 x = s;
+      auto weigh = [&](int c) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        o[e] = Half<SZO_F16>::product(Half<SZO_F16>::codes(v.w[e].x, v.w[e].y), p[0], o[e]);
-        o[e] = Half<SZO_F16>::product(Half<SZO_F16>::codes(v.w[e].z, v.w[e].w), p[1], o[e]);
-      }
-    } else if (next >= 0) {
-      k = load_block<D>(d.cache.k, next, lane);
+        for (int i = 0; i < 8; ++i) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[8 * c + i], factor, base));
+          sum += w;
+          p[c][i] = (_Float16)w;
+        }
+      };
+      weigh(0);
+      scores(k);
+      if (WK == 1) k = load_block<D, ONCE>(d.cache.k, known(next), lane);       // one path of instructions up to here: no condition
+      weigh(1);
+      l = fmaf(sum, unshift, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = product(halves(v.w[e].x, v.w[e].y), p[0], o[e]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = product(halves(v.w[e].z, v.w[e].w), p[1], o[e]);
+      if (WK == 1 || j + WK < j1) v = load_block<D, ONCE>(d.cache.v, known(now), lane);
+      if (WK > 1 && j + 2 * WK < j1) k = load_block<D, ONCE>(d.cache.k, known(next), lane);
     }
-    block = next;
   }
+
   l = halves_sum(l);
+  uint32_t any = 0;
+#pragma unroll
+  for (int e = 0; e < E; e += 2) any |= poison[e / 2];
+  if (__any(any != 0)) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[e][i] = poison[e / 2] >> (e % 2 * 16 + i) & 1 ? __builtin_nanf("") : o[e][i];
+  }
 
   if constexpr (WK > 1) {
     // the walkers' sums meet in the first one's registers
@@ -260,7 +360,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel
     float top = m;
 #pragma unroll
     for (int w = 1; w < WK; ++w) top = fmaxf(top, meet[((w - 1) * WR + wave % WR) * kPer + D / 2 * 64 + lane]);
-    const float scale = exp2f(m - top);
+    const float scale = __builtin_amdgcn_exp2f(m - top);
+    m = top;
     l *= scale;
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -269,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel
 #pragma unroll
     for (int w = 1; w < WK; ++w) {
       const float* from = meet + ((w - 1) * WR + wave % WR) * kPer;
-      const float part = exp2f(from[D / 2 * 64 + lane] - top);
+      const float part = __builtin_amdgcn_exp2f(from[D / 2 * 64 + lane] - top);
       l = fmaf(from[D / 2 * 64 + 64 + lane], part, l);
 #pragma unroll
       for (int e = 0; e < E; ++e)
@@ -282,37 +383,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) attn_cached_kernel
           o[e][i + 3] = fmaf(x.w, part, o[e][i + 3]);
         }
     }
-    m = top;
   }
-  if (!valid) return;
-
-  if (a.splits > 1) {
-    const int64_t tiles = (int64_t)a.tiles * WR;
-    float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * a.rows_cap * (D + 2);
-    float* mine = to + (int64_t)column * D;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
-    if (half == 0) {
-      to[(int64_t)a.rows_cap * D + 2 * column] = m;
-      to[(int64_t)a.rows_cap * D + 2 * column + 1] = l;
-    }
-    return;
-  }
-  const float by = l == 0.f ? 0.f : 1.f / l;
-  const int64_t at = (int64_t)(start + query) * d.out_token_stride + (int64_t)q_head * d.out_head_stride;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float y[4] = {o[e][i] * by, o[e][i + 1] * by, o[e][i + 2] * by, o[e][i + 3] * by};
-      if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at + 32 * e + 2 * i + 4 * half, y);
-      else store_f32<TYPE, 4, false>(d.out, at + 32 * e + 2 * i + 4 * half, y);
-    }
-  if (d.lse && half == 0)
-    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.693147180559945309f;
+  if (valid) put_row<TYPE, D>(a, o, m, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, start + query, q_head, column, half);
 }
 
 // Joins the parts of a row: one workgroup per sequence, key head and wave tile, D / 4 lanes a row.
@@ -347,24 +419,36 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, i
     if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
     else store_f32<TYPE, 4, false>(d.out, at, y);
     if (d.lse && f == 0)
-      d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.693147180559945309f;
+      d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
+// How rows and cache go to waves.
+//   Four waves of a workgroup take rows side by side (wr 4) or share the cache of one tile of 32 rows (wr 1), and meet in LDS.  Side by side from
+// 2048 tiles on, which fill the chip's 2048 waves by themselves, or from half of that where there is no cache to share, eight blocks at most.  us of
+// one pass, 32 query and 8 key heads of 128, side by side / shared: one prompt of 1024 tokens (1032 tiles) 28 / 22, of 2048 55 / 57, 4 of 512 27 / 32,
+// 4 of 1024 59 / 76, 16 of 256 34 / 52, 16 of 64 10.0 / 14.9.
+//   With few workgroups a tile's cache is split over several, two workgroups a CU if every wave keeps two blocks, and a second kernel joins the parts; long
+// caches of uneven sequences are split once more, while waves keep 24 blocks.  us of one token each behind n tokens, 1, 2, 4, 8, 16, 32 parts: 1 sequence of 1000
+// 11.8, 11.0, 9.6, 9.5, 10.8, 13.3; 1 of 8000 75, 43, 26, 18, 14.9, 15.3; 8 of 4000 43, 28, 19.2, 18.8, 23, 37; 16 of 8000 83, 51, 47, 52, 59, 76; 64 of 1000
+// 27, 33, 38, 55, 87, 156; 64 of 500 to 8192 112, 108.
 struct Plan { int wr, tiles, splits, rows_cap; };
 
 Plan plan_of(const szo_attn_desc* d) {
   Plan p;
-  const int64_t rows = (int64_t)d->max_q * (d->q_heads / d->cache.kv_heads);
-  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  const int64_t group = d->q_heads / d->cache.kv_heads, rows = (int64_t)d->max_q * group;
+  const int64_t pairs = (int64_t)d->cache.sequences * d->cache.kv_heads;
+  const int64_t blocks = ((int64_t)std::max(d->max_len, 1) + kKvBlock - 1) / kKvBlock;
+  // tiles of 32 rows that hold something, about: a sequence's last one is partly filled
+  const int64_t held = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((rows + 31) / 32)) * d->cache.kv_heads;
+  p.wr = rows > 32 && (held >= 2048 || (held >= 1024 && blocks <= 8)) ? 4 : 1;
   p.tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
   p.rows_cap = (int)std::min<int64_t>(32, rows);
-  const int64_t base = (int64_t)d->cache.sequences * d->cache.kv_heads * p.tiles;
-  const int64_t blocks = ((int64_t)std::max(d->max_len, 1) + kKvBlock - 1) / kKvBlock;
-  const int64_t most = std::max<int64_t>(1, blocks / (kWaves / p.wr));
-  p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / base), std::min<int64_t>(most, 64));
+  const int64_t base = pairs * p.tiles, walkers = 4 / p.wr;
+  const int64_t fill = std::min(512 / base, blocks / (2 * walkers)), even = std::min(1024 / base, blocks / (24 * walkers));
+  p.splits = (int)std::min<int64_t>(std::max<int64_t>({1, fill, even}), 64);
   return p;
 }
 
@@ -384,21 +468,22 @@ int check(const szo_attn_desc* d) {
   if (d->q_token_stride < 0 || d->q_head_stride < 0 || (d->tokens > 1 && d->out_token_stride < c.head_dim) || (d->q_heads > 1 && d->out_head_stride < c.head_dim))
     return SZO_EINVAL;
   if ((int64_t)d->max_q * (d->q_heads / c.kv_heads) > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
+  if ((int64_t)c.pages * c.kv_heads * (c.page_tokens / kKvBlock) > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
   const Plan p = plan_of(d);
   if ((int64_t)c.sequences * c.kv_heads * p.tiles * p.wr * p.splits > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
   return SZO_OK;
 }
 bool nothing(const szo_attn_desc* d) { return d->cache.sequences == 0 || d->q_heads == 0 || d->tokens == 0 || d->max_q == 0; }
 
-template <int TYPE, int D, int WR>
+template <int TYPE, int D, int WR, int WK, bool ONCE>
 int launch(const AttnArgs& a, int64_t groups, hipStream_t s) {
-  constexpr size_t lds = WR == kWaves ? 0 : (size_t)(kWaves - WR) * 64 * (D / 2 + 2) * sizeof(float);
+  constexpr size_t lds = (size_t)WR * (WK - 1) * 64 * (D / 2 + 2) * sizeof(float);
   static std::atomic<uint64_t> raised{0};
   if (lds > 64 * 1024) {
-    const int rc = set_lds_limit_once(raised, (const void*)attn_cached_kernel<TYPE, D, WR>, lds);
+    const int rc = set_lds_limit_once(raised, (const void*)attn_walk_kernel<TYPE, D, WR, WK, ONCE>, lds);
     if (rc != SZO_OK) return rc;
   }
-  attn_cached_kernel<TYPE, D, WR><<<dim3((unsigned)groups), kThreads, lds, s>>>(a);
+  attn_walk_kernel<TYPE, D, WR, WK, ONCE><<<dim3((unsigned)groups), 64 * WR * WK, lds, s>>>(a);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }
@@ -406,7 +491,11 @@ int launch(const AttnArgs& a, int64_t groups, hipStream_t s) {
 template <int TYPE, int D>
 int launch_all(const AttnArgs& a, const Plan& p, hipStream_t s) {
   const int64_t groups = (int64_t)a.d.cache.sequences * a.d.cache.kv_heads * p.tiles * p.splits;
-  const int rc = p.wr == 1 ? launch<TYPE, D, 1>(a, groups, s) : p.wr == 2 ? launch<TYPE, D, 2>(a, groups, s) : launch<TYPE, D, 4>(a, groups, s);
+  int rc;
+  // with one tile of rows a block is read by one workgroup only: 64 sequences of up to 8192 tokens 124 -> 112 us (108 in two parts), 5.7 TB/s
+  if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, groups, s);
+  else if (p.tiles == 1) rc = launch<TYPE, D, 1, 4, true>(a, groups, s);
+  else rc = launch<TYPE, D, 1, 4, false>(a, groups, s);
   if (rc != SZO_OK || p.splits == 1) return rc;
   attn_join_kernel<TYPE, D><<<dim3((unsigned)(groups / p.splits * p.wr)), kThreads, 0, s>>>(a, p.tiles * p.wr);
   SZO_LAUNCH_CHECK();
@@ -450,7 +539,8 @@ int szo_attn_cached(const szo_attn_desc* d, void* workspace, void* stream) {
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.rows_cap = p.rows_cap;
-  a.to_log2 = d->scale * 1.44269504088896341f;
+  a.to_log2 = (d->scale < 0.f ? -d->scale : d->scale) * 1.44269504088896341f;
+  a.negate = d->scale < 0.f;
   a.partial = (float*)workspace;
   a.vec_q = aligned_to(d->q, 16) && d->q_token_stride % 8 == 0 && d->q_head_stride % 8 == 0;
   a.vec_out = aligned_to(d->out, 8) && d->out_token_stride % 4 == 0 && d->out_head_stride % 4 == 0;

@@ -24,6 +24,9 @@ __device__ __forceinline__ int64_t block_of(const szo_kv_cache& c, int sequence,
 // 2^e for |e| <= 126.
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+__device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) < __builtin_inff() ? x : __builtin_nanf(""); }
+__device__ __forceinline__ float finite_size(float x) { const float a = fabsf(x); return a < __builtin_inff() ? a : 0.f; }
+
 int check_cache(const szo_kv_cache* c);      // szo_kvcache.hip
 
 }  // namespace szo

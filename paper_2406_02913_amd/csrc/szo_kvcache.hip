@@ -45,9 +45,6 @@ struct Share {
   }
 };
 
-__device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) < __builtin_inff() ? x : __builtin_nanf(""); }
-__device__ __forceinline__ float finite_size(float x) { const float a = fabsf(x); return a < __builtin_inff() ? a : 0.f; }
-
 __device__ __forceinline__ int exponent_for(float most) {
   const uint32_t b = __float_as_uint(most);
   // most = m 2^x, m in [1, 2): 448 = 1.75 * 2^8; values below the normal range end at the lower limit anyway
