@@ -4,8 +4,10 @@
 //   gradient = scale (g ([v = target] - p) - h p (log p + entropy)),  p = exp(u) / S
 //
 // Bound by reading the logits: once, with a running maximum and two running sums in every thread.  The alternatives cost the stream nothing:
-// the threads' own maxima are there already, and the top-th largest of them is a lower bound of the top-th largest logit that
-// only the elements of as many threads can reach.  Those threads' elements (about top / 512 of the row) are read again, from cache, and ranked.
+// the threads' own maxima are there already.  The top-th largest among the maxima of groups of 16 threads bounds the top-th largest logit from below, and
+// few others reach it (of 64 groups, 24 logits for 20 alternatives): the threads whose maximum does look through their elements again, and what they
+// find is ranked.
+// With few rows a row is split over workgroups, whose parts a second kernel joins.
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_types.h"
@@ -13,9 +15,9 @@
 namespace szo {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kCandidates = 1024;
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kMostParts = 32;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.402823466e38f;
 
 // 16 bytes of logits at any element; gfx950 loads them at any address.
@@ -38,21 +40,22 @@ template <int TYPE> struct Chunk {
   static __device__ __forceinline__ float one(const void* base, int64_t at) { return (float)static_cast<const T*>(base)[at]; }
 };
 
-// Running statistics: sums relative to the maximum so far, which starts at the lowest finite value so that differences stay defined.
+// Running statistics in powers of two, u = (x - m) scale log2(e): relative to the maximum so far, which starts at the lowest finite value so that
+// differences stay defined.
 struct Running {
-  float m, s, t;                     // maximum, sum exp(u), sum u exp(u)
+  float m, s, t;                     // maximum, sum 2^u, sum u 2^u
   __device__ Running() : m(kLowest), s(0.f), t(0.f) {}
   // to a maximum that is not smaller
   __device__ void rebase(float to, float scale) {
-    const float du = (m - to) * scale, f = exp2f(du * kLog2e);
-    t = f * (t + (du > -200.f ? du : -200.f) * s);             // u becomes u + du; below -200 the factor is 0 anyway
+    const float du = (m - to) * scale, f = __builtin_amdgcn_exp2f(du);
+    t = f * fmaf(fmaxf(du, -300.f), s, t);                     // u becomes u + du; below -300 the factor is 0 anyway
     s *= f;
     m = to;
   }
   __device__ void add(float x, float scale) {
-    const float u = (x - m) * scale, e = exp2f(u * kLog2e);
+    const float u = (x - m) * scale, e = __builtin_amdgcn_exp2f(u);
     s += e;
-    t = fmaf(e, fmaxf(u, -200.f), t);                          // -inf: 0 times a finite number
+    t = fmaf(e, fmaxf(u, -300.f), t);                          // -inf: 0 times a finite number
   }
 };
 
@@ -62,152 +65,169 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ uint64_t key_of(float x, int index) { return (uint64_t)order_of(x) << 32 | (uint32_t)~index; }
+__device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t k = (uint32_t)(key >> 32);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);         // 0xFFFFFFFF is a NaN as well
+}
 
-struct LogpArgs { szo_logprobs_desc d; };
+// Parts of rows: statistics [row][part][3], then the keys of the part's best [row][part][top], 0 where there are fewer.
+struct LogpArgs { szo_logprobs_desc d; int parts; float* stats; uint64_t* best; };
 
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogpArgs a) {
+// A row's results, from its statistics.
+struct Finish {
+  float m, s, log_s, scale;
+  bool empty;
+  __device__ Finish(float m_, float s_, float scale_) : m(m_), s(s_), log_s(logf(s_)), scale(scale_), empty(s_ == 0.f) {}     // a row of -inf alone: s is 0
+  __device__ float logp(float x) const { return empty ? -__builtin_inff() : (x - m) * scale - log_s; }
+  template <int TYPE>
+  __device__ void write(const szo_logprobs_desc& d, int64_t row, float t) const {
+    const int target = d.targets ? d.targets[row] : -1;
+    if (d.logp) d.logp[row] = target >= 0 && target < d.vocab ? logp(Chunk<TYPE>::one(d.logits, row * d.row_stride + target)) : 0.f;
+    if (d.entropy) d.entropy[row] = empty ? 0.f : log_s - t / s * kLn2;
+    if (d.stats) { d.stats[2 * row] = empty ? -__builtin_inff() : m; d.stats[2 * row + 1] = s; }
+  }
+  __device__ void put(const szo_logprobs_desc& d, int64_t row, int rank, uint64_t key) const {
+    if (d.top_logp) d.top_logp[row * d.top + rank] = logp(value_of(key));
+    if (d.top_index) d.top_index[row * d.top + rank] = index_of(key);
+  }
+};
+
+// THREADS and U: threads of a workgroup and 16-byte pieces that each has on the way.
+template <int TYPE, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs a) {
   typedef Chunk<TYPE> C;
-  constexpr int N = C::N;
+  constexpr int N = C::N, kWaves = THREADS / 64;
   __shared__ float red[3][kWaves];
-  __shared__ float maxima[kThreads];
+  __shared__ __attribute__((aligned(16))) float maxima[THREADS / 16];
   __shared__ uint64_t found[kCandidates];
-  __shared__ int count, winners, more;
-  __shared__ float bound;
-  __shared__ short winner[kThreads];
+  __shared__ int count, winners;
+  __shared__ short winner[THREADS];
   const szo_logprobs_desc& d = a.d;
-  const int64_t row = blockIdx.x, from = row * d.row_stride;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int vocab = (int)d.vocab, chunks = vocab / N;
+  const int64_t row = blockIdx.x / a.parts, from = row * d.row_stride;
+  const int part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int vocab = (int)d.vocab, all = vocab / N, share = (all + a.parts - 1) / a.parts;
+  const int c0 = min(all, part * share), chunks = min(all, (part + 1) * share);        // this part's pieces; the last part has what is behind them
+  const float scale = d.scale * kLog2e;
   Running r;
-  int c = tid;
-  constexpr int U = 4;
-  for (; c + (U - 1) * kThreads < chunks; c += U * kThreads) {
-    float v[U][N];
+  float v[U][N];
+  for (int c = c0 + tid; c < chunks; c += U * THREADS) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) C::load(d.logits, from + (int64_t)(c + i * kThreads) * N, v[i]);
+    for (int i = 0; i < U; ++i) C::load(d.logits, from + (int64_t)min(c + i * THREADS, chunks - 1) * N, v[i]);
     float most = r.m;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const bool in = c + i * THREADS < chunks;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        v[i][n] = in ? v[i][n] : -__builtin_inff();
+        most = fmaxf(most, v[i][n]);
+      }
+    }
+    r.rebase(most, scale);
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int n = 0; n < N; ++n) most = fmaxf(most, v[i][n]);
-    r.rebase(most, d.scale);
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int n = 0; n < N; ++n) r.add(v[i][n], d.scale);
+      for (int n = 0; n < N; ++n) r.add(v[i][n], scale);
   }
-  for (; c < chunks; c += kThreads) {
-    float v[N];
-    C::load(d.logits, from + (int64_t)c * N, v);
-    float most = r.m;
-#pragma unroll
-    for (int n = 0; n < N; ++n) most = fmaxf(most, v[n]);
-    r.rebase(most, d.scale);
-#pragma unroll
-    for (int n = 0; n < N; ++n) r.add(v[n], d.scale);
-  }
-  const int tail = chunks * N + tid;                           // fewer than N elements
+  const int tail = part == a.parts - 1 ? all * N + tid : vocab;                        // fewer than N elements
   if (tail < vocab) {
     const float x = C::one(d.logits, from + tail);
-    r.rebase(fmaxf(r.m, x), d.scale);
-    r.add(x, d.scale);
+    r.rebase(fmaxf(r.m, x), scale);
+    r.add(x, scale);
   }
-  maxima[tid] = r.m;
-  float m = lanes_max<64>(r.m);
+  const float own = r.m;
+  float m = lanes_max<16>(own);
+  if (lane % 16 == 0) maxima[tid / 16] = m;
+  m = lanes_max<64>(own);
   if (lane == 0) red[0][wave] = m;
+  if (tid == 0) { count = 0; winners = 0; }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) m = fmaxf(m, red[0][w]);
-  r.rebase(m, d.scale);
+  r.rebase(m, scale);
   float s = lanes_sum<64>(r.s), t = lanes_sum<64>(r.t);
   if (lane == 0) { red[1][wave] = s; red[2][wave] = t; }
-  if (tid == 0) { count = 0; winners = 0; more = 0; }
   __syncthreads();
   s = t = 0.f;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) { s += red[1][w]; t += red[2][w]; }
-  const float log_s = logf(s);                                 // a row of -inf alone: s is 0
-  const bool empty = s == 0.f;
+  const Finish f(m, s, d.scale);
   if (tid == 0) {
-    const int target = d.targets ? d.targets[row] : -1;
-    if (d.logp) {
-      float y = 0.f;
-      if (target >= 0 && target < vocab) y = empty ? -__builtin_inff() : (C::one(d.logits, from + target) - m) * d.scale - log_s;
-      d.logp[row] = y;
+    if (a.parts == 1) f.write<TYPE>(d, row, t);
+    else {
+      float* to = a.stats + (row * a.parts + part) * 3;
+      to[0] = m; to[1] = s; to[2] = t;
     }
-    if (d.entropy) d.entropy[row] = empty ? 0.f : log_s - t / s;
-    if (d.stats) { d.stats[2 * row] = empty ? -__builtin_inff() : m; d.stats[2 * row + 1] = s; }
   }
   const int top = d.top;
   if (!top || !(d.top_logp || d.top_index)) return;
 
-  auto put = [&](int rank, float x, int index) {
-    if (d.top_logp) d.top_logp[row * top + rank] = empty ? -__builtin_inff() : (x - m) * d.scale - log_s;
-    if (d.top_index) d.top_index[row * top + rank] = index;
+  auto put = [&](int rank, uint64_t key) {
+    if (a.parts == 1) f.put(d, row, rank, key);
+    else a.best[(row * a.parts + part) * top + rank] = key;
   };
-  const bool plain = s - s == 0.f && !empty;                   // NaN or infinite logits make s NaN
+  const bool plain = s - s == 0.f && !f.empty;                 // NaN or infinite logits make s NaN
   if (plain) {
-    // the top-th largest of the threads' maxima, by halving in one wave
-    if (wave == 0) {
-      uint32_t key[kWaves];
+    // the smallest of the groups' maxima that fewer than top of them exceed; every wave for itself
+    constexpr int kGroups = THREADS / 16;
+    const float mine = maxima[lane % kGroups];
+    int above = 0;
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) key[i] = order_of(maxima[i * 64 + lane]);
-      uint32_t lo = 0, hi = order_of(m);                       // at least top keys are >= lo
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo + 1) / 2;
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) n += __popcll(__ballot(key[i] >= mid));
-        if (n >= top) lo = mid; else hi = mid - 1;
-        if (n == top) break;
-      }
-      if (lane == 0) bound = __uint_as_float(lo & 0x80000000u ? lo & 0x7FFFFFFFu : ~lo);
+    for (int i = 0; i < kGroups; i += 4) {
+      const float4 g = *reinterpret_cast<const float4*>(maxima + i);
+      above += (g.x > mine) + (g.y > mine) + (g.z > mine) + (g.w > mine);
     }
-    __syncthreads();
-    const float least = bound;
-    if (maxima[tid] >= least) winner[atomicAdd(&winners, 1)] = (short)tid;
-    __syncthreads();
-    const int per = (chunks + kThreads - 1) / kThreads, items = winners * per;
-    for (int i = tid; i < items; i += kThreads) {
-      const int at = winner[i / per] + i % per * kThreads;
-      if (at >= chunks) continue;
-      float v[N];
-      C::load(d.logits, from + (int64_t)at * N, v);
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-        if (v[n] >= least) {
-          const int to = atomicAdd(&count, 1);
-          if (to < kCandidates) found[to] = (uint64_t)order_of(v[n]) << 32 | (uint32_t)~(at * N + n);
-        }
-    }
-    if (tail < vocab) {
-      const float x = C::one(d.logits, from + tail);
+    const float least = -lanes_max<64>(above < top ? -mine : -__builtin_inff());
+    auto take = [&](float x, int index) {
       if (x >= least) {
         const int to = atomicAdd(&count, 1);
-        if (to < kCandidates) found[to] = (uint64_t)order_of(x) << 32 | (uint32_t)~tail;
+        if (to < kCandidates) found[to] = key_of(x, index);
+      }
+    };
+    if (chunks - c0 <= U * THREADS) {                          // still in registers
+      if (own >= least) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (c0 + tid + i * THREADS < chunks)
+#pragma unroll
+            for (int n = 0; n < N; ++n) take(v[i][n], (c0 + tid + i * THREADS) * N + n);
+      }
+    } else {
+      if (own >= least) winner[atomicAdd(&winners, 1)] = (short)tid;
+      __syncthreads();
+      const int per = (chunks - c0 + THREADS - 1) / THREADS, items = winners * per;
+      for (int i = tid; i < items; i += THREADS) {
+        const int at = c0 + winner[i / per] + i % per * THREADS;
+        if (at >= chunks) continue;
+        float y[N];
+        C::load(d.logits, from + (int64_t)at * N, y);
+#pragma unroll
+        for (int n = 0; n < N; ++n) take(y[n], at * N + n);
       }
     }
+    if (tail < vocab) take(C::one(d.logits, from + tail), tail);
     __syncthreads();
-    if (count >= top && count <= kCandidates) {      // fewer: most of the row is -inf
-      for (int i = tid; i < count; i += kThreads) {
+    if (count >= top && count <= kCandidates) {
+      for (int i = tid; i < count; i += THREADS) {
         const uint64_t mine = found[i];
+        const int n = count;
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += found[j] > mine;
-        if (rank < top) {
-          const int index = (int)~(uint32_t)mine;
-          put(rank, C::one(d.logits, from + index), index);
-        }
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += found[j] > mine;
+        if (rank < top) put(rank, mine);
       }
       return;
     }
   }
-  // Rows with NaN, infinities or very many equal logits: one pass over the row for each alternative.
+  // Rows with NaN, infinities, very many equal logits or fewer finite ones than are asked for: one pass for each alternative.
+  const int begin = c0 * N, end = part == a.parts - 1 ? vocab : chunks * N;
   uint64_t last = ~0ull;
   for (int rank = 0; rank < top; ++rank) {
     uint64_t best = 0;
-    for (int i = tid; i < vocab; i += kThreads) {
-      const uint64_t key = (uint64_t)order_of(C::one(d.logits, from + i)) << 32 | (uint32_t)~i;
+    for (int i = begin + tid; i < end; i += THREADS) {
+      const uint64_t key = key_of(C::one(d.logits, from + i), i);
       if (key < last && key > best) best = key;
     }
 #pragma unroll
@@ -220,11 +240,38 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogpArgs
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) best = found[w] > best ? found[w] : best;
-    if (tid == 0) {
-      const int index = (int)~(uint32_t)best;
-      put(rank, C::one(d.logits, from + index), index);
-    }
+    if (tid == 0) put(rank, best);                             // 0 where the part has no further element
     last = best;
+  }
+}
+
+// Parts of a row to its results: one workgroup a row.
+template <int TYPE>
+__global__ void __launch_bounds__(256) token_logprobs_join_kernel(const LogpArgs a) {
+  __shared__ uint64_t keys[kMostParts * SZO_LOGPROBS_MAX_TOP];
+  const szo_logprobs_desc& d = a.d;
+  const int64_t row = blockIdx.x;
+  const float* part = a.stats + row * a.parts * 3;
+  const float scale = d.scale * kLog2e;
+  Running r;
+  for (int i = 0; i < a.parts; ++i) r.m = fmaxf(r.m, part[3 * i]);
+  for (int i = 0; i < a.parts; ++i) {
+    Running p;
+    p.m = part[3 * i]; p.s = part[3 * i + 1]; p.t = part[3 * i + 2];
+    p.rebase(r.m, scale);
+    r.s += p.s;
+    r.t += p.t;
+  }
+  const Finish f(r.m, r.s, d.scale);
+  if (threadIdx.x == 0) f.write<TYPE>(d, row, r.t);
+  if (!d.top || !(d.top_logp || d.top_index)) return;
+  const int n = a.parts * d.top;
+  for (int i = threadIdx.x; i < n; i += 256) keys[i] = a.best[row * n + i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += keys[j] > keys[i];
+    if (rank < d.top && keys[i]) f.put(d, row, rank, keys[i]);
   }
 }
 
@@ -264,7 +311,7 @@ __global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const 
   const float by = 1.f / s, log_s = logf(s), entropy = a.g_entropy ? d.entropy[row] : 0.f;
   const int64_t from = row * d.row_stride, to = row * a.out_stride;
   auto gradient = [&](float x, int v) {
-    const float u = (x - m) * d.scale, p = exp2f(u * kLog2e) * by;
+    const float u = (x - m) * d.scale, p = __builtin_amdgcn_exp2f(u * kLog2e) * by;
     float y = -g * p;
     if (a.g_entropy) y = fmaf(-h * p, fmaxf(u, -200.f) - log_s + entropy, y);
     if (v == target) y += g;
@@ -299,6 +346,26 @@ int check(const szo_logprobs_desc* d) {
   return SZO_OK;
 }
 
+// Few rows: 1024 threads and eight pieces each, 128 KiB on the way at once, and the row in parts where that is not all of it and the chip has room.
+struct Plan { bool few; int parts; };
+Plan plan_of(const szo_logprobs_desc* d) {
+  Plan p;
+  p.few = d->rows <= 256;
+  const int64_t pieces = d->vocab * (int64_t)type_bytes(d->type) / 16, batch = 1024 * (d->type == SZO_F32 ? 8 : 4);
+  p.parts = !p.few || d->rows == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({(pieces + batch - 1) / batch, 512 / d->rows, kMostParts}));
+  return p;
+}
+size_t best_at(const szo_logprobs_desc* d, const Plan& p) { return ((size_t)d->rows * p.parts * 3 * sizeof(float) + 15) / 16 * 16; }
+
+template <int TYPE>
+void launch(const LogpArgs& a, const Plan& p, hipStream_t s) {
+  constexpr int U = TYPE == SZO_F32 ? 8 : 4;
+  const dim3 grid((unsigned)(a.d.rows * p.parts));
+  if (p.few) token_logprobs_kernel<TYPE, 1024, U><<<grid, 1024, 0, s>>>(a);
+  else token_logprobs_kernel<TYPE, 512, 4><<<grid, 512, 0, s>>>(a);
+  if (p.parts > 1) token_logprobs_join_kernel<TYPE><<<dim3((unsigned)a.d.rows), 256, 0, s>>>(a);
+}
+
 }  // namespace
 }  // namespace szo
 
@@ -307,23 +374,24 @@ using namespace szo;
 extern "C" {
 
 size_t szo_logprobs_workspace_bytes(const szo_logprobs_desc* d) {
-  (void)d;
-  return 16;
+  if (check(d) != SZO_OK) return 16;
+  const Plan p = plan_of(d);
+  return p.parts == 1 ? 16 : best_at(d, p) + (size_t)d->rows * p.parts * d->top * sizeof(uint64_t);
 }
 
 int szo_token_logprobs(const szo_logprobs_desc* d, void* workspace, void* stream) {
-  (void)workspace;
   const int rc = check(d);
   if (rc != SZO_OK) return rc;
   if (d->loss_acc && !d->logp) return SZO_EINVAL;
   if (d->rows == 0) return SZO_OK;
   if (d->vocab == 0) return SZO_EINVAL;
+  const Plan p = plan_of(d);
+  if (p.parts > 1 && (!workspace || !aligned_to(workspace, 16))) return SZO_EINVAL;
   hipStream_t s = (hipStream_t)stream;
-  const LogpArgs a = {*d};
-  const dim3 grid((unsigned)d->rows);
-  if (d->type == SZO_F32) token_logprobs_kernel<SZO_F32><<<grid, kThreads, 0, s>>>(a);
-  else if (d->type == SZO_BF16) token_logprobs_kernel<SZO_BF16><<<grid, kThreads, 0, s>>>(a);
-  else token_logprobs_kernel<SZO_F16><<<grid, kThreads, 0, s>>>(a);
+  const LogpArgs a = {*d, p.parts, (float*)workspace, p.parts > 1 ? (uint64_t*)((char*)workspace + best_at(d, p)) : nullptr};
+  if (d->type == SZO_F32) launch<SZO_F32>(a, p, s);
+  else if (d->type == SZO_BF16) launch<SZO_BF16>(a, p, s);
+  else launch<SZO_F16>(a, p, s);
   SZO_LAUNCH_CHECK();
   if (d->loss_acc) {
     logp_loss_kernel<<<1, 1024, 0, s>>>(d->logp, d->targets, d->rows, d->vocab, d->loss_scale, d->loss_acc);
