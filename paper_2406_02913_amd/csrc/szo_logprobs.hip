@@ -4,8 +4,8 @@
 //   gradient = scale (g ([v = target] - p) - h p (log p + entropy)),  p = exp(u) / S
 //
 // Bound by reading the logits: once, with a running maximum and two running sums in every thread.  The alternatives cost the stream nothing:
-// the threads' own maxima are there already.  The top-th largest among the maxima of groups of 16 threads bounds the top-th largest logit from below, and
-// few others reach it (of 64 groups, 24 logits for 20 alternatives): the threads whose maximum does look through their elements again, and what they
+// the threads' own maxima are there already.  The top-th largest among the maxima of groups of 8 threads bounds the top-th largest logit from below, and
+// few others reach it (of 32 groups, 31 logits for 20 alternatives): the threads whose maximum does look through their elements again, and what they
 // find is ranked.
 // With few rows a row is split over workgroups, whose parts a second kernel joins.
 #include <algorithm>
@@ -16,6 +16,7 @@ namespace szo {
 namespace {
 
 constexpr int kCandidates = 1024;
+constexpr int kThreads = 256;
 constexpr int kMostParts = 32;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.402823466e38f;
@@ -94,16 +95,17 @@ struct Finish {
   }
 };
 
-// THREADS and U: threads of a workgroup and 16-byte pieces that each has on the way.
-template <int TYPE, int THREADS, int U>
-__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs a) {
+// 256 threads with four pieces each on the way.  4096 rows of 32000 in fp32: 95 us with 20 alternatives (5.5 TB/s), 89 without; 512 threads 93 and 88, but
+// rows of 2000 43 instead of 24, of 8000 61 instead of 54.
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogpArgs a) {
   typedef Chunk<TYPE> C;
-  constexpr int N = C::N, kWaves = THREADS / 64;
+  constexpr int N = C::N, U = 4, kWaves = kThreads / 64, kGroups = kThreads / 8;      // U: pieces of a thread on the way; as many groups as alternatives
   __shared__ float red[3][kWaves];
-  __shared__ __attribute__((aligned(16))) float maxima[THREADS / 16];
+  __shared__ __attribute__((aligned(16))) float maxima[kGroups];
   __shared__ uint64_t found[kCandidates];
   __shared__ int count, winners;
-  __shared__ short winner[THREADS];
+  __shared__ short winner[kThreads];
   const szo_logprobs_desc& d = a.d;
   const int64_t row = blockIdx.x / a.parts, from = row * d.row_stride;
   const int part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -111,21 +113,26 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
   const int c0 = min(all, part * share), chunks = min(all, (part + 1) * share);        // this part's pieces; the last part has what is behind them
   const float scale = d.scale * kLog2e;
   Running r;
+  float own = kLowest, second = kLowest;                       // the largest logit of this thread, and of its other pieces
+  int piece = -1;                                              // where the largest is
   float v[U][N];
-  for (int c = c0 + tid; c < chunks; c += U * THREADS) {
+  for (int c = c0 + tid; c < chunks; c += U * kThreads) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) C::load(d.logits, from + (int64_t)min(c + i * THREADS, chunks - 1) * N, v[i]);
-    float most = r.m;
+    for (int i = 0; i < U; ++i) C::load(d.logits, from + (int64_t)min(c + i * kThreads, chunks - 1) * N, v[i]);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const bool in = c + i * THREADS < chunks;
+      const bool in = c + i * kThreads < chunks;
+      float here = -__builtin_inff();
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         v[i][n] = in ? v[i][n] : -__builtin_inff();
-        most = fmaxf(most, v[i][n]);
+        here = fmaxf(here, v[i][n]);
       }
+      second = fmaxf(second, fminf(own, here));
+      piece = here > own ? c + i * kThreads : piece;
+      own = fmaxf(own, here);
     }
-    r.rebase(most, scale);
+    r.rebase(own, scale);
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -137,9 +144,9 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
     r.rebase(fmaxf(r.m, x), scale);
     r.add(x, scale);
   }
-  const float own = r.m;
-  float m = lanes_max<16>(own);
-  if (lane % 16 == 0) maxima[tid / 16] = m;
+  own = r.m;                                                   // its element behind the pieces among them
+  float m = lanes_max<8>(own);
+  if (lane % 8 == 0) maxima[tid / 8] = m;
   m = lanes_max<64>(own);
   if (lane == 0) red[0][wave] = m;
   if (tid == 0) { count = 0; winners = 0; }
@@ -171,7 +178,6 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
   const bool plain = s - s == 0.f && !f.empty;                 // NaN or infinite logits make s NaN
   if (plain) {
     // the smallest of the groups' maxima that fewer than top of them exceed; every wave for itself
-    constexpr int kGroups = THREADS / 16;
     const float mine = maxima[lane % kGroups];
     int above = 0;
 #pragma unroll
@@ -186,22 +192,28 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
         if (to < kCandidates) found[to] = key_of(x, index);
       }
     };
-    if (chunks - c0 <= U * THREADS) {                          // still in registers
+    if (chunks - c0 <= U * kThreads) {                          // still in registers
       if (own >= least) {
 #pragma unroll
         for (int i = 0; i < U; ++i)
-          if (c0 + tid + i * THREADS < chunks)
+          if (c0 + tid + i * kThreads < chunks)
 #pragma unroll
-            for (int n = 0; n < N; ++n) take(v[i][n], (c0 + tid + i * THREADS) * N + n);
+            for (int n = 0; n < N; ++n) take(v[i][n], (c0 + tid + i * kThreads) * N + n);
       }
     } else {
-      if (own >= least) winner[atomicAdd(&winners, 1)] = (short)tid;
+      // most find one piece with such elements and know it; others look through all of theirs, together
+      float y[N];
+      if (own >= least && second >= least) winner[atomicAdd(&winners, 1)] = (short)tid;
+      else if (own >= least && piece >= 0) {
+        C::load(d.logits, from + (int64_t)piece * N, y);
+#pragma unroll
+        for (int n = 0; n < N; ++n) take(y[n], piece * N + n);
+      }
       __syncthreads();
-      const int per = (chunks - c0 + THREADS - 1) / THREADS, items = winners * per;
-      for (int i = tid; i < items; i += THREADS) {
-        const int at = c0 + winner[i / per] + i % per * THREADS;
+      const int per = (chunks - c0 + kThreads - 1) / kThreads, items = winners * per;
+      for (int i = tid; i < items; i += kThreads) {
+        const int at = c0 + winner[i / per] + i % per * kThreads;
         if (at >= chunks) continue;
-        float y[N];
         C::load(d.logits, from + (int64_t)at * N, y);
 #pragma unroll
         for (int n = 0; n < N; ++n) take(y[n], at * N + n);
@@ -210,7 +222,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
     if (tail < vocab) take(C::one(d.logits, from + tail), tail);
     __syncthreads();
     if (count >= top && count <= kCandidates) {
-      for (int i = tid; i < count; i += THREADS) {
+      for (int i = tid; i < count; i += kThreads) {
         const uint64_t mine = found[i];
         const int n = count;
         int rank = 0;
@@ -226,7 +238,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogpArgs 
   uint64_t last = ~0ull;
   for (int rank = 0; rank < top; ++rank) {
     uint64_t best = 0;
-    for (int i = begin + tid; i < end; i += THREADS) {
+    for (int i = begin + tid; i < end; i += kThreads) {
       const uint64_t key = key_of(C::one(d.logits, from + i), i);
       if (key < last && key > best) best = key;
     }
@@ -346,23 +358,20 @@ int check(const szo_logprobs_desc* d) {
   return SZO_OK;
 }
 
-// Few rows: 1024 threads and eight pieces each, 128 KiB on the way at once, and the row in parts where that is not all of it and the chip has room.
-struct Plan { bool few; int parts; };
+// With few rows a row goes to several workgroups, 64 KiB of it at least to each.  us of 1 / 16 / 64 rows of fp32 with 5 alternatives, whole and in parts:
+// vocabulary of 131072 17, 18, 25 -> 9.5, 10.1, 13.4; of 50257 9.4, 10.2, 12.5 -> 9.0, 9.8, 11.1; of 32000 7.2, 7.7, 8.2 whole, 8.0, 8.9, 9.3 in parts of 32 KiB.
+struct Plan { int parts; };
 Plan plan_of(const szo_logprobs_desc* d) {
   Plan p;
-  p.few = d->rows <= 256;
-  const int64_t pieces = d->vocab * (int64_t)type_bytes(d->type) / 16, batch = 1024 * (d->type == SZO_F32 ? 8 : 4);
-  p.parts = !p.few || d->rows == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({(pieces + batch - 1) / batch, 512 / d->rows, kMostParts}));
+  const int64_t pieces = d->vocab * (int64_t)type_bytes(d->type) / 16;
+  p.parts = d->rows == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({pieces / 4096, 512 / d->rows, kMostParts}));
   return p;
 }
 size_t best_at(const szo_logprobs_desc* d, const Plan& p) { return ((size_t)d->rows * p.parts * 3 * sizeof(float) + 15) / 16 * 16; }
 
 template <int TYPE>
 void launch(const LogpArgs& a, const Plan& p, hipStream_t s) {
-  constexpr int U = TYPE == SZO_F32 ? 8 : 4;
-  const dim3 grid((unsigned)(a.d.rows * p.parts));
-  if (p.few) token_logprobs_kernel<TYPE, 1024, U><<<grid, 1024, 0, s>>>(a);
-  else token_logprobs_kernel<TYPE, 512, 4><<<grid, 512, 0, s>>>(a);
+  token_logprobs_kernel<TYPE><<<dim3((unsigned)(a.d.rows * p.parts)), kThreads, 0, s>>>(a);
   if (p.parts > 1) token_logprobs_join_kernel<TYPE><<<dim3((unsigned)a.d.rows), 256, 0, s>>>(a);
 }
 
