@@ -143,20 +143,22 @@ struct Walk {
   }
 };
 
-// A lane's half of a row: finished, or as this split's partial sum.
-template <int TYPE, int D>
+// A lane's half of a row: finished, or as this split's partial sum.  Of WK waves each has the features 32 e .. + 31 with e = walker modulo WK.
+template <int TYPE, int D, int WK>
 __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
-                                        int token, int q_head, int column, int half) {
+                                        int walker, int token, int q_head, int column, int half) {
   const szo_attn_desc& d = a.d;
   if (a.splits > 1) {
     float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * a.rows_cap * (D + 2);
     float* mine = to + (int64_t)column * D;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
+    for (int e = 0; e < D / 32; ++e) {
+      if (e % WK != walker) continue;
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
         *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
-    if (half == 0) {
+    }
+    if (half == 0 && walker == 0) {
       to[(int64_t)a.rows_cap * D + 2 * column] = m;
       to[(int64_t)a.rows_cap * D + 2 * column + 1] = l;
     }
@@ -165,14 +167,16 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
   const float by = l == 0.f ? 0.f : 1.f / l;
   const int64_t at = (int64_t)token * d.out_token_stride + (int64_t)q_head * d.out_head_stride;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
+  for (int e = 0; e < D / 32; ++e) {
+    if (e % WK != walker) continue;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       const float y[4] = {o[e][i] * by, o[e][i + 1] * by, o[e][i + 2] * by, o[e][i + 3] * by};
       if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at + 32 * e + 2 * i + 4 * half, y);
       else store_f32<TYPE, 4, false>(d.out, at + 32 * e + 2 * i + 4 * half, y);
     }
-  if (d.lse && half == 0) d.lse[(int64_t)token * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
+  }
+  if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
 }
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   const int split = id % a.splits;
   id /= a.splits;
   const int tile = a.tiles - 1 - id % a.tiles, sequence = id / a.tiles;    // later rows see more: they start first
-  const int wave_tile = tile * WR + wave % WR, walker = wave / WR;
+  const int wave_tile = tile * WR + wave % WR, walker = WK == 1 ? 0 : wave / WR;
   const int start = max(d.q_start[sequence], 0), stop = (int)min((int64_t)d.q_start[sequence + 1], d.tokens);
   const int n = max(0, min(stop - start, d.max_q));
   const int whole = d.cache.lengths[sequence];
@@ -342,49 +346,55 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   }
 
   if constexpr (WK > 1) {
-    // the walkers' sums meet in the first one's registers
+    // the walkers' sums meet: each adds up every WK-th tile of 32 features (one of them all: 16 short answers 26.2 -> 25.8 us, one token behind 1000 10.3 -> 9.9)
     extern __shared__ __attribute__((aligned(16))) float meet[];
     constexpr int kPer = 64 * (D / 2 + 2);
-    if (walker > 0) {
-      float* to = meet + ((walker - 1) * WR + wave % WR) * kPer;
+    static_assert(WR == 1, "one tile of rows");
+    {
+      float* to = meet + walker * kPer;
 #pragma unroll
-      for (int e = 0; e < E; ++e)
+      for (int e = 0; e < E; ++e) {
+        if (e % WK == walker) continue;
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
           *reinterpret_cast<float4*>(to + (e * 4 + i / 4) * 256 + lane * 4) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
+      }
       to[D / 2 * 64 + lane] = m;
       to[D / 2 * 64 + 64 + lane] = l;
     }
     __syncthreads();
-    if (walker > 0) return;
-    float top = m;
+    float top = kNone, part[WK];
 #pragma unroll
-    for (int w = 1; w < WK; ++w) top = fmaxf(top, meet[((w - 1) * WR + wave % WR) * kPer + D / 2 * 64 + lane]);
-    const float scale = __builtin_amdgcn_exp2f(m - top);
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, meet[w * kPer + D / 2 * 64 + lane]);
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      part[w] = __builtin_amdgcn_exp2f(meet[w * kPer + D / 2 * 64 + lane] - top);
+      l = fmaf(meet[w * kPer + D / 2 * 64 + 64 + lane], part[w], l);
+    }
+    const float own = __builtin_amdgcn_exp2f(m - top);
     m = top;
-    l *= scale;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
+      if (e % WK != walker) continue;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[e][i] *= scale;
+      for (int i = 0; i < 16; ++i) o[e][i] *= own;
 #pragma unroll
-    for (int w = 1; w < WK; ++w) {
-      const float* from = meet + ((w - 1) * WR + wave % WR) * kPer;
-      const float part = __builtin_amdgcn_exp2f(from[D / 2 * 64 + lane] - top);
-      l = fmaf(from[D / 2 * 64 + 64 + lane], part, l);
-#pragma unroll
-      for (int e = 0; e < E; ++e)
+      for (int w = 0; w < WK; ++w) {
+        if (w == walker) continue;
+        const float* from = meet + w * kPer;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const float4 x = *reinterpret_cast<const float4*>(from + (e * 4 + i / 4) * 256 + lane * 4);
-          o[e][i] = fmaf(x.x, part, o[e][i]);
-          o[e][i + 1] = fmaf(x.y, part, o[e][i + 1]);
-          o[e][i + 2] = fmaf(x.z, part, o[e][i + 2]);
-          o[e][i + 3] = fmaf(x.w, part, o[e][i + 3]);
+          o[e][i] = fmaf(x.x, part[w], o[e][i]);
+          o[e][i + 1] = fmaf(x.y, part[w], o[e][i + 1]);
+          o[e][i + 2] = fmaf(x.z, part[w], o[e][i + 2]);
+          o[e][i + 3] = fmaf(x.w, part[w], o[e][i + 3]);
         }
+      }
     }
   }
-  if (valid) put_row<TYPE, D>(a, o, m, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, start + query, q_head, column, half);
+  if (valid) put_row<TYPE, D, WK>(a, o, m, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
 }
 
 // Joins the parts of a row: one workgroup per sequence, key head and wave tile, D / 4 lanes a row.
@@ -477,7 +487,7 @@ bool nothing(const szo_attn_desc* d) { return d->cache.sequences == 0 || d->q_he
 
 template <int TYPE, int D, int WR, int WK, bool ONCE>
 int launch(const AttnArgs& a, int64_t groups, hipStream_t s) {
-  constexpr size_t lds = (size_t)WR * (WK - 1) * 64 * (D / 2 + 2) * sizeof(float);
+  constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 2) * sizeof(float);
   static std::atomic<uint64_t> raised{0};
   if (lds > 64 * 1024) {
     const int rc = set_lds_limit_once(raised, (const void*)attn_walk_kernel<TYPE, D, WR, WK, ONCE>, lds);

@@ -234,3 +234,26 @@ def test_a_long_cache_behind_32_bits():
         off = (D / 8 + 8) * 2.0 ** -24 * 0.5 * float((q[0, h].abs().float().cpu().sum() * kv[0].abs().max().cpu())) * 1.5
         tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * off) * size + 2 * n * 2.0 ** -25 * float(vals.abs().max())
         assert ((out[0, h].double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("drop", [6.0, 12.0, 16.0])
+def test_many_small_weights_beside_a_large_one(drop):
+    """40000 tokens with weights of e^-drop beside one of 1: what they add up to keeps the precision of a single weight."""
+    n, D = 40000, 64
+    per = -(-n // 64)
+    k, v, ke, ve = szo.new_kv_cache(per, 64, 1, D)
+    lengths = torch.tensor([n], dtype=torch.int32, device=DEV)
+    cache = szo.make_kv_cache(k, v, ke, ve, torch.arange(per, dtype=torch.int32, device=DEV)[None], lengths)
+    start = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    keys, values = torch.zeros(n, 1, D, device=DEV), torch.ones(n, 1, D, device=DEV)
+    keys[777, 0, 0], values[777] = 16.0, 0.0
+    szo.szo_kv_cache_write(cache, szo.make_kv_tokens(keys, values, start, n))
+    q = torch.zeros(1, 1, D, device=DEV, dtype=torch.float16)
+    q[0, 0, 0] = 1.0
+    out, lse = torch.empty_like(q), torch.empty(1, 1, device=DEV)
+    d = szo.make_attn_desc(cache, q, out, torch.tensor([0, 1], dtype=torch.int32, device=DEV), 1, n, drop / 16, lse=lse)
+    szo.szo_attn_cached(d, torch.empty(szo.szo_attn_workspace_bytes(d), dtype=torch.uint8, device=DEV))
+    rest = (n - 1) * math.exp(-drop)
+    # a weight to 2^-11, the output to 2^-11, the sums of 40000 equal terms in chains of some hundreds in fp32
+    assert (out.double() - rest / (1 + rest)).abs().max().item() <= (2.0 ** -10 + 2.0 ** -14) * rest / (1 + rest)
+    assert abs(lse.item() - (drop + math.log1p(rest))) < 1e-5
