@@ -138,7 +138,9 @@ struct Walk {
   }
   // Number of the block in the cache; -1: no page.  Below the sequence's length, so inside the page table.
   __device__ __forceinline__ int at(const szo_kv_cache& c, const int32_t* table, int head, int blocks_per_page) const {
-    const int page = table[page_at];
+    return on(c, table[page_at], head, blocks_per_page);
+  }
+  __device__ __forceinline__ int on(const szo_kv_cache& c, int page, int head, int blocks_per_page) const {
     return (uint32_t)page >= (uint32_t)c.pages ? -1 : (page * c.kv_heads + head) * blocks_per_page + sub;
   }
 };
@@ -181,24 +183,24 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
 //   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
-// one step do not depend on each other.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192, registers run out).
+// one step do not depend on each other.  The arguments that the first loads need come first, where they are in registers when a wave starts; the page of the
+// first block is read along with the lengths, for the case that it starts there.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192, registers run out).
 template <int TYPE, int D, int WR, int WK, bool ONCE>
-__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
+                                                                                   int max_pages, int bpp, int splits, int tiles, const AttnArgs a) {
   constexpr int E = D / 32;
   const szo_attn_desc& d = a.d;
   const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), column = lane % 32, half = lane / 32;
   // key heads vary fastest: workgroups are dealt out to the 8 XCDs in turn, so the row tiles of one key head share an L2
-  int id = blockIdx.x;
-  const int head = id % d.cache.kv_heads;
-  id /= d.cache.kv_heads;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int tile = a.tiles - 1 - id % a.tiles, sequence = id / a.tiles;    // later rows see more: they start first
+  const int head = blockIdx.x, sequence = blockIdx.z;
+  const int split = splits == 1 ? 0 : blockIdx.y % splits;
+  const int tile = tiles - 1 - (splits == 1 ? blockIdx.y : blockIdx.y / splits);          // later rows see more: they start first
   const int wave_tile = tile * WR + wave % WR, walker = WK == 1 ? 0 : wave / WR;
-  const int start = max(d.q_start[sequence], 0), stop = (int)min((int64_t)d.q_start[sequence + 1], d.tokens);
+  const int32_t* table = page_table + (int64_t)sequence * max_pages;
+  const int whole = lengths[sequence], guess = max_pages > walker / bpp ? table[walker / bpp] : -1;
+  const int start = max(q_start[sequence], 0), stop = (int)min((int64_t)q_start[sequence + 1], d.tokens);
   const int n = max(0, min(stop - start, d.max_q));
-  const int whole = d.cache.lengths[sequence];
-  const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)d.cache.max_pages * d.cache.page_tokens));
+  const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
   const int rows = n * a.group, first_row = wave_tile * 32;
   if (tile * WR * 32 >= rows) return;                    // the workgroup as a whole
   const int behind = whole - (stop - start);             // position of the sequence's first query
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
   const int reach = first_row >= rows || d.cache.pages == 0 ? 0 : d.causal ? min(length, pos_last + 1) : length;
   const int lo = d.window > 0 ? max(0, pos_first - d.window + 1) / kKvBlock : 0, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
-  const int share = (max(hi - lo, 0) + a.splits - 1) / a.splits;
+  const int share = splits == 1 ? max(hi - lo, 0) : (max(hi - lo, 0) + splits - 1) / splits;
   const int j0 = lo + split * share + walker, j1 = min(hi, lo + (split + 1) * share);
   const int see_all = d.causal ? min(length, pos_first + 1) : length;     // tokens before this one are seen by every row, but for the window
   const int see_all_from = d.window > 0 ? pos_last - d.window + 1 : 0;
@@ -228,10 +230,8 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
 
   if (j0 < j1) {
     // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
-    const int bpp = a.blocks_per_page;
-    const int32_t* table = d.cache.page_table + (int64_t)sequence * d.cache.max_pages;
     Walk walk(j0, bpp);
-    int now = walk.at(d.cache, table, head, bpp), next = now;
+    int now = j0 == walker ? walk.on(d.cache, guess, head, bpp) : walk.at(d.cache, table, head, bpp), next = now;
     if (j0 + WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
     auto known = [](int b) { return max(b, 0); };
     auto scores = [&](const Raw<D>& k) {
@@ -399,21 +399,19 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
 
 // Joins the parts of a row: one workgroup per sequence, key head and wave tile, D / 4 lanes a row.
 template <int TYPE, int D>
-__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, int wave_tiles) {
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
   const szo_attn_desc& d = a.d;
-  int64_t id = blockIdx.x;
-  const float* from = a.partial + id * a.splits * a.rows_cap * (D + 2);
-  const int wave_tile = (int)(id % wave_tiles);
-  id /= wave_tiles;
-  const int head = (int)(id % d.cache.kv_heads), sequence = (int)(id / d.cache.kv_heads);
-  const int start = max(d.q_start[sequence], 0), stop = (int)min((int64_t)d.q_start[sequence + 1], d.tokens);
+  const int wave_tile = blockIdx.x, head = blockIdx.y, sequence = blockIdx.z;
+  const float* from = partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * rows_cap * (D + 2);
+  const int start = max(q_start[sequence], 0), stop = (int)min((int64_t)q_start[sequence + 1], d.tokens);
   const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
   for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
     const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
     float m = kNone, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-      const float* part = from + (int64_t)s * a.rows_cap * (D + 2);
-      const float ms = part[(int64_t)a.rows_cap * D + 2 * column], ls = part[(int64_t)a.rows_cap * D + 2 * column + 1];
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const float* part = from + (int64_t)s * rows_cap * (D + 2);
+      const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
       const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
       const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
       m = top;
@@ -480,34 +478,36 @@ int check(const szo_attn_desc* d) {
   if ((int64_t)d->max_q * (d->q_heads / c.kv_heads) > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
   if ((int64_t)c.pages * c.kv_heads * (c.page_tokens / kKvBlock) > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
   const Plan p = plan_of(d);
-  if ((int64_t)c.sequences * c.kv_heads * p.tiles * p.wr * p.splits > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
+  if ((int64_t)c.sequences * c.kv_heads * p.tiles * p.wr * p.splits > 0x7FFFFFFF || (int64_t)p.tiles * p.splits > 65535 || c.sequences > 65535) return SZO_EUNSUPPORTED;
   return SZO_OK;
 }
 bool nothing(const szo_attn_desc* d) { return d->cache.sequences == 0 || d->q_heads == 0 || d->tokens == 0 || d->max_q == 0; }
 
 template <int TYPE, int D, int WR, int WK, bool ONCE>
-int launch(const AttnArgs& a, int64_t groups, hipStream_t s) {
+int launch(const AttnArgs& a, hipStream_t s) {
   constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 2) * sizeof(float);
   static std::atomic<uint64_t> raised{0};
   if (lds > 64 * 1024) {
     const int rc = set_lds_limit_once(raised, (const void*)attn_walk_kernel<TYPE, D, WR, WK, ONCE>, lds);
     if (rc != SZO_OK) return rc;
   }
-  attn_walk_kernel<TYPE, D, WR, WK, ONCE><<<dim3((unsigned)groups), 64 * WR * WK, lds, s>>>(a);
+  const dim3 grid((unsigned)a.d.cache.kv_heads, (unsigned)(a.tiles * a.splits), (unsigned)a.d.cache.sequences);
+  attn_walk_kernel<TYPE, D, WR, WK, ONCE><<<grid, 64 * WR * WK, lds, s>>>(a.d.q_start, a.d.cache.lengths, a.d.cache.page_table, a.d.cache.max_pages, a.blocks_per_page,
+                                                                     a.splits, a.tiles, a);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }
 
 template <int TYPE, int D>
 int launch_all(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  const int64_t groups = (int64_t)a.d.cache.sequences * a.d.cache.kv_heads * p.tiles * p.splits;
   int rc;
   // with one tile of rows a block is read by one workgroup only: 64 sequences of up to 8192 tokens 124 -> 112 us (108 in two parts), 5.7 TB/s
-  if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, groups, s);
-  else if (p.tiles == 1) rc = launch<TYPE, D, 1, 4, true>(a, groups, s);
-  else rc = launch<TYPE, D, 1, 4, false>(a, groups, s);
+  if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, s);
+  else if (p.tiles == 1) rc = launch<TYPE, D, 1, 4, true>(a, s);
+  else rc = launch<TYPE, D, 1, 4, false>(a, s);
   if (rc != SZO_OK || p.splits == 1) return rc;
-  attn_join_kernel<TYPE, D><<<dim3((unsigned)(groups / p.splits * p.wr)), kThreads, 0, s>>>(a, p.tiles * p.wr);
+  const dim3 grid((unsigned)(p.tiles * p.wr), (unsigned)a.d.cache.kv_heads, (unsigned)a.d.cache.sequences);
+  attn_join_kernel<TYPE, D><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, p.tiles * p.wr, a.splits, a.rows_cap, a);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }

@@ -20,19 +20,18 @@ constexpr int kRow = kKvBlock + 4;         // bytes of a feature's row of values
 struct KvArgs {
   szo_kv_cache c;
   szo_kv_tokens t;
-  int blocks_per_page, touched;            // touched: most blocks that the new tokens of a sequence reach
+  int blocks_per_page;
 };
 
 // The block that a workgroup owns, and the tokens of it that the call is about: slots [first, end), slot s being row from + s.
 struct Share {
   int head, index, first, end;
   int64_t row, block;
-  __device__ bool find(const KvArgs& a) {
-    const int sequence = blockIdx.y;
-    head = blockIdx.x % a.c.kv_heads;
-    const int nth = blockIdx.x / a.c.kv_heads;
-    const int start = a.t.token_start[sequence], stop = a.t.token_start[sequence + 1];
-    const int64_t length = a.c.lengths[sequence], had = length - (int64_t)(stop - start);
+  __device__ bool find(const int32_t* token_start, const int32_t* lengths, const KvArgs& a) {
+    const int sequence = blockIdx.z, nth = blockIdx.y;
+    head = blockIdx.x;
+    const int start = token_start[sequence], stop = token_start[sequence + 1];
+    const int64_t length = lengths[sequence], had = length - (int64_t)(stop - start);
     if (stop <= start || length <= 0) return false;
     const int64_t at = (had > 0 ? had : 0) / kKvBlock + nth;             // tokens before position 0 have no place
     if (at * kKvBlock >= length) return false;
@@ -88,13 +87,13 @@ __device__ __forceinline__ void move_down(uint8_t* block, int first, int end, fl
   }
 }
 
-// VEC: groups of four features lie at multiples of their size.
+// What the first loads need comes first in the arguments, where it is in registers when a wave starts.  VEC: groups of four features lie at multiples of their size.
 template <int TYPE, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const KvArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const int32_t* token_start, const int32_t* lengths, const KvArgs a) {
   __shared__ float maxima[2][kThreads / 64];
   __shared__ __attribute__((aligned(16))) uint8_t tile[D * kRow];
   Share s;
-  if (!s.find(a) || s.block < 0) return;
+  if (!s.find(token_start, lengths, a) || s.block < 0) return;
   constexpr int kKeys = D * kKvBlock / 8, kValues = D * kKvBlock / 16;          // units: 8 features of a token; 4 features of 4 tokens
   constexpr int kPerK = (kKeys + kThreads - 1) / kThreads, kPerV = (kValues + kThreads - 1) / kThreads;
   float k[kPerK][8], v[kPerV][4][4];
@@ -185,10 +184,10 @@ __global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const KvArgs a
 }
 
 template <int TYPE, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const KvArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const int32_t* token_start, const int32_t* lengths, const KvArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[D * kRow];
   Share s;
-  if (!s.find(a)) return;
+  if (!s.find(token_start, lengths, a)) return;
   constexpr int kKeys = D * kKvBlock / 8, kValues = D * kKvBlock / 16;
   const bool there = s.block >= 0;
   const uint8_t* kb = a.c.k + (there ? s.block * (D * kKvBlock) : 0);
@@ -235,11 +234,11 @@ __global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const KvArgs a)
 template <int TYPE, int D>
 void launch_type(const KvArgs& a, dim3 grid, bool vec, bool write, hipStream_t s) {
   if (write) {
-    if (vec) kv_cache_write_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a);
-    else kv_cache_write_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a);
+    if (vec) kv_cache_write_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
+    else kv_cache_write_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
   } else {
-    if (vec) kv_cache_read_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a);
-    else kv_cache_read_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a);
+    if (vec) kv_cache_read_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
+    else kv_cache_read_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
   }
 }
 template <int D>
@@ -269,9 +268,8 @@ int move_tokens(const szo_kv_cache* c, const szo_kv_tokens* t, bool write, hipSt
   int64_t touched = (t->max_new + kKvBlock - 2) / kKvBlock + 1;
   if (write) touched = std::min(touched, room);
   if (touched == 0) return SZO_OK;
-  if (touched * c->kv_heads > 0x7FFFFFFF || c->sequences > 65535) return SZO_EUNSUPPORTED;
-  a.touched = (int)touched;
-  const dim3 grid((unsigned)(touched * c->kv_heads), (unsigned)c->sequences);
+  if (touched > 65535 || c->sequences > 65535) return SZO_EUNSUPPORTED;
+  const dim3 grid((unsigned)c->kv_heads, (unsigned)touched, (unsigned)c->sequences);
   const size_t four = 4 * type_bytes(t->type);
   const bool vec = aligned_to(t->k, four) && aligned_to(t->v, four) && t->k_token_stride % 4 == 0 && t->k_head_stride % 4 == 0 && t->v_token_stride % 4 == 0 &&
                    t->v_head_stride % 4 == 0;
