@@ -448,7 +448,8 @@ Plan plan_of(const szo_attn_desc* d) {
   Plan p;
   const int64_t group = d->q_heads / d->cache.kv_heads, rows = (int64_t)d->max_q * group;
   const int64_t pairs = (int64_t)d->cache.sequences * d->cache.kv_heads;
-  const int64_t blocks = ((int64_t)std::max(d->max_len, 1) + kKvBlock - 1) / kKvBlock;
+  const int64_t seen = d->window > 0 ? std::min<int64_t>(d->max_len, (int64_t)d->window + d->max_q) : d->max_len;       // tokens of a sequence, at most
+  const int64_t blocks = (std::max<int64_t>(seen, 1) + kKvBlock - 1) / kKvBlock;
   // tiles of 32 rows that hold something, about: a sequence's last one is partly filled
   const int64_t held = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((rows + 31) / 32)) * d->cache.kv_heads;
   p.wr = rows > 32 && (held >= 2048 || (held >= 1024 && blocks <= 8)) ? 4 : 1;

@@ -4,6 +4,7 @@ import os
 import subprocess
 
 import pytest
+import torch                                   # noqa: F401 -- before the library, as everywhere: both have to share one HIP runtime
 
 from paper_2406_02913_amd import szo
 
