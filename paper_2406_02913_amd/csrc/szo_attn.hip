@@ -184,7 +184,10 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
 //   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
 // one step do not depend on each other.  The arguments that the first loads need come first, where they are in registers when a wave starts; the page of the
-// first block is read along with the lengths, for the case that it starts there.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192, registers run out).
+// first block is read along with the lengths, for the case that it starts there.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192,
+// registers run out).
+//   A prompt of 8192 tokens with 32 query and 8 key heads of 128, causal: 570 us, 965 TFLOP/s, bound by the issue of instructions: matrix products take 45 % of
+// the cycles, and a step has 182 vector instructions beside 16 products.  One token of each of 64 sequences of up to 8192: 107 us, 5.76 TB/s of the cache.
 template <int TYPE, int D, int WR, int WK, bool ONCE>
 __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
                                                                                    int max_pages, int bpp, int splits, int tiles, const AttnArgs a) {
@@ -397,38 +400,49 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   if (valid) put_row<TYPE, D, WK>(a, o, m, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
 }
 
-// Joins the parts of a row: one workgroup per sequence, key head and wave tile, D / 4 lanes a row.
-template <int TYPE, int D>
+// Joins the parts of a row, four features of it at a time, by G neighbouring lanes: each takes every G-th part and they add each other up by row
+// permutations.  One lane, up to four parts on the way, for up to five parts and for full tiles, 16 lanes otherwise (1 sequence of 8000 in 32 parts 12.4 -> 10.5 us,
+// 32 rows of it in 8 parts 18.7 -> 19.2).  Workgroups go over sequences, key heads, wave tiles and a tile's pieces.
+template <int TYPE, int D, int G>
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
   const szo_attn_desc& d = a.d;
-  const int wave_tile = blockIdx.x, head = blockIdx.y, sequence = blockIdx.z;
+  const int wave_tile = blockIdx.x % wave_tiles, head = blockIdx.y, sequence = blockIdx.z;
   const float* from = partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * rows_cap * (D + 2);
   const int start = max(q_start[sequence], 0), stop = (int)min((int64_t)q_start[sequence + 1], d.tokens);
   const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
-    const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
-    float m = kNone, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-      const float* part = from + (int64_t)s * rows_cap * (D + 2);
-      const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
-      const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
-      const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
-      m = top;
-      l = l * keep + ls * add;
-      o[0] = o[0] * keep + x.x * add;
-      o[1] = o[1] * keep + x.y * add;
-      o[2] = o[2] * keep + x.z * add;
-      o[3] = o[3] * keep + x.w * add;
-    }
-    const float by = l == 0.f ? 0.f : 1.f / l;
-    const float y[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
-    const int64_t at = (int64_t)(start + query) * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
-    if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
-    else store_f32<TYPE, 4, false>(d.out, at, y);
-    if (d.lse && f == 0)
-      d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
+  const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
+  const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
+  if (column >= rows) return;                  // G lanes at once
+  float m = kNone, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAhead = G == 1 ? 4 : 2;
+#pragma unroll kAhead
+  for (int s = g; s < splits; s += G) {
+    const float* part = from + (int64_t)s * rows_cap * (D + 2);
+    const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
+    const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
+    m = top;
+    l = l * keep + ls * add;
+    o[0] = o[0] * keep + x.x * add;
+    o[1] = o[1] * keep + x.y * add;
+    o[2] = o[2] * keep + x.z * add;
+    o[3] = o[3] * keep + x.w * add;
   }
+  if constexpr (G > 1) {
+    const float top = lanes_max<G>(m), keep = exp2f(m - top);
+    m = top;
+    l = lanes_sum<G>(l * keep);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = lanes_sum<G>(o[k] * keep);
+    if (g) return;
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  const float y[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+  const int64_t at = (int64_t)(start + query) * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
+  if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
+  else store_f32<TYPE, 4, false>(d.out, at, y);
+  if (d.lse && f == 0)
+    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -436,13 +450,17 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
 // How rows and cache go to waves.
 //   Four waves of a workgroup take rows side by side (wr 4) or share the cache of one tile of 32 rows (wr 1), and meet in LDS.  Side by side from
 // 2048 tiles on, which fill the chip's 2048 waves by themselves, or from half of that where there is no cache to share, eight blocks at most.  us of
-// one pass, 32 query and 8 key heads of 128, side by side / shared: one prompt of 1024 tokens (1032 tiles) 28 / 22, of 2048 55 / 57, 4 of 512 27 / 32,
-// 4 of 1024 59 / 76, 16 of 256 34 / 52, 16 of 64 10.0 / 14.9.
-//   With few workgroups a tile's cache is split over several, two workgroups a CU if every wave keeps two blocks, and a second kernel joins the parts; long
-// caches of uneven sequences are split once more, while waves keep 24 blocks.  us of one token each behind n tokens, 1, 2, 4, 8, 16, 32 parts: 1 sequence of 1000
-// 11.8, 11.0, 9.6, 9.5, 10.8, 13.3; 1 of 8000 75, 43, 26, 18, 14.9, 15.3; 8 of 4000 43, 28, 19.2, 18.8, 23, 37; 16 of 8000 83, 51, 47, 52, 59, 76; 64 of 1000
-// 27, 33, 38, 55, 87, 156; 64 of 500 to 8192 112, 108.
-struct Plan { int wr, tiles, splits, rows_cap; };
+// one pass, 32 query and 8 key heads of 128, side by side / shared: one prompt of 1024 tokens (1032 tiles) 31 / 21, of 2048 54 / 57, 4 of 512 26 / 32,
+// 4 of 1024 57 / 76, 16 of 256 31 / 50, 16 of 64 7.9 / 13.1.
+//   With few workgroups a tile's cache is split over several, and a second kernel joins the parts.  That costs 2 us where a tile has few rows and 4 to 6
+// with 32, whose parts are 16 KiB each, and every workgroup 5 us to begin and to end: few rows go to up to 512 workgroups with a single block a wave (from 64
+// workgroups on with four), full tiles to 256 with four blocks a wave, and to twice as many of either only in caches of thousands.  us of parts 1, 2, 4, 8, 16, 32,
+// one token each: 1 sequence of 1000 10.3, 10.2, 8.6, 8.1, 8.1, 8.3; 1 of 8000 53, 33, 21, 14.7, 11.2, 9.6; 8 of 4000 35, 23, 17, 18, 20, 26; 16 of 8000 80, 49, 46,
+// 50, 56, 70; 32 of 1000 14, 18, 21; 64 of 500 to 8192 110, 106, 105.  64 tokens of one sequence (8 tiles for each key head) behind 2000 16.7, 15.8, 14.3, 18.6;
+// behind 8000 59, 38, 25, 24, 32; 200 tokens behind 4000 29, 32, 39, behind 8000 60, 47, 55.
+//   Blocks that one workgroup alone reads, 128 MiB of them or more, pass the caches by (once): 64 sequences of 500 to 8192 121 -> 106 us, 16 of 8000 52 -> 46,
+// 32 of 1000 (64 MiB) 14.2 -> 15.4.
+struct Plan { int wr, tiles, splits, rows_cap; bool once; };
 
 Plan plan_of(const szo_attn_desc* d) {
   Plan p;
@@ -455,8 +473,12 @@ Plan plan_of(const szo_attn_desc* d) {
   p.wr = rows > 32 && (held >= 2048 || (held >= 1024 && blocks <= 8)) ? 4 : 1;
   p.tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
   p.rows_cap = (int)std::min<int64_t>(32, rows);
-  const int64_t base = pairs * p.tiles, walkers = 4 / p.wr;
-  const int64_t fill = std::min(512 / base, blocks / (2 * walkers)), even = std::min(1024 / base, blocks / (24 * walkers));
+  p.once = p.wr == 1 && p.tiles == 1 && pairs * blocks * kKvBlock * 2 * d->cache.head_dim >= (int64_t)128 << 20;
+  const int64_t walkers = 4 / p.wr, some = std::max<int64_t>(1, std::min(held / p.wr, pairs * p.tiles));          // workgroups that hold something
+  const bool few = rows <= 16;
+  const bool single = few && some <= 64;                // a block a wave
+  const int64_t chip = few ? 512 : 256, step = single ? walkers : 4 * walkers, parts = blocks < (single ? 24 : 48) ? 1 : std::min<int64_t>((blocks + step - 1) / step, 32);
+  const int64_t fill = few && chip / some < 3 ? 1 : std::min(chip / some, parts), even = std::min(2 * chip / some, blocks / (walkers * (few ? 15 : 20)));
   p.splits = (int)std::min<int64_t>(std::max<int64_t>({1, fill, even}), 64);
   return p;
 }
@@ -499,18 +521,23 @@ int launch(const AttnArgs& a, hipStream_t s) {
   return SZO_OK;
 }
 
+template <int TYPE, int D, int G>
+int join(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  const int pieces = (a.rows_cap * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
+  const dim3 grid((unsigned)(p.tiles * p.wr * pieces), (unsigned)a.d.cache.kv_heads, (unsigned)a.d.cache.sequences);
+  attn_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, p.tiles * p.wr, a.splits, a.rows_cap, a);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
 template <int TYPE, int D>
 int launch_all(const AttnArgs& a, const Plan& p, hipStream_t s) {
   int rc;
-  // with one tile of rows a block is read by one workgroup only: 64 sequences of up to 8192 tokens 124 -> 112 us (108 in two parts), 5.7 TB/s
   if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, s);
-  else if (p.tiles == 1) rc = launch<TYPE, D, 1, 4, true>(a, s);
+  else if (p.once) rc = launch<TYPE, D, 1, 4, true>(a, s);
   else rc = launch<TYPE, D, 1, 4, false>(a, s);
   if (rc != SZO_OK || p.splits == 1) return rc;
-  const dim3 grid((unsigned)(p.tiles * p.wr), (unsigned)a.d.cache.kv_heads, (unsigned)a.d.cache.sequences);
-  attn_join_kernel<TYPE, D><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, p.tiles * p.wr, a.splits, a.rows_cap, a);
-  SZO_LAUNCH_CHECK();
-  return SZO_OK;
+  return p.splits < 6 || a.rows_cap > 16 ? join<TYPE, D, 1>(a, p, s) : join<TYPE, D, 16>(a, p, s);
 }
 
 template <int TYPE>

@@ -15,6 +15,7 @@ namespace szo {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / kThreads;     // a launch counts its threads in 32 bits
 constexpr int kBwdGroups = 1280;     // workgroups of a backward: what a chip holds at a time; each leaves one partial sum per feature
 
 struct QkArgs {
@@ -348,7 +349,9 @@ int szo_qk_norm_rope(const szo_qk_desc* d, void* stream) {
                                                      four_ok(d->q_out, d->q_out_token_stride, d->q_out_head_stride, d->out_type))) &&
                    (!d->kv_heads || (four_ok(d->k, d->k_token_stride, d->k_head_stride, d->in_type) &&
                                      four_ok(d->k_out, d->k_out_token_stride, d->k_out_head_stride, d->out_type)));
-  launch_in(a, (d->tokens + a.tokens_per_wg - 1) / a.tokens_per_wg, false, d->out_type, vec, (hipStream_t)stream);
+  const int64_t groups = (d->tokens + a.tokens_per_wg - 1) / a.tokens_per_wg;
+  if (groups > kMostGroups) return SZO_EUNSUPPORTED;
+  launch_in(a, groups, false, d->out_type, vec, (hipStream_t)stream);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }

@@ -60,12 +60,12 @@ template <int CTRL>
 __device__ __forceinline__ float lane_permuted(float v) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
 }
-// Sum over groups of L neighbouring lanes (8, 16, 32 or 64), in every lane.
+// Sum over groups of L neighbouring lanes (4, 8, 16, 32 or 64), in every lane.
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
   v += lane_permuted<0xB1>(v);          // lanes 1 apart
   v += lane_permuted<0x4E>(v);          // 2 apart
-  v += lane_permuted<0x141>(v);         // halves of 8
+  if constexpr (L >= 8) v += lane_permuted<0x141>(v);         // halves of 8
   if constexpr (L >= 16) v += lane_permuted<0x140>(v);
 #if defined(__HIP_DEVICE_COMPILE__)
   if constexpr (L >= 32) {
@@ -83,7 +83,7 @@ template <int L>
 __device__ __forceinline__ float lanes_max(float v) {
   v = fmaxf(v, lane_permuted<0xB1>(v));
   v = fmaxf(v, lane_permuted<0x4E>(v));
-  v = fmaxf(v, lane_permuted<0x141>(v));
+  if constexpr (L >= 8) v = fmaxf(v, lane_permuted<0x141>(v));
   if constexpr (L >= 16) v = fmaxf(v, lane_permuted<0x140>(v));
 #if defined(__HIP_DEVICE_COMPILE__)
   if constexpr (L >= 32) {
