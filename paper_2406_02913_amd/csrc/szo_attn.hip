@@ -458,9 +458,12 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
 // one token each: 1 sequence of 1000 10.3, 10.2, 8.6, 8.1, 8.1, 8.3; 1 of 8000 53, 33, 21, 14.7, 11.2, 9.6; 8 of 4000 35, 23, 17, 18, 20, 26; 16 of 8000 80, 49, 46,
 // 50, 56, 70; 32 of 1000 14, 18, 21; 64 of 500 to 8192 110, 106, 105.  64 tokens of one sequence (8 tiles for each key head) behind 2000 16.7, 15.8, 14.3, 18.6;
 // behind 8000 59, 38, 25, 24, 32; 200 tokens behind 4000 29, 32, 39, behind 8000 60, 47, 55.
+//   Between 65 and 256 workgroups, a CU each, eight waves share a tile's cache of 1000 tokens or more instead of four (wk): 8 x 29 answers behind up to 2000
+// 20.3 -> 16.4 us, 200 tokens behind 2000 17.0 -> 15.5, behind 8000 47 -> 40; with fewer workgroups parts are better (one token behind 8000 10.2 -> 10.6),
+// and short tiles read enough at once when three quarters of the CUs have one (32 sequences of 1000 14.2 -> 15.2).
 //   Blocks that one workgroup alone reads, 128 MiB of them or more, pass the caches by (once): 64 sequences of 500 to 8192 121 -> 106 us, 16 of 8000 52 -> 46,
 // 32 of 1000 (64 MiB) 14.2 -> 15.4.
-struct Plan { int wr, tiles, splits, rows_cap; bool once; };
+struct Plan { int wr, wk, tiles, splits, rows_cap; bool once; };
 
 Plan plan_of(const szo_attn_desc* d) {
   Plan p;
@@ -473,12 +476,14 @@ Plan plan_of(const szo_attn_desc* d) {
   p.wr = rows > 32 && (held >= 2048 || (held >= 1024 && blocks <= 8)) ? 4 : 1;
   p.tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
   p.rows_cap = (int)std::min<int64_t>(32, rows);
-  p.once = p.wr == 1 && p.tiles == 1 && pairs * blocks * kKvBlock * 2 * d->cache.head_dim >= (int64_t)128 << 20;
-  const int64_t walkers = 4 / p.wr, some = std::max<int64_t>(1, std::min(held / p.wr, pairs * p.tiles));          // workgroups that hold something
+  p.once = p.wr == 1 && p.tiles == 1 && blocks * kKvBlock * 2 * d->cache.head_dim >= ((int64_t)128 << 20) / pairs;
+  const int64_t some = std::max<int64_t>(1, std::min(held / p.wr, pairs * p.tiles));          // workgroups that hold something
+  p.wk = p.wr == 4 ? 1 : d->cache.head_dim <= 128 && !p.once && some > 64 && some <= (p.tiles == 1 ? 192 : 256) && blocks >= 32 ? 8 : 4;
+  const int64_t walkers = p.wk;
   const bool few = rows <= 16;
   const bool single = few && some <= 64;                // a block a wave
   const int64_t chip = few ? 512 : 256, step = single ? walkers : 4 * walkers, parts = blocks < (single ? 24 : 48) ? 1 : std::min<int64_t>((blocks + step - 1) / step, 32);
-  const int64_t fill = few && chip / some < 3 ? 1 : std::min(chip / some, parts), even = std::min(2 * chip / some, blocks / (walkers * (few ? 15 : 20)));
+  const int64_t fill = p.wk == 8 ? std::min(256 / some, blocks / 32) : few && chip / some < 3 ? 1 : std::min(chip / some, parts), even = p.wk == 8 ? 1 : std::min(2 * chip / some, blocks / (walkers * (few ? 15 : 20)));
   p.splits = (int)std::min<int64_t>(std::max<int64_t>({1, fill, even}), 64);
   return p;
 }
@@ -534,6 +539,7 @@ template <int TYPE, int D>
 int launch_all(const AttnArgs& a, const Plan& p, hipStream_t s) {
   int rc;
   if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, s);
+  else if (p.wk == 8) rc = launch<TYPE, D <= 128 ? D : 128, 1, 8, false>(a, s);           // 133 KiB of LDS at 128
   else if (p.once) rc = launch<TYPE, D, 1, 4, true>(a, s);
   else rc = launch<TYPE, D, 1, 4, false>(a, s);
   if (rc != SZO_OK || p.splits == 1) return rc;

@@ -166,3 +166,11 @@ def test_log_probabilities_limits():
                                        ({}, (P + 1, P, P, 10)), ({}, (P, P + 2, P, 10)), ({}, (P, P, P + 1, 10))])
 def test_gradient_of_log_probabilities_refuses(desc, args):
     assert szo.lib.szo_token_logprobs_bwd(C.byref(logp(**desc)), *args, None) == szo.EINVAL
+
+
+def test_launches_that_cannot_be_counted_are_refused():
+    """A launch counts its threads in 32 bits: more is refused by the call, not by the launch."""
+    assert szo.lib.szo_qk_norm_rope(C.byref(qk(tokens=0x7FFFFFFF)), None) == szo.EUNSUPPORTED
+    assert szo.lib.szo_token_logprobs(C.byref(logp(rows=1 << 25)), P, None) == szo.EUNSUPPORTED
+    assert szo.lib.szo_token_logprobs_bwd(C.byref(logp(rows=1 << 25)), P, P, P, 10, None) == szo.EUNSUPPORTED
+    assert szo.lib.szo_kv_cache_write(C.byref(cache(kv_heads=65536)), C.byref(tokens()), None) == szo.EUNSUPPORTED

@@ -257,3 +257,37 @@ def test_many_small_weights_beside_a_large_one(drop):
     # a weight to 2^-11, the output to 2^-11, the sums of 40000 equal terms in chains of some hundreds in fp32
     assert (out.double() - rest / (1 + rest)).abs().max().item() <= (2.0 ** -10 + 2.0 ** -14) * rest / (1 + rest)
     assert abs(lse.item() - (drop + math.log1p(rest))) < 1e-5
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,window", [(64, 0), (96, 700), (128, 0), (128, 40)])
+def test_eight_waves_share_a_tile(D, window, kind):
+    """Some hundred tiles with a long cache among them: as many workgroups as the chip has CUs, or half."""
+    def change(x):
+        x[1, 900, 0, 3] = np.nan
+        x[0, 1030, 1, 5] = np.nan
+
+    lengths = [1070, 1, 0, 33, 64, 257, 290, 1024, 8, 95]
+    b = filled(lengths, 8, D, 64, change=change)
+    check(b, lengths, [1] * 10, 4, kind, window=window)
+    check(b, lengths, [20, 1, 0, 9, 3, 17, 1, 1, 8, 2], 4, kind, window=window)
+    check(b, lengths, [60, 1, 0, 9, 3, 17, 1, 1, 8, 2], 2, kind, causal=False, window=window)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,new", [(64, 1, 1), (96, 3, 5), (128, 4, 1), (128, 2, 8), (128, 5, 13), (256, 4, 1), (256, 1, 40)])
+def test_many_parts(D, group, new, kind):
+    """A long sequence beside short ones: most parts of those hold nothing."""
+    lengths = [1601, 5, 130]
+    b = filled(lengths, 1, D, 32)
+    check(b, lengths, [new, 1, new], group, kind)
+    check(b, lengths, [new, 1, new], group, kind, window=100)
+    check(b, lengths, [new, 1, new], group, kind, max_len=40000)          # more parts than blocks
+
+
+def test_hints_of_any_size_choose_among_right_ways():
+    lengths = [300, 40, 1, 700]
+    b = filled(lengths, 2, 128, 64)
+    for hint in (1, 300, 800, 1600, 5000, 33000, 1 << 20, 1 << 30):
+        for new in ([1, 1, 1, 1], [5, 2, 1, 9], [100, 40, 1, 90]):
+            check(b, lengths, new, 4, "bf16", max_len=hint)
