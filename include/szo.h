@@ -253,7 +253,9 @@ int szo_workspace_init(void* workspace, void* stream);
  * position rotation, a key/value cache in 8 bits, attention over it, and log probabilities of given tokens (the
  * scalar f of Definition 1 for a language model is their negative mean).  The same conventions as above: the
  * calls enqueue on `stream`, allocate nothing, never synchronise, and can be captured into a HIP graph.  Strides count
- * elements; the last axis of every tensor is contiguous. */
+ * elements; the last axis of every tensor is contiguous.  SZO_EUNSUPPORTED, with nothing enqueued: head dimensions and numbers of
+ * alternatives other than those named below, more than 65535 key heads or sequences, and calls of more threads than a launch
+ * counts in 32 bits (about 16 million rows or tokens). */
 
 /* Element types of these calls. */
 #define SZO_F32   0
