@@ -235,12 +235,12 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogpArgs
   }
   // Rows with NaN, infinities, very many equal logits or fewer finite ones than are asked for: one pass for each alternative.
   const int begin = c0 * N, end = part == a.parts - 1 ? vocab : chunks * N;
-  uint64_t last = ~0ull;
+  uint64_t last = 0;                                           // of the alternative before; the first has none (a NaN at index 0 is the largest key there is)
   for (int rank = 0; rank < top; ++rank) {
     uint64_t best = 0;
     for (int i = begin + tid; i < end; i += kThreads) {
       const uint64_t key = key_of(C::one(d.logits, from + i), i);
-      if (key < last && key > best) best = key;
+      if ((rank == 0 || key < last) && key > best) best = key;
     }
 #pragma unroll
     for (int step = 32; step; step /= 2) {
