@@ -11,7 +11,9 @@
 // scores of 20 were off by 1e-4.)
 //   Values: codes become fp16, exactly; weights are rounded to fp16.  A block's exponent goes into the exponent of its weights: with
 // x = log2(e) s + v_exp the running maximum is over x, sum 2^(x - m) code is the output's numerator and sum 2^(x - m) 2^-v_exp the
-// denominator, so that the weights are relative to the largest contribution of the row.
+// denominator, so that the weights are relative to the largest contribution of the row.  A block whose exponent is far below that of others may add nothing to the
+// numerator and all the same most of the denominator (a block of zeros has exponent -32, others up to 120): its 2^(x - m) leaves fp32's range,
+// 2^(x - m - v_exp) does not, and is what is added up there (attn_walk_kernel: `apart`).
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_kv.h"
@@ -23,6 +25,10 @@ constexpr int kThreads = 256;              // of the joining kernel
 constexpr float kNone = -1e30f;            // running maximum of a row that has seen nothing
 constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
 constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
+// The denominator is held times 2^40 beside that.  Its largest term is the one of the block with exponent e that sets the maximum, 2^(51 - e), from 2^-73 (with the slack)
+// on: what is 2^-50 of it is still a normal number; no term is above 2^(15 + 32 + 40), so that 2^31 of them are finite.
+constexpr int kSumLift = 40;
+constexpr int kApart = 90;                 // exponents of values further apart than this: terms of the denominator may leave fp32's range on the way
 
 struct AttnArgs {
   szo_attn_desc d;
@@ -125,6 +131,19 @@ __device__ __forceinline__ float halves_sum(float v) {
   return v;
 }
 
+// A denominator l scaled by 2^by, in two steps: l may be so large that it matters where 2^by by itself would be 0 (by from -152 on).
+__device__ __forceinline__ float scaled_sum(float l, float by) {
+  const float half = __builtin_amdgcn_exp2f(0.5f * by);
+  return l * half * half;
+}
+// What the numerators are multiplied by, and log sum exp: the exponents of maximum and denominator cancel, so they go first.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : power_of_two(kSumLift) / l; }
+__device__ __forceinline__ float log_sum(float m, float l) {
+  if (l == 0.f) return -__builtin_inff();
+  const float e = (float)__builtin_amdgcn_frexp_expf(l) - (kLift + (float)kSumLift);
+  return ((m + e) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147180559945309f;
+}
+
 // 0x80 in each byte of w that is the code of NaN
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
@@ -166,7 +185,7 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
     }
     return;
   }
-  const float by = l == 0.f ? 0.f : 1.f / l;
+  const float by = inverse_sum(l);
   const int64_t at = (int64_t)token * d.out_token_stride + (int64_t)q_head * d.out_head_stride;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
@@ -178,7 +197,7 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
       else store_f32<TYPE, 4, false>(d.out, at + 32 * e + 2 * i + 4 * half, y);
     }
   }
-  if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
+  if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, l);
 }
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
@@ -246,16 +265,19 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       }
     };
     Raw<D> k = load_block<D, ONCE>(d.cache.k, known(now), lane), v = load_block<D, ONCE>(d.cache.v, known(now), lane);
-    int ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)];
+    int ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)], most_vexp = kExpMin;
     scores(k);
     k = load_block<D, ONCE>(d.cache.k, known(next), lane);
     for (int j = j0; j < j1; j += WK) {        // k: keys of the next step, v: values of this one
       const bool there = now >= 0;
       now = next;
       if (j + 2 * WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
-      const float factor = score_factor(a.to_log2, ke);
-      const int vexp = min(max(ve - kExpBias, kExpMin), kExpMax);
-      const float shift = (float)vexp, unshift = power_of_two(-vexp);
+      float factor = score_factor(a.to_log2, ke);
+      const int vexp = uniform(min(max(ve - kExpBias, kExpMin), kExpMax));
+      const float shift = (float)vexp;
+      float unshift = power_of_two(kSumLift - vexp);
+      most_vexp = max(most_vexp, vexp);
+      const bool apart = most_vexp - vexp > kApart;
       ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)];
       const int token = j * kKvBlock + 4 * half, to = there ? see_to - token : 0, from = see_from - token;      // of s[0]; s[i] is 8 (i / 4) + i % 4 further
       const bool all = there && (j + 1) * kKvBlock <= see_all && j * kKvBlock >= see_all_from;
@@ -272,8 +294,8 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       most = fmaf(halves_max(most), factor, shift);
       if (__any(most > m + kSlack)) {
         const float top = fmaxf(m, most), scale = __builtin_amdgcn_exp2f(m - top);
+        l = scaled_sum(l, m - top);
         m = top;
-        l *= scale;
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -312,8 +334,18 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       // Half of the weights beside the scores, the other half beside the first half of the output: there are vector instructions for every product to run beside
       // (all of them first: 576 us instead of 556 for a prompt of 8192).
       f16x8 p[2];
-      const float base = shift - m + kLift;
-      float sum = 0.f;
+      float base = shift - m + kLift, sum = 0.f;
+      if (apart) {             // the terms of the denominator by themselves; what follows adds those of the numerator alone
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = fmaf(s[i], factor, shift - m);
+          l += __builtin_amdgcn_exp2f(x - shift + (kLift + (float)kSumLift));
+          s[i] = x;
+        }
+        factor = 1.f;
+        base = kLift;
+        unshift = 0.f;
+      }
       const f32x16 x = s;
       auto weigh = [&](int c) {
 #pragma unroll
@@ -372,8 +404,9 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
     l = 0.f;
 #pragma unroll
     for (int w = 0; w < WK; ++w) {
-      part[w] = __builtin_amdgcn_exp2f(meet[w * kPer + D / 2 * 64 + lane] - top);
-      l = fmaf(meet[w * kPer + D / 2 * 64 + 64 + lane], part[w], l);
+      const float by = meet[w * kPer + D / 2 * 64 + lane] - top;
+      part[w] = __builtin_amdgcn_exp2f(by);
+      l += scaled_sum(meet[w * kPer + D / 2 * 64 + 64 + lane], by);
     }
     const float own = __builtin_amdgcn_exp2f(m - top);
     m = top;
@@ -421,8 +454,8 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
     const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
     const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
     const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
+    l = scaled_sum(l, m - top) + scaled_sum(ls, ms - top);
     m = top;
-    l = l * keep + ls * add;
     o[0] = o[0] * keep + x.x * add;
     o[1] = o[1] * keep + x.y * add;
     o[2] = o[2] * keep + x.z * add;
@@ -430,19 +463,19 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
   }
   if constexpr (G > 1) {
     const float top = lanes_max<G>(m), keep = exp2f(m - top);
+    l = lanes_sum<G>(scaled_sum(l, m - top));
     m = top;
-    l = lanes_sum<G>(l * keep);
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = lanes_sum<G>(o[k] * keep);
     if (g) return;
   }
-  const float by = l == 0.f ? 0.f : 1.f / l;
+  const float by = inverse_sum(l);
   const float y[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
   const int64_t at = (int64_t)(start + query) * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
   if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
   else store_f32<TYPE, 4, false>(d.out, at, y);
   if (d.lse && f == 0)
-    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = l == 0.f ? -__builtin_inff() : (m - kLift + __log2f(l)) * 0.693147180559945309f;
+    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = log_sum(m, l);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------

@@ -1,0 +1,54 @@
+"""Attention over the cache at the ends of its ranges: exponents of values far apart."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_02913_amd import szo
+from test_gpu_attn_cached import DEV, TYPES, check, filled
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(k, v, q, scale, new, causal=True, kind="bf16", max_len=None, page=64):
+    """One sequence: k, v fp32 [length, heads, D], the queries q [new, heads * group, D] -> out, lse and what the cache holds, as numpy."""
+    n, heads, D = k.shape
+    pages = -(-n // page)
+    mem = szo.new_kv_cache(pages, page, heads, D)
+    lengths = torch.tensor([n], dtype=torch.int32, device=DEV)
+    cache = szo.make_kv_cache(*mem, torch.arange(pages, dtype=torch.int32, device=DEV)[None], lengths)
+    start = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    szo.szo_kv_cache_write(cache, szo.make_kv_tokens(k.to(DEV), v.to(DEV), start, n))
+    held = torch.empty(2, n, heads, D, device=DEV)
+    szo.szo_kv_cache_read(cache, szo.make_kv_tokens(held[0], held[1], start, n))
+    q = q.to(TYPES[kind]).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    d = szo.make_attn_desc(cache, q, out, torch.tensor([0, new], dtype=torch.int32, device=DEV), new, n if max_len is None else max_len, scale, causal, lse=lse)
+    szo.szo_attn_cached(d, torch.full((szo.szo_attn_workspace_bytes(d),), 0xFF, dtype=torch.uint8, device=DEV))
+    return out.double().cpu().numpy(), lse.double().cpu().numpy(), held.double().cpu().numpy(), q.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,new,max_len", [(33, 1, None), (64, 3, None), (300, 1, None), (300, 40, None), (3000, 1, None), (3000, 20, None), (2500, 1200, None)])
+@pytest.mark.parametrize("value,at", [(1e36, 32), (3e38, 0), (1e36, -1), (2.0 ** 90, 35)])
+def test_blocks_of_zeros_beside_a_huge_value_count_in_the_sum(value, at, n, new, max_len, D):
+    """Equal scores: the output is the huge value over the number of tokens, whatever the exponents of the other blocks are."""
+    k, v = torch.zeros(n, 1, D), torch.zeros(n, 1, D)
+    at = min(at, n - 1) % n
+    v[at] = value
+    out, lse, held, _ = attend(k, v, torch.ones(new, 2, D), 1.0, new, max_len=max_len)
+    sees = np.arange(n - new + 1, n + 1)
+    want = np.where(sees > at, held[1, at, 0, 0] / sees, 0.0)[:, None, None]
+    # a weight to fp16 and the output to bf16; the sum of n equal terms in fp32, in chains of at most n / 16 steps with as many roundings
+    assert np.all(np.abs(out - want) <= (2.0 ** -8 + 2.0 ** -11 + (n / 16 + 16) * 2.0 ** -24) * want)
+    assert np.all(np.abs(lse - np.log(sees)[:, None]) <= (n / 16 + 16) * 2.0 ** -24 + 2.0 ** -22 * np.log(sees)[:, None] + 2.0 ** -21)
+
+
+def test_exponents_that_fall_and_rise_from_block_to_block():
+    """Values from 2^-40 to 2^120 by turns, scores that do not go with them, against the definition: sums of a part's waves and of parts as well."""
+    def change(x):
+        power = np.random.default_rng(5).integers(-40, 119, x.shape[1] // 32 + 1)
+        x[1] = np.clip(x[1], -2, 2) * (2.0 ** power.astype(float))[np.arange(x.shape[1]) // 32][:, None, None]
+
+    for lengths, new in (([700], [1]), ([700], [50]), ([2000, 90], [2, 1]), ([300], [300])):
+        b = filled(lengths, 1, 64, 64, seed=sum(lengths), change=change)
+        check(b, lengths, new, 2, "bf16")
