@@ -36,9 +36,12 @@ struct AttnArgs {
   int tiles, splits, rows_cap;             // row tiles of a workgroup, parts of the cache, rows kept per wave tile in partial sums
   float to_log2;                           // |scale| * log2(e)
   bool negate;                             // scale < 0: queries change sign
-  float* partial;                          // [sequence][key head][wave tile][split][rows_cap][head_dim + 2]
+  float* partial;                          // [sequence][key head][wave tile][split] of part_floats()
   bool vec_q, vec_out;
 };
+
+// A part's sums: rows_cap rows of head_dim numerators, then maximum and denominator of each.  A multiple of 16 bytes, which rows are stored and read in.
+__host__ __device__ constexpr int part_floats(int rows_cap, int head_dim) { return (rows_cap * (head_dim + 2) + 3) / 4 * 4; }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -170,7 +173,7 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
                                         int walker, int token, int q_head, int column, int half) {
   const szo_attn_desc& d = a.d;
   if (a.splits > 1) {
-    float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * a.rows_cap * (D + 2);
+    float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * part_floats(a.rows_cap, D);
     float* mine = to + (int64_t)column * D;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) {
@@ -440,7 +443,7 @@ template <int TYPE, int D, int G>
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
   const szo_attn_desc& d = a.d;
   const int wave_tile = blockIdx.x % wave_tiles, head = blockIdx.y, sequence = blockIdx.z;
-  const float* from = partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * rows_cap * (D + 2);
+  const float* from = partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
   const int start = max(q_start[sequence], 0), stop = (int)min((int64_t)q_start[sequence + 1], d.tokens);
   const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
   const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
   constexpr int kAhead = G == 1 ? 4 : 2;
 #pragma unroll kAhead
   for (int s = g; s < splits; s += G) {
-    const float* part = from + (int64_t)s * rows_cap * (D + 2);
+    const float* part = from + (int64_t)s * part_floats(rows_cap, D);
     const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
     const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
     const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
@@ -600,7 +603,7 @@ size_t szo_attn_workspace_bytes(const szo_attn_desc* d) {
   if (check(d) != SZO_OK || nothing(d)) return 16;
   const Plan p = plan_of(d);
   if (p.splits == 1) return 16;
-  return (size_t)d->cache.sequences * d->cache.kv_heads * p.tiles * p.wr * p.splits * p.rows_cap * (d->cache.head_dim + 2) * sizeof(float);
+  return (size_t)d->cache.sequences * d->cache.kv_heads * p.tiles * p.wr * p.splits * part_floats(p.rows_cap, d->cache.head_dim) * sizeof(float);
 }
 
 int szo_attn_cached(const szo_attn_desc* d, void* workspace, void* stream) {

@@ -1,0 +1,18 @@
+"""Sizes of workspaces and bounds that the calls between the linear layers keep to: on the host, no kernel is launched."""
+import pytest
+
+from test_decoder_refusals import attn, cache
+from paper_2406_02913_amd import szo
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("group,new", [(1, 1), (3, 1), (5, 1), (7, 1), (1, 3), (4, 1)])
+def test_parts_of_a_cache_are_stored_at_multiples_of_16_bytes(D, group, new):
+    """One sequence of one key head in some number of parts, at most 64: each is a whole number of 16 bytes and holds its rows' sums."""
+    rows = group * new
+    for length in (1200, 2000, 2500, 3300, 5000, 9000, 40000):
+        d = attn(q_heads=group, max_q=new, tokens=new, max_len=length, cache=cache(kv_heads=1, sequences=1, head_dim=D, max_pages=1000, page_tokens=64),
+                 q_token_stride=group * D, q_head_stride=D, out_token_stride=group * D, out_head_stride=D)
+        size = szo.szo_attn_workspace_bytes(d)
+        least = 4 * rows * (D + 2)                # numerators, maximum, denominator; one statistic more would still be a row's sums
+        assert size > 16 and any(size % parts == 0 and size // parts % 16 == 0 and 0 <= size // parts - least < 16 + 4 * rows for parts in range(2, 65)), (length, size)
