@@ -14,6 +14,7 @@
 // denominator, so that the weights are relative to the largest contribution of the row.  A block whose exponent is far below that of others may add nothing to the
 // numerator and all the same most of the denominator (a block of zeros has exponent -32, others up to 120): its 2^(x - m) leaves fp32's range,
 // 2^(x - m - v_exp) does not, and is what is added up there (attn_walk_kernel: `apart`).
+//   A maximum is held as two numbers, log2(e) s of the token that sets it and the exponent of its block: their sum would lose the exponent where scores are large.
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_kv.h"
@@ -22,13 +23,14 @@ namespace szo {
 namespace {
 
 constexpr int kThreads = 256;              // of the joining kernel
-constexpr float kNone = -1e30f;            // running maximum of a row that has seen nothing
+constexpr float kNone = -3.402823466e38f;  // running maximum of a row that has seen nothing: the lowest finite value, so that differences stay defined
 constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
 constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
 // The denominator is held times 2^40 beside that.  Its largest term is the one of the block with exponent e that sets the maximum, 2^(51 - e), from 2^-73 (with the slack)
 // on: what is 2^-50 of it is still a normal number; no term is above 2^(15 + 32 + 40), so that 2^31 of them are finite.
 constexpr int kSumLift = 40;
 constexpr int kApart = 90;                 // exponents of values further apart than this: terms of the denominator may leave fp32's range on the way
+constexpr float kFar = 1048576.f;          // maxima beyond 2^20: a fused product minus the rounded maximum is no longer a difference of rounded products
 
 struct AttnArgs {
   szo_attn_desc d;
@@ -40,8 +42,9 @@ struct AttnArgs {
   bool vec_q, vec_out;
 };
 
-// A part's sums: rows_cap rows of head_dim numerators, then maximum and denominator of each.  A multiple of 16 bytes, which rows are stored and read in.
-__host__ __device__ constexpr int part_floats(int rows_cap, int head_dim) { return (rows_cap * (head_dim + 2) + 3) / 4 * 4; }
+// A part's sums: rows_cap rows of head_dim numerators, then maximum (two floats) and denominator of each.  A multiple of 16 bytes, which rows are stored
+// and read in.
+__host__ __device__ constexpr int part_floats(int rows_cap, int head_dim) { return (rows_cap * (head_dim + 3) + 3) / 4 * 4; }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -134,17 +137,19 @@ __device__ __forceinline__ float halves_sum(float v) {
   return v;
 }
 
-// A denominator l scaled by 2^by, in two steps: l may be so large that it matters where 2^by by itself would be 0 (by from -152 on).
-__device__ __forceinline__ float scaled_sum(float l, float by) {
-  const float half = __builtin_amdgcn_exp2f(0.5f * by);
-  return l * half * half;
-}
+// Sums are scaled by 2^by in two steps of half of it: a denominator may be so large that it matters where 2^by by itself is 0 (by from -152 on).
+__device__ __forceinline__ float half_of(float by) { return __builtin_amdgcn_exp2f(0.5f * by); }
 // What the numerators are multiplied by, and log sum exp: the exponents of maximum and denominator cancel, so they go first.
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : power_of_two(kSumLift) / l; }
-__device__ __forceinline__ float log_sum(float m, float l) {
+__device__ __forceinline__ float log_sum(float m, float m_exp, float l) {
   if (l == 0.f) return -__builtin_inff();
   const float e = (float)__builtin_amdgcn_frexp_expf(l) - (kLift + (float)kSumLift);
-  return ((m + e) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147180559945309f;
+  return ((m + (m_exp + e)) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147180559945309f;
+}
+
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
 }
 
 // 0x80 in each byte of w that is the code of NaN
@@ -169,7 +174,7 @@ struct Walk {
 
 // A lane's half of a row: finished, or as this split's partial sum.  Of WK waves each has the features 32 e .. + 31 with e = walker modulo WK.
 template <int TYPE, int D, int WK>
-__device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
+__device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float m_exp, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
                                         int walker, int token, int q_head, int column, int half) {
   const szo_attn_desc& d = a.d;
   if (a.splits > 1) {
@@ -183,8 +188,9 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
         *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
     }
     if (half == 0 && walker == 0) {
-      to[(int64_t)a.rows_cap * D + 2 * column] = m;
-      to[(int64_t)a.rows_cap * D + 2 * column + 1] = l;
+      to[(int64_t)a.rows_cap * D + 3 * column] = m;
+      to[(int64_t)a.rows_cap * D + 3 * column + 1] = m_exp;
+      to[(int64_t)a.rows_cap * D + 3 * column + 2] = l;
     }
     return;
   }
@@ -200,7 +206,7 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
       else store_f32<TYPE, 4, false>(d.out, at + 32 * e + 2 * i + 4 * half, y);
     }
   }
-  if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, l);
+  if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, m_exp, l);
 }
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
@@ -248,7 +254,8 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   const int see_all_from = d.window > 0 ? pos_last - d.window + 1 : 0;
 
   f32x16 o[E], s = {};
-  float m = kNone, l = 0.f;
+  float m = kNone, m_exp = 0.f, l = 0.f;
+  bool far = false;                        // some row's maximum is beyond kFar
   uint32_t poison[(E + 1) / 2];            // one bit for each of the lane's sums: it is NaN
 #pragma unroll
   for (int e = 0; e < E; ++e) { o[e] = f32x16{}; poison[e / 2] = 0; }
@@ -294,11 +301,15 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       float most = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
-      most = fmaf(halves_max(most), factor, shift);
-      if (__any(most > m + kSlack)) {
-        const float top = fmaxf(m, most), scale = __builtin_amdgcn_exp2f(m - top);
-        l = scaled_sum(l, m - top);
-        m = top;
+      most = rounded_product(halves_max(most), factor);
+      const float over = (most - m) + (shift - m_exp);
+      if (__any(over > kSlack)) {
+        const bool up = over > 0.f;
+        const float by_half = half_of(up ? -over : 0.f), scale = by_half * by_half;
+        l = l * by_half * by_half;
+        m = up ? most : m;
+        m_exp = up ? shift : m_exp;
+        far |= __any(up && fabsf(m) > kFar);
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -337,11 +348,12 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       // Half of the weights beside the scores, the other half beside the first half of the output: there are vector instructions for every product to run beside
       // (all of them first: 576 us instead of 556 for a prompt of 8192).
       f16x8 p[2];
-      float base = shift - m + kLift, sum = 0.f;
-      if (apart) {             // the terms of the denominator by themselves; what follows adds those of the numerator alone
+      const float step = shift - m_exp;
+      float base = step - m + kLift, sum = 0.f;
+      if (apart || far) {      // the terms of the denominator by themselves, of products that are rounded as the maximum is; what follows adds those of the numerator alone
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float x = fmaf(s[i], factor, shift - m);
+          const float x = rounded_product(s[i], factor) - m + step;
           l += __builtin_amdgcn_exp2f(x - shift + (kLift + (float)kSumLift));
           s[i] = x;
         }
@@ -386,7 +398,7 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   if constexpr (WK > 1) {
     // the walkers' sums meet: each adds up every WK-th tile of 32 features (one of them all: 16 short answers 26.2 -> 25.8 us, one token behind 1000 10.3 -> 9.9)
     extern __shared__ __attribute__((aligned(16))) float meet[];
-    constexpr int kPer = 64 * (D / 2 + 2);
+    constexpr int kPer = 64 * (D / 2 + 3);
     static_assert(WR == 1, "one tile of rows");
     {
       float* to = meet + walker * kPer;
@@ -398,21 +410,29 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
           *reinterpret_cast<float4*>(to + (e * 4 + i / 4) * 256 + lane * 4) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
       }
       to[D / 2 * 64 + lane] = m;
-      to[D / 2 * 64 + 64 + lane] = l;
+      to[D / 2 * 64 + 64 + lane] = m_exp;
+      to[D / 2 * 64 + 128 + lane] = l;
     }
     __syncthreads();
-    float top = kNone, part[WK];
+    // the largest of the first numbers, and of the second ones relative to it: no walker's maximum is above the two, and one is equal to them
+    float top = kNone, top_exp = kNone, part[WK];
 #pragma unroll
     for (int w = 0; w < WK; ++w) top = fmaxf(top, meet[w * kPer + D / 2 * 64 + lane]);
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      part[w] = meet[w * kPer + D / 2 * 64 + lane] - top + meet[w * kPer + D / 2 * 64 + 64 + lane];
+      top_exp = fmaxf(top_exp, part[w]);
+    }
     l = 0.f;
 #pragma unroll
     for (int w = 0; w < WK; ++w) {
-      const float by = meet[w * kPer + D / 2 * 64 + lane] - top;
-      part[w] = __builtin_amdgcn_exp2f(by);
-      l += scaled_sum(meet[w * kPer + D / 2 * 64 + 64 + lane], by);
+      const float by_half = half_of(part[w] - top_exp);
+      part[w] = by_half * by_half;
+      l = fmaf(meet[w * kPer + D / 2 * 64 + 128 + lane] * by_half, by_half, l);
     }
-    const float own = __builtin_amdgcn_exp2f(m - top);
+    const float own_half = half_of(m - top + m_exp - top_exp), own = own_half * own_half;
     m = top;
+    m_exp = top_exp;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       if (e % WK != walker) continue;
@@ -433,7 +453,7 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       }
     }
   }
-  if (valid) put_row<TYPE, D, WK>(a, o, m, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
+  if (valid) put_row<TYPE, D, WK>(a, o, m, m_exp, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
 }
 
 // Joins the parts of a row, four features of it at a time, by G neighbouring lanes: each takes every G-th part and they add each other up by row
@@ -449,25 +469,29 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
   const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
   const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
   if (column >= rows) return;                  // G lanes at once
-  float m = kNone, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  float m = kNone, m_exp = 0.f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int kAhead = G == 1 ? 4 : 2;
 #pragma unroll kAhead
   for (int s = g; s < splits; s += G) {
     const float* part = from + (int64_t)s * part_floats(rows_cap, D);
-    const float ms = part[(int64_t)rows_cap * D + 2 * column], ls = part[(int64_t)rows_cap * D + 2 * column + 1];
+    const float* stats = part + (int64_t)rows_cap * D + 3 * column;
+    const float ms = stats[0], es = stats[1], ls = stats[2];
     const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
-    const float top = fmaxf(m, ms), keep = exp2f(m - top), add = exp2f(ms - top);
-    l = scaled_sum(l, m - top) + scaled_sum(ls, ms - top);
-    m = top;
+    const float over = (ms - m) + (es - m_exp), keep_half = half_of(fminf(-over, 0.f)), add_half = half_of(fminf(over, 0.f));
+    const float keep = keep_half * keep_half, add = add_half * add_half;
+    l = fmaf(l * keep_half, keep_half, ls * add_half * add_half);
+    m = over > 0.f ? ms : m;
+    m_exp = over > 0.f ? es : m_exp;
     o[0] = o[0] * keep + x.x * add;
     o[1] = o[1] * keep + x.y * add;
     o[2] = o[2] * keep + x.z * add;
     o[3] = o[3] * keep + x.w * add;
   }
   if constexpr (G > 1) {
-    const float top = lanes_max<G>(m), keep = exp2f(m - top);
-    l = lanes_sum<G>(scaled_sum(l, m - top));
+    const float top = lanes_max<G>(m), rest = m - top + m_exp, top_exp = lanes_max<G>(rest), keep_half = half_of(rest - top_exp), keep = keep_half * keep_half;
+    l = lanes_sum<G>(l * keep_half * keep_half);
     m = top;
+    m_exp = top_exp;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = lanes_sum<G>(o[k] * keep);
     if (g) return;
@@ -478,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
   if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
   else store_f32<TYPE, 4, false>(d.out, at, y);
   if (d.lse && f == 0)
-    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = log_sum(m, l);
+    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = log_sum(m, m_exp, l);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -549,7 +573,7 @@ bool nothing(const szo_attn_desc* d) { return d->cache.sequences == 0 || d->q_he
 
 template <int TYPE, int D, int WR, int WK, bool ONCE>
 int launch(const AttnArgs& a, hipStream_t s) {
-  constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 2) * sizeof(float);
+  constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 3) * sizeof(float);
   static std::atomic<uint64_t> raised{0};
   if (lds > 64 * 1024) {
     const int rc = set_lds_limit_once(raised, (const void*)attn_walk_kernel<TYPE, D, WR, WK, ONCE>, lds);
@@ -575,7 +599,7 @@ template <int TYPE, int D>
 int launch_all(const AttnArgs& a, const Plan& p, hipStream_t s) {
   int rc;
   if (p.wr == 4) rc = launch<TYPE, D, 4, 1, false>(a, s);
-  else if (p.wk == 8) rc = launch<TYPE, D <= 128 ? D : 128, 1, 8, false>(a, s);           // 133 KiB of LDS at 128
+  else if (p.wk == 8) rc = launch<TYPE, D <= 128 ? D : 128, 1, 8, false>(a, s);           // 134 KiB of LDS at 128
   else if (p.once) rc = launch<TYPE, D, 1, 4, true>(a, s);
   else rc = launch<TYPE, D, 1, 4, false>(a, s);
   if (rc != SZO_OK || p.splits == 1) return rc;

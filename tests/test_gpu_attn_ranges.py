@@ -1,10 +1,12 @@
-"""Attention over the cache at the ends of its ranges: exponents of values far apart."""
+"""Attention over the cache at the ends of its ranges: exponents of values far apart, scores of any size."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2406_02913_amd import szo
-from test_gpu_attn_cached import DEV, TYPES, check, filled
+from test_gpu_attn_cached import DEV, STORE, TYPES, check, filled
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +54,32 @@ def test_exponents_that_fall_and_rise_from_block_to_block():
     for lengths, new in (([700], [1]), ([700], [50]), ([2000, 90], [2, 1]), ([300], [300])):
         b = filled(lengths, 1, 64, 64, seed=sum(lengths), change=change)
         check(b, lengths, new, 2, "bf16")
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("kind,power", [("bf16", 10), ("bf16", 20), ("bf16", 24), ("bf16", 30), ("bf16", 60), ("bf16", 100), ("bf16", 119), ("f16", 24), ("f16", 100)])
+@pytest.mark.parametrize("n,new", [(40, 1), (500, 7), (2000, 1), (300, 300)])
+def test_scores_of_any_size_that_fp32_holds(n, new, kind, power, sign):
+    """Scores j * 2^power, j of 1 to 15, with either sign: the weights stand on the largest that a query sees, and are shared by its equals."""
+    rng = np.random.default_rng(n + power)
+    j = rng.integers(1, 16, n)
+    j[0] = 8
+    high = 0 if kind == "bf16" else power - 14
+    k, v = torch.zeros(n, 1, 64), torch.from_numpy(rng.integers(-8, 9, (n, 1, 64)).astype(np.float32))       # held exactly
+    v *= 2.0 ** (3 * (torch.arange(n) // 32 % 3))[:, None, None]          # equal scores in blocks of different exponents
+    k[:, 0, 5] = torch.from_numpy(j * 2.0 ** high).float()
+    q = torch.zeros(new, 2, 64)
+    q[:, :, 5] = sign * 2.0 ** (power - high)
+    out, lse, held, _ = attend(k, v, q, 1.0, new, kind=kind)
+    assert np.array_equal(held[1], v.double().numpy()) and np.array_equal(held[0], k.double().numpy())
+    for i in range(new):
+        see = n - new + i + 1
+        s = sign * j[:see] * 2.0 ** power
+        w = np.exp(s - s.max())
+        want = (w / w.sum()) @ v[:see, 0].double().numpy()
+        size = (w / w.sum()) @ np.abs(v[:see, 0].double().numpy())
+        rel, floor = STORE[kind]
+        # neighbouring scores lie 2^10 apart and more: equal ones have equal weights, each to 2^-11, all others 0
+        assert np.all(np.abs(out[i] - want) <= rel * np.abs(want) + floor + (2.0 ** -11 + 2.0 ** -16) * size), (i, s.max())
+        # one rounding of the largest score's product by log2(e), of log2(e) itself, and of the way back
+        assert np.all(np.abs(lse[i] - (s.max() + math.log(w.sum()))) <= 2.0 ** -21 * abs(s.max()) + 2.0 ** -20)
