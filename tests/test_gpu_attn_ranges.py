@@ -1,4 +1,4 @@
-"""Attention over the cache at the ends of its ranges: exponents of values far apart, scores of any size."""
+"""Attention over the cache at the ends of its ranges: exponents of values far apart, scores of any size, windows of any size."""
 import math
 
 import numpy as np
@@ -83,3 +83,21 @@ def test_scores_of_any_size_that_fp32_holds(n, new, kind, power, sign):
         assert np.all(np.abs(out[i] - want) <= rel * np.abs(want) + floor + (2.0 ** -11 + 2.0 ** -16) * size), (i, s.max())
         # one rounding of the largest score's product by log2(e), of log2(e) itself, and of the way back
         assert np.all(np.abs(lse[i] - (s.max() + math.log(w.sum()))) <= 2.0 ** -21 * abs(s.max()) + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 64, 2 ** 30])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_wider_than_any_sequence_hide_nothing(window, causal):
+    lengths = [40, 75, 130, 20]
+    b = filled(lengths, 2, 64, 64)
+    for new in ([1, 1, 1, 1], [40, 9, 130, 20], [40, 33, 50, 1]):
+        q = b.rng.standard_normal((sum(new), 4, 64))
+        wide = check(b, lengths, new, 2, "bf16", causal, window, q=q)
+        assert np.array_equal(wide, check(b, lengths, new, 2, "bf16", causal, 0, q=q))
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 20, 5])
+def test_windows_with_more_new_tokens_than_the_length(window):
+    b = filled([20, 64], 1, 64, 32)
+    check(b, [20, 64], [30, 100], 2, "bf16", True, window)
+    check(b, [20, 64], [30, 100], 2, "bf16", False, window)
