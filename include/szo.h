@@ -262,6 +262,9 @@ int szo_workspace_init(void* workspace, void* stream);
 #define SZO_BF16  1
 #define SZO_F16   2
 
+/* Largest size of a scale of logits or scores: beyond it scale * log2(e), which they are multiplied by, is infinite. */
+#define SZO_MOST_SCALE 2.35e38f
+
 /* Queries and keys of a batch of tokens: for each token and head
  *   u = x * w / sqrt(mean(x^2) + eps)      (norm != 0; w = 1 where the weight is NULL; u = x without norm)
  *   out = u, its first rot_dim features turned pairwise by the angles of the token's position:
@@ -377,7 +380,7 @@ size_t szo_attn_workspace_bytes(const szo_attn_desc* desc /* host */);
 typedef struct szo_logprobs_desc {
   int64_t rows, vocab, row_stride;
   int32_t type, top;            /* type of the logits; 0 <= top <= 32, top <= vocab                      */
-  float   scale;                /* 1 / temperature, finite and > 0                                       */
+  float   scale;                /* 1 / temperature, > 0 and at most SZO_MOST_SCALE                       */
   int32_t reserved;             /* 0                                                                     */
   const void* logits;           /* device [rows, vocab]                                                  */
   const int32_t* targets;       /* device [rows]; NULL: every target ignored                             */

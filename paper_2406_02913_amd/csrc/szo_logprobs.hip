@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const 
 
 int check(const szo_logprobs_desc* d) {
   if (!d || d->rows < 0 || d->vocab < 0 || !valid_type(d->type) || d->reserved) return SZO_EINVAL;
-  if (d->top < 0 || d->top > d->vocab || !(d->scale > 0.f && d->scale < 3.4e38f)) return SZO_EINVAL;
+  if (d->top < 0 || d->top > d->vocab || !(d->scale > 0.f && d->scale <= SZO_MOST_SCALE)) return SZO_EINVAL;
   if (d->top > SZO_LOGPROBS_MAX_TOP || d->vocab > (1 << 30) || d->rows > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
   if (d->rows > 1 && d->row_stride < 0) return SZO_EINVAL;
   if (d->rows && d->vocab && (!d->logits || !aligned_to(d->logits, type_bytes(d->type)))) return SZO_EINVAL;

@@ -24,6 +24,7 @@ FORMAT_UNIFORM, FORMAT_LUT = 0, 1
 F32, BF16, F16 = 0, 1, 2                  # element types of the calls between the linear layers
 KV_BLOCK = 32                             # tokens that share an exponent in the cache
 LOGPROBS_MAX_TOP = 32
+MOST_SCALE = 2.35e38                      # of logits and scores
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "

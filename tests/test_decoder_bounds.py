@@ -1,7 +1,7 @@
 """Sizes of workspaces and bounds that the calls between the linear layers keep to: on the host, no kernel is launched."""
 import pytest
 
-from test_decoder_refusals import attn, cache
+from test_decoder_refusals import P, attn, cache, logp
 from paper_2406_02913_amd import szo
 
 
@@ -16,3 +16,10 @@ def test_parts_of_a_cache_are_stored_at_multiples_of_16_bytes(D, group, new):
         size = szo.szo_attn_workspace_bytes(d)
         least = 4 * rows * (D + 2)                # numerators, maximum, denominator; one statistic more would still be a row's sums
         assert size > 16 and any(size % parts == 0 and size // parts % 16 == 0 and 0 <= size // parts - least < 16 + 4 * rows for parts in range(2, 65)), (length, size)
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.3e38])
+def test_log_probabilities_refuse_a_scale_whose_product_by_log2_e_is_infinite(scale):
+    assert szo.lib.szo_token_logprobs(logp(scale=scale), P, None) == szo.EINVAL
+    assert szo.lib.szo_token_logprobs_bwd(logp(scale=scale), P, P, P, 10, None) == szo.EINVAL
+    assert szo.lib.szo_token_logprobs(logp(scale=szo.MOST_SCALE, rows=0), P, None) == szo.OK
