@@ -356,7 +356,7 @@ typedef struct szo_attn_desc {
   szo_kv_cache cache;
   int32_t q_heads, type;        /* type of q and out: SZO_BF16 or SZO_F16                                */
   int32_t causal, window;
-  float   scale;
+  float   scale;                /* at most SZO_MOST_SCALE in size                                        */
   int32_t max_q;                /* most queries of one sequence; further ones are left out               */
   int32_t max_len, reserved;    /* longest sequence: a hint that the split of the work goes by            */
   int64_t tokens;               /* rows of q                                                             */

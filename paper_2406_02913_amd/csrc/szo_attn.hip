@@ -116,9 +116,9 @@ template <int TYPE, int D> struct Query {
   }
 };
 
-// Factor of a block's scores, in powers of two; never 0, so that masked ones stay -inf.
+// Factor of a block's scores, in powers of two; never 0, so that masked ones stay -inf, and finite, so that scores of 0 stay 0.
 __device__ __forceinline__ float score_factor(float to_log2, int key_exp) {
-  return fmaxf(to_log2 * power_of_two(min(max(key_exp - kExpBias, kExpMin), kExpMax)), 1e-37f);
+  return __builtin_amdgcn_fmed3f(to_log2 * power_of_two(min(max(key_exp - kExpBias, kExpMin), kExpMax)), 1e-37f, -kNone);
 }
 
 // max and sum of a value and its other half's (lane +- 32)
@@ -558,7 +558,7 @@ int check(const szo_attn_desc* d) {
   const szo_kv_cache& c = d->cache;
   if ((d->type != SZO_BF16 && d->type != SZO_F16) || (d->causal & ~1) || d->reserved || d->q_heads < 0 || d->window < 0 || d->max_q < 0 || d->max_len < 0 ||
       d->tokens < 0) return SZO_EINVAL;
-  if (!(d->scale > -3.4e38f && d->scale < 3.4e38f)) return SZO_EINVAL;
+  if (!(d->scale >= -SZO_MOST_SCALE && d->scale <= SZO_MOST_SCALE)) return SZO_EINVAL;
   if (d->tokens > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
   if (c.kv_heads == 0 ? d->q_heads != 0 : d->q_heads % c.kv_heads != 0) return SZO_EINVAL;
   if (c.sequences == 0 || d->q_heads == 0 || d->tokens == 0 || d->max_q == 0) return SZO_OK;

@@ -23,3 +23,9 @@ def test_log_probabilities_refuse_a_scale_whose_product_by_log2_e_is_infinite(sc
     assert szo.lib.szo_token_logprobs(logp(scale=scale), P, None) == szo.EINVAL
     assert szo.lib.szo_token_logprobs_bwd(logp(scale=scale), P, P, P, 10, None) == szo.EINVAL
     assert szo.lib.szo_token_logprobs(logp(scale=szo.MOST_SCALE, rows=0), P, None) == szo.OK
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -3.3e38])
+def test_attention_refuses_a_scale_whose_product_by_log2_e_is_infinite(scale):
+    assert szo.lib.szo_attn_cached(attn(scale=scale), P, None) == szo.EINVAL
+    assert szo.lib.szo_attn_cached(attn(scale=-szo.MOST_SCALE, tokens=0), None, None) == szo.OK

@@ -85,6 +85,23 @@ def test_scores_of_any_size_that_fp32_holds(n, new, kind, power, sign):
         assert np.all(np.abs(lse[i] - (s.max() + math.log(w.sum()))) <= 2.0 ** -21 * abs(s.max()) + 2.0 ** -20)
 
 
+@pytest.mark.parametrize("scale", [1e4, szo.MOST_SCALE, -szo.MOST_SCALE])
+@pytest.mark.parametrize("n,new", [(40, 1), (300, 40)])
+def test_scores_of_zero_beside_keys_as_large_as_they_get(n, new, scale):
+    """Queries of zeros, and such that see only a zero feature of their keys: equal weights, though scale times the keys' exponent passes fp32."""
+    k, v = torch.full((n, 1, 64), 3e38), torch.from_numpy(np.random.default_rng(n).integers(-8, 9, (n, 1, 64)).astype(np.float32))
+    k[:, 0, 9] = 0
+    q = torch.zeros(new, 2, 64)
+    q[:, 1, 9] = 5.0
+    out, lse, held, _ = attend(k, v, q, scale, new)
+    for i in range(new):
+        see = n - new + i + 1
+        want, size = held[1][:see, 0].mean(0), np.abs(held[1][:see, 0]).mean(0)
+        # equal weights, rounded to bf16; sums of n equal terms
+        assert np.all(np.abs(out[i] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -18) * size)
+        assert np.all(np.abs(lse[i] - math.log(see)) <= 2.0 ** -19)
+
+
 @pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 64, 2 ** 30])
 @pytest.mark.parametrize("causal", [True, False])
 def test_windows_wider_than_any_sequence_hide_nothing(window, causal):
