@@ -293,7 +293,8 @@ int check_cache(const szo_kv_cache* c) {
   if (c->kv_heads > 65535) return SZO_EUNSUPPORTED;            // a side of a grid
   if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128 && c->head_dim != 256) return SZO_EUNSUPPORTED;
   if ((int64_t)c->max_pages * c->page_tokens > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
-  if (c->sequences && c->max_pages && (!c->page_table || !c->lengths || !aligned_to(c->page_table, 4) || !aligned_to(c->lengths, 4))) return SZO_EINVAL;
+  if (c->sequences && (!c->lengths || !aligned_to(c->lengths, 4))) return SZO_EINVAL;          // read for every sequence, with or without pages
+  if (c->sequences && c->max_pages && (!c->page_table || !aligned_to(c->page_table, 4))) return SZO_EINVAL;
   if (c->pages && c->kv_heads && (!c->k || !c->v || !c->k_exp || !c->v_exp || !aligned_to(c->k, 16) || !aligned_to(c->v, 16))) return SZO_EINVAL;
   return SZO_OK;
 }

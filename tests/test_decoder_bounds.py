@@ -1,7 +1,7 @@
 """Sizes of workspaces and bounds that the calls between the linear layers keep to: on the host, no kernel is launched."""
 import pytest
 
-from test_decoder_refusals import P, attn, cache, logp
+from test_decoder_refusals import P, attn, cache, logp, tokens
 from paper_2406_02913_amd import szo
 
 
@@ -29,3 +29,12 @@ def test_log_probabilities_refuse_a_scale_whose_product_by_log2_e_is_infinite(sc
 def test_attention_refuses_a_scale_whose_product_by_log2_e_is_infinite(scale):
     assert szo.lib.szo_attn_cached(attn(scale=scale), P, None) == szo.EINVAL
     assert szo.lib.szo_attn_cached(attn(scale=-szo.MOST_SCALE, tokens=0), None, None) == szo.OK
+
+
+@pytest.mark.parametrize("call", ["szo_kv_cache_write", "szo_kv_cache_read"])
+@pytest.mark.parametrize("lengths", [None, P + 2])
+def test_cache_calls_want_lengths_whatever_the_page_table_holds(call, lengths):
+    """Without pages a read still asks every sequence's length."""
+    for kw in (dict(max_pages=0), dict(max_pages=0, page_table=None), dict(pages=0, max_pages=0)):
+        assert getattr(szo.lib, call)(cache(lengths=lengths, **kw), tokens(), None) == szo.EINVAL
+    assert getattr(szo.lib, call)(cache(lengths=lengths, sequences=0, max_pages=0), tokens(), None) == szo.OK
