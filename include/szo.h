@@ -334,6 +334,7 @@ typedef struct szo_kv_tokens {
   const int32_t* token_start;   /* device [sequences + 1], ascending from 0                              */
   void *k, *v;                  /* device [tokens, kv_heads, head_dim]                                   */
   int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t tokens;               /* rows of k and v: what token_start has outside [0, tokens) is left out  */
 } szo_kv_tokens;
 
 /* Quantises new tokens into the cache.  A block whose first token is among them is written whole (codes behind the last

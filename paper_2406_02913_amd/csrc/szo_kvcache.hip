@@ -29,10 +29,10 @@ struct KvArgs {
 struct Share {
   int head, index, first, end;
   int64_t row, block;
-  __device__ bool find(const int32_t* token_start, const int32_t* lengths, const KvArgs& a) {
+  __device__ bool find(const int32_t* token_start, const int32_t* lengths, int64_t tokens, const KvArgs& a) {
     const int sequence = blockIdx.z, nth = blockIdx.y;
     head = blockIdx.x;
-    const int start = token_start[sequence], stop = token_start[sequence + 1];
+    const int start = max(token_start[sequence], 0), stop = max((int)min((int64_t)token_start[sequence + 1], tokens), 0);      // rows that there are
     const int64_t length = lengths[sequence], had = length - (int64_t)(stop - start);
     if (stop <= start || length <= 0) return false;
     const int64_t at = (had > 0 ? had : 0) / kKvBlock + nth;             // tokens before position 0 have no place
@@ -91,11 +91,11 @@ __device__ __forceinline__ void move_down(uint8_t* block, int first, int end, fl
 
 // What the first loads need comes first in the arguments, where it is in registers when a wave starts.  VEC: groups of four features lie at multiples of their size.
 template <int TYPE, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const int32_t* token_start, const int32_t* lengths, const KvArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const int32_t* token_start, const int32_t* lengths, int64_t tokens, const KvArgs a) {
   __shared__ float maxima[2][kThreads / 64];
   __shared__ __attribute__((aligned(16))) uint8_t tile[D * kRow];
   Share s;
-  if (!s.find(token_start, lengths, a) || s.block < 0) return;
+  if (!s.find(token_start, lengths, tokens, a) || s.block < 0) return;
   constexpr int kKeys = D * kKvBlock / 8, kValues = D * kKvBlock / 16;          // units: 8 features of a token; 4 features of 4 tokens
   constexpr int kPerK = (kKeys + kThreads - 1) / kThreads, kPerV = (kValues + kThreads - 1) / kThreads;
   float k[kPerK][8], v[kPerV][4][4];
@@ -186,10 +186,10 @@ __global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(const int32_t*
 }
 
 template <int TYPE, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const int32_t* token_start, const int32_t* lengths, const KvArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const int32_t* token_start, const int32_t* lengths, int64_t tokens, const KvArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[D * kRow];
   Share s;
-  if (!s.find(token_start, lengths, a)) return;
+  if (!s.find(token_start, lengths, tokens, a)) return;
   constexpr int kKeys = D * kKvBlock / 8, kValues = D * kKvBlock / 16;
   const bool there = s.block >= 0;
   const uint8_t* kb = a.c.k + (there ? s.block * (D * kKvBlock) : 0);
@@ -236,11 +236,11 @@ __global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(const int32_t* 
 template <int TYPE, int D>
 void launch_type(const KvArgs& a, dim3 grid, bool vec, bool write, hipStream_t s) {
   if (write) {
-    if (vec) kv_cache_write_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
-    else kv_cache_write_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
+    if (vec) kv_cache_write_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a.t.tokens, a);
+    else kv_cache_write_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a.t.tokens, a);
   } else {
-    if (vec) kv_cache_read_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
-    else kv_cache_read_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a);
+    if (vec) kv_cache_read_kernel<TYPE, D, true><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a.t.tokens, a);
+    else kv_cache_read_kernel<TYPE, D, false><<<grid, kThreads, 0, s>>>(a.t.token_start, a.c.lengths, a.t.tokens, a);
   }
 }
 template <int D>
@@ -253,7 +253,7 @@ void launch_dim(const KvArgs& a, dim3 grid, bool vec, bool write, hipStream_t s)
 int move_tokens(const szo_kv_cache* c, const szo_kv_tokens* t, bool write, hipStream_t s) {
   const int rc = check_cache(c);
   if (rc != SZO_OK) return rc;
-  if (!t || !valid_type(t->type) || t->reserved || t->max_new < 0) return SZO_EINVAL;
+  if (!t || !valid_type(t->type) || t->reserved || t->max_new < 0 || t->tokens < 0) return SZO_EINVAL;
   if (t->k_token_stride < 0 || t->k_head_stride < 0 || t->v_token_stride < 0 || t->v_head_stride < 0) return SZO_EINVAL;
   if (!write) {                            // rows that are written may not run into each other
     if (t->k_token_stride < c->head_dim || t->v_token_stride < c->head_dim) return SZO_EINVAL;

@@ -69,7 +69,7 @@ class KvCache(C.Structure):
 
 class KvTokens(C.Structure):
     _fields_ = (_fields(_I32, "type reserved") + _fields(_I64, "max_new") + _fields(_PTR, "token_start k v") +
-                _fields(_I64, "k_token_stride k_head_stride v_token_stride v_head_stride"))
+                _fields(_I64, "k_token_stride k_head_stride v_token_stride v_head_stride tokens"))
 
 
 class AttnDesc(C.Structure):
@@ -360,6 +360,7 @@ def make_kv_tokens(k, v, token_start, max_new):
     t = KvTokens(_type(k), 0, max_new, _typed(token_start, torch.int32, token_start.shape))
     t.k, t.k_token_stride, t.k_head_stride = _strided(k, k.shape)
     t.v, t.v_token_stride, t.v_head_stride = _strided(v, k.shape)
+    t.tokens = k.shape[0]
     t.shape = tuple(k.shape[1:]), token_start.shape[0]
     t.keep = (k, v, token_start)
     return t

@@ -38,3 +38,8 @@ def test_cache_calls_want_lengths_whatever_the_page_table_holds(call, lengths):
     for kw in (dict(max_pages=0), dict(max_pages=0, page_table=None), dict(pages=0, max_pages=0)):
         assert getattr(szo.lib, call)(cache(lengths=lengths, **kw), tokens(), None) == szo.EINVAL
     assert getattr(szo.lib, call)(cache(lengths=lengths, sequences=0, max_pages=0), tokens(), None) == szo.OK
+
+
+@pytest.mark.parametrize("call", ["szo_kv_cache_write", "szo_kv_cache_read"])
+def test_cache_calls_refuse_a_negative_number_of_rows(call):
+    assert getattr(szo.lib, call)(cache(), tokens(tokens=-1), None) == szo.EINVAL
