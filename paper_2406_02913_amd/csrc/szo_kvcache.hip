@@ -267,7 +267,9 @@ int move_tokens(const szo_kv_cache* c, const szo_kv_tokens* t, bool write, hipSt
   a.t = *t;
   a.blocks_per_page = c->page_tokens / kKvBlock;
   const int64_t room = (int64_t)c->max_pages * a.blocks_per_page;            // blocks behind the page table hold nothing
-  int64_t touched = (t->max_new + kKvBlock - 2) / kKvBlock + 1;
+  const int64_t most = std::min<int64_t>({t->max_new, t->tokens, 0x7FFFFFFF});          // new tokens of a sequence; rows are counted in 32 bits
+  if (most == 0) return SZO_OK;
+  int64_t touched = (most + kKvBlock - 2) / kKvBlock + 1;
   if (write) touched = std::min(touched, room);
   if (touched == 0) return SZO_OK;
   if (touched > 65535 || c->sequences > 65535) return SZO_EUNSUPPORTED;

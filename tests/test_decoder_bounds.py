@@ -43,3 +43,13 @@ def test_cache_calls_want_lengths_whatever_the_page_table_holds(call, lengths):
 @pytest.mark.parametrize("call", ["szo_kv_cache_write", "szo_kv_cache_read"])
 def test_cache_calls_refuse_a_negative_number_of_rows(call):
     assert getattr(szo.lib, call)(cache(), tokens(tokens=-1), None) == szo.EINVAL
+
+
+def test_new_tokens_that_no_grid_counts_are_refused():
+    """A hint of any size is met by the rows that there are; what is left of it is counted in 64 bits."""
+    most = 2 ** 63 - 1
+    for new, rows in ((most, most), (most, 2 ** 31 - 1), (most - 7, 1 << 40), (1 << 40, most)):
+        assert szo.lib.szo_kv_cache_read(cache(), tokens(max_new=new, tokens=rows), None) == szo.EUNSUPPORTED
+        assert szo.lib.szo_kv_cache_write(cache(max_pages=1 << 20), tokens(max_new=new, tokens=rows), None) == szo.EUNSUPPORTED
+    for call in (szo.lib.szo_kv_cache_read, szo.lib.szo_kv_cache_write):
+        assert call(cache(), tokens(max_new=most, tokens=0), None) == szo.OK
