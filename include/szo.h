@@ -368,7 +368,9 @@ typedef struct szo_attn_desc {
   int64_t out_token_stride, out_head_stride;
   float* lse;                   /* device [tokens, q_heads]: log of the sum of exp(scale q k), or NULL    */
 } szo_attn_desc;
-/* workspace: device, szo_attn_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs. */
+/* workspace: device, szo_attn_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs.  The size is that of this very descriptor (q_heads,
+ * sequences, kv_heads, head_dim, window, max_q, max_len, tokens): it does not grow with them, since few sequences are split into more parts than many, so a
+ * program that keeps one workspace asks for every descriptor that it will call with, or before each call. */
 int szo_attn_cached(const szo_attn_desc* desc /* host */, void* workspace, void* stream);
 size_t szo_attn_workspace_bytes(const szo_attn_desc* desc /* host */);
 
@@ -394,7 +396,8 @@ typedef struct szo_logprobs_desc {
                                  * in fp64 and a fixed order (logp may then not be NULL)                  */
   double loss_scale;
 } szo_logprobs_desc;
-/* workspace: device, szo_logprobs_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs. */
+/* workspace: device, szo_logprobs_workspace_bytes(desc), 16-byte aligned, for this call alone while it runs.  The size is that of this very descriptor (rows,
+ * vocab, type, top): few rows may need more than many. */
 int szo_token_logprobs(const szo_logprobs_desc* desc /* host */, void* workspace, void* stream);
 size_t szo_logprobs_workspace_bytes(const szo_logprobs_desc* desc /* host */);
 /* Gradient by the logits of a scalar whose gradients by logp and by entropy are grad_logp and grad_entropy (device fp32

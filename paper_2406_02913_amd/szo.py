@@ -278,6 +278,13 @@ def _typed(t, dtype, shape):
     return _dev(t)
 
 
+def _room(workspace, need):
+    """Pointer of a workspace of at least as many bytes (None -> NULL: the call says whether it can do without)."""
+    if workspace is not None and workspace.nbytes < need:
+        raise ValueError(f"a workspace of {workspace.nbytes} bytes, this call needs {need}")
+    return _dev(workspace)
+
+
 def make_qk_desc(q, k, positions, cos_table, sin_table, q_out=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, norm=None):
     """q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (or None), any strides with a contiguous last axis; tables fp32
     [rows, rot_dim / 2] (None: no rotation).  `norm` is on where a weight is given, unless said otherwise.  Without outputs: for the backward."""
@@ -325,7 +332,8 @@ def szo_qk_norm_rope(desc, stream=None):
 def szo_qk_norm_rope_bwd(desc, grads, workspace=None, stream=None):
     if grads.shapes != ((desc.tokens, desc.q_heads, desc.head_dim), desc.kv_heads, desc.in_type):
         raise ValueError("gradients of other shapes or another type than the inputs")
-    _check("szo_qk_norm_rope_bwd", lib.szo_qk_norm_rope_bwd(C.byref(desc), C.byref(grads), _dev(workspace), _stream(stream)))
+    need = lib.szo_qk_workspace_bytes(C.byref(desc)) if grads.q_weight_grad or grads.k_weight_grad else 0
+    _check("szo_qk_norm_rope_bwd", lib.szo_qk_norm_rope_bwd(C.byref(desc), C.byref(grads), _room(workspace, need), _stream(stream)))
 
 
 def szo_qk_workspace_bytes(desc):
@@ -399,7 +407,9 @@ def make_attn_desc(cache, q, out, q_start, max_q, max_len, scale, causal=True, w
 
 
 def szo_attn_cached(desc, workspace=None, stream=None):
-    _check("szo_attn_cached", lib.szo_attn_cached(C.byref(desc), _dev(workspace), _stream(stream)))
+    """workspace: of szo_attn_workspace_bytes() for this very descriptor; fewer sequences or a longer max_len may need more than a larger batch did."""
+    room = _room(workspace, lib.szo_attn_workspace_bytes(C.byref(desc)))
+    _check("szo_attn_cached", lib.szo_attn_cached(C.byref(desc), room, _stream(stream)))
 
 
 def szo_attn_workspace_bytes(desc):
@@ -423,7 +433,9 @@ def make_logprobs_desc(logits, targets=None, logp=None, entropy=None, stats=None
 
 
 def szo_token_logprobs(desc, workspace=None, stream=None):
-    _check("szo_token_logprobs", lib.szo_token_logprobs(C.byref(desc), _dev(workspace), _stream(stream)))
+    """workspace: of szo_logprobs_workspace_bytes() for this very descriptor; fewer rows may need more than many did."""
+    room = _room(workspace, lib.szo_logprobs_workspace_bytes(C.byref(desc)))
+    _check("szo_token_logprobs", lib.szo_token_logprobs(C.byref(desc), room, _stream(stream)))
 
 
 def szo_logprobs_workspace_bytes(desc):

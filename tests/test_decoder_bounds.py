@@ -1,7 +1,7 @@
 """Sizes of workspaces and bounds that the calls between the linear layers keep to: on the host, no kernel is launched."""
 import pytest
 
-from test_decoder_refusals import P, attn, cache, logp, tokens
+from test_decoder_refusals import P, attn, cache, grads, logp, qk, tokens
 from paper_2406_02913_amd import szo
 
 
@@ -53,3 +53,45 @@ def test_new_tokens_that_no_grid_counts_are_refused():
         assert szo.lib.szo_kv_cache_write(cache(max_pages=1 << 20), tokens(max_new=new, tokens=rows), None) == szo.EUNSUPPORTED
     for call in (szo.lib.szo_kv_cache_read, szo.lib.szo_kv_cache_write):
         assert call(cache(), tokens(max_new=most, tokens=0), None) == szo.OK
+
+
+class Room:
+    """What the binding asks of a device tensor, without a device."""
+    is_cuda = True
+
+    def __init__(self, nbytes):
+        self.nbytes = nbytes
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+def decode(sequences, **kw):
+    """One token each of sequences of up to 4000 tokens, 32 query and 8 key heads of 128."""
+    return attn(q_heads=32, max_q=1, tokens=sequences, max_len=4000, q_token_stride=4096, out_token_stride=4096,
+                cache=cache(kv_heads=8, sequences=sequences, max_pages=100, page_tokens=64), **kw)
+
+
+def test_a_workspace_for_a_larger_batch_may_be_too_small_for_a_smaller_one_and_is_refused():
+    size = {n: szo.szo_attn_workspace_bytes(decode(n)) for n in (8, 16, 64, 128)}
+    assert size[8] > size[16] and size[64] > size[128]             # fewer sequences are split into more parts
+    for n in size:
+        for room in (size[n] - 1, size[128], 16):
+            if room < size[n]:
+                with pytest.raises(ValueError, match="workspace"):
+                    szo.szo_attn_cached(decode(n), Room(room), stream=0)
+
+
+def test_workspaces_of_log_probabilities_and_of_weight_gradients_are_checked():
+    d = logp(rows=4, vocab=131072, row_stride=131072, top=5)
+    size = szo.szo_logprobs_workspace_bytes(d)
+    assert size > 16 and szo.szo_logprobs_workspace_bytes(logp(rows=600, vocab=131072, row_stride=131072, top=5)) == 16
+    with pytest.raises(ValueError, match="workspace"):
+        szo.szo_token_logprobs(d, Room(size - 1), stream=0)
+    g = grads()
+    g.shapes = (4, 2, 64), 1, szo.F32
+    with pytest.raises(ValueError, match="workspace"):
+        szo.szo_qk_norm_rope_bwd(qk(), g, Room(szo.szo_qk_workspace_bytes(qk()) - 1), stream=0)
