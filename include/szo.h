@@ -373,6 +373,9 @@ typedef struct szo_attn_desc {
  * program that keeps one workspace asks for every descriptor that it will call with, or before each call. */
 int szo_attn_cached(const szo_attn_desc* desc /* host */, void* workspace, void* stream);
 size_t szo_attn_workspace_bytes(const szo_attn_desc* desc /* host */);
+/* Inspection: how the call goes about this descriptor.  plan[0]: tiles of 32 rows side by side in a workgroup (4 or 1), plan[1]: waves that share a tile's cache,
+ * plan[2]: parts of the cache, plan[3]: 1 where codes pass the caches by; all 0 where there is nothing to do. */
+int szo_attn_plan(const szo_attn_desc* desc /* host */, int32_t* plan /* host, 4 */);
 
 /* Log probabilities of given tokens under softmax(scale * logits), row by row, in one pass over the logits:
  *   logp = scale x_target - log sum exp(scale x)      entropy = -sum p log p      alternatives: the `top` largest logits

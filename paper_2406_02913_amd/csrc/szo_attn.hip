@@ -633,6 +633,18 @@ size_t szo_attn_workspace_bytes(const szo_attn_desc* d) {
   return (size_t)d->cache.sequences * d->cache.kv_heads * p.tiles * p.wr * p.splits * part_floats(p.rows_cap, d->cache.head_dim) * sizeof(float);
 }
 
+int szo_attn_plan(const szo_attn_desc* d, int32_t* plan) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!plan) return SZO_EINVAL;
+  const Plan p = nothing(d) ? Plan{} : plan_of(d);
+  plan[0] = p.wr;
+  plan[1] = p.wk;
+  plan[2] = p.splits;
+  plan[3] = p.once;
+  return SZO_OK;
+}
+
 int szo_attn_cached(const szo_attn_desc* d, void* workspace, void* stream) {
   const int rc = check(d);
   if (rc != SZO_OK) return rc;

@@ -123,6 +123,7 @@ _SIGS = {
     "szo_kv_cache_write": (C.c_int, [_P(KvCache), _P(KvTokens), C.c_void_p]),
     "szo_kv_cache_read": (C.c_int, [_P(KvCache), _P(KvTokens), C.c_void_p]),
     "szo_attn_cached": (C.c_int, [_P(AttnDesc), C.c_void_p, C.c_void_p]),
+    "szo_attn_plan": (C.c_int, [_P(AttnDesc), C.c_void_p]),
     "szo_attn_workspace_bytes": (C.c_size_t, [_P(AttnDesc)]),
     "szo_token_logprobs": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p]),
     "szo_logprobs_workspace_bytes": (C.c_size_t, [_P(LogprobsDesc)]),
@@ -414,6 +415,13 @@ def szo_attn_cached(desc, workspace=None, stream=None):
 
 def szo_attn_workspace_bytes(desc):
     return int(lib.szo_attn_workspace_bytes(C.byref(desc)))
+
+
+def szo_attn_plan(desc):
+    """(tiles of rows side by side, waves that share a tile's cache, parts of the cache, codes pass the caches by)"""
+    plan = (C.c_int32 * 4)()
+    _check("szo_attn_plan", lib.szo_attn_plan(C.byref(desc), plan))
+    return tuple(plan)
 
 
 def make_logprobs_desc(logits, targets=None, logp=None, entropy=None, stats=None, top_logp=None, top_index=None, scale=1.0, loss_acc=None, loss_scale=1.0):

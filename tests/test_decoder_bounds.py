@@ -95,3 +95,11 @@ def test_workspaces_of_log_probabilities_and_of_weight_gradients_are_checked():
     g.shapes = (4, 2, 64), 1, szo.F32
     with pytest.raises(ValueError, match="workspace"):
         szo.szo_qk_norm_rope_bwd(qk(), g, Room(szo.szo_qk_workspace_bytes(qk()) - 1), stream=0)
+
+
+def test_the_way_of_a_call_can_be_asked():
+    assert szo.szo_attn_plan(decode(1))[2] > 1 and szo.szo_attn_plan(decode(128))[2] == 1
+    assert szo.szo_attn_plan(attn(tokens=0)) == (0, 0, 0, 0)
+    assert szo.lib.szo_attn_plan(attn(), None) == szo.EINVAL
+    with pytest.raises(szo.SzoError):
+        szo.szo_attn_plan(attn(type=szo.F32))
