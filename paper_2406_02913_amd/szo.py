@@ -295,7 +295,7 @@ def make_qk_desc(q, k, positions, cos_table, sin_table, q_out=None, k_out=None, 
     if k is not None and k.dtype != q.dtype or (q_out is not None and k_out is not None and q_out.dtype != k_out.dtype):
         raise ValueError("queries and keys are of one type, and so are their outputs")
     rows, rot = (0, 0) if cos_table is None else (cos_table.shape[0], 2 * cos_table.shape[1])
-    out = q_out if q_out is not None else q
+    out = q_out if q_out is not None else k_out if k_out is not None else q
     d = QkDesc(T, heads, kv, D, rot, _type(q), _type(out), int((q_weight is not None or k_weight is not None) if norm is None else norm), int(interleaved), eps, 0)
     d.q, d.q_token_stride, d.q_head_stride = _strided(q, (T, heads, D))
     d.k, d.k_token_stride, d.k_head_stride = _strided(k, (T, kv, D))

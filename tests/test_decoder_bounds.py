@@ -1,8 +1,9 @@
 """Sizes of workspaces and bounds that the calls between the linear layers keep to: on the host, no kernel is launched."""
 import pytest
+import torch
 
-from test_decoder_refusals import P, attn, cache, grads, logp, qk, tokens
 from paper_2406_02913_amd import szo
+from test_decoder_refusals import P, attn, cache, grads, logp, qk, tokens
 
 
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
@@ -103,3 +104,18 @@ def test_the_way_of_a_call_can_be_asked():
     assert szo.lib.szo_attn_plan(attn(), None) == szo.EINVAL
     with pytest.raises(szo.SzoError):
         szo.szo_attn_plan(attn(type=szo.F32))
+
+
+def fake(shape, dtype=torch.float32):
+    """A tensor that says it is on the device; nothing is launched with it."""
+    class On(torch.Tensor):
+        is_cuda = True
+
+    return torch.empty(shape, dtype=dtype).as_subclass(On)
+
+
+def test_a_call_for_keys_alone_goes_by_the_type_of_its_output():
+    d = szo.make_qk_desc(fake((4, 0, 64)), fake((4, 2, 64)), None, None, None, None, fake((4, 2, 64), torch.bfloat16), norm=True)
+    assert (d.in_type, d.out_type) == (szo.F32, szo.BF16)
+    d = szo.make_qk_desc(fake((4, 2, 64)), None, None, None, None, fake((4, 2, 64), torch.float16), norm=True)
+    assert (d.in_type, d.out_type) == (szo.F32, szo.F16)
