@@ -311,15 +311,16 @@ def make_qk_desc(q, k, positions, cos_table, sin_table, q_out=None, k_out=None, 
 
 def make_qk_grads(q_out_grad, k_out_grad, q_grad, k_grad, q_weight_grad=None, k_weight_grad=None):
     import torch
-    D = q_grad.shape[2]
+    T, _, D = q_grad.shape
     if k_grad is not None and (k_grad.dtype != q_grad.dtype or k_out_grad.dtype != q_out_grad.dtype):
         raise ValueError("gradients of queries and keys are of one type")
     g = QkGrads(_type(q_out_grad), 0)
     g.q_out_grad, g.q_out_token_stride, g.q_out_head_stride = _strided(q_out_grad, q_grad.shape)
     g.q_grad, g.q_token_stride, g.q_head_stride = _strided(q_grad, q_grad.shape)
     if k_grad is not None:
-        g.k_out_grad, g.k_out_token_stride, g.k_out_head_stride = _strided(k_out_grad, k_grad.shape)
-        g.k_grad, g.k_token_stride, g.k_head_stride = _strided(k_grad, k_grad.shape)
+        shape = (T, k_grad.shape[1], D)
+        g.k_out_grad, g.k_out_token_stride, g.k_out_head_stride = _strided(k_out_grad, shape)
+        g.k_grad, g.k_token_stride, g.k_head_stride = _strided(k_grad, shape)
     g.q_weight_grad, g.k_weight_grad = _typed(q_weight_grad, torch.float32, (D,)), _typed(k_weight_grad, torch.float32, (D,))
     g.shapes = tuple(q_grad.shape), (0 if k_grad is None else k_grad.shape[1]), _type(q_grad)
     g.keep = (q_out_grad, k_out_grad, q_grad, k_grad, q_weight_grad, k_weight_grad)

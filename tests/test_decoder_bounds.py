@@ -119,3 +119,16 @@ def test_a_call_for_keys_alone_goes_by_the_type_of_its_output():
     assert (d.in_type, d.out_type) == (szo.F32, szo.BF16)
     d = szo.make_qk_desc(fake((4, 2, 64)), None, None, None, None, fake((4, 2, 64), torch.float16), norm=True)
     assert (d.in_type, d.out_type) == (szo.F32, szo.F16)
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 64), (5, 1, 64), (4, 1, 32), (4, 2, 64)])
+def test_gradients_of_keys_have_the_tokens_and_features_of_the_queries(shape):
+    """The call goes by the inputs' numbers of tokens, heads and features: buffers of others are refused."""
+    d = qk()                                      # 4 tokens, 2 + 1 heads of 64
+    q = fake((4, 2, 64))
+    with pytest.raises(ValueError):
+        szo.szo_qk_norm_rope_bwd(d, szo.make_qk_grads(q, fake(shape), q, fake(shape)), None, stream=0)
+    with pytest.raises(ValueError):
+        szo.make_qk_grads(q, fake((4, 1, 64)), q, fake((4, 3, 64)))
+    with pytest.raises(ValueError):
+        szo.make_qk_grads(fake((3, 2, 64)), None, q, None)
