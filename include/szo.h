@@ -254,8 +254,13 @@ int szo_workspace_init(void* workspace, void* stream);
  * scalar f of Definition 1 for a language model is their negative mean).  The same conventions as above: the
  * calls enqueue on `stream`, allocate nothing, never synchronise, and can be captured into a HIP graph.  Strides count
  * elements; the last axis of every tensor is contiguous.  SZO_EUNSUPPORTED, with nothing enqueued: head dimensions and numbers of
- * alternatives other than those named below, more than 65535 key heads or sequences, and calls of more threads than a launch
- * counts in 32 bits (about 16 million rows or tokens). */
+ * alternatives other than those named below; a cache of more than 65535 key heads or sequences; more than 65536 heads of norms; a vocabulary above 2^30;
+ * and calls of more workgroups than a launch takes:
+ *   norms and rotation             2^24 - 1 workgroups, of one token each or, with few heads, of several
+ *   log probabilities              2^24 - 1 rows
+ *   their gradient                 2^24 - 1 pieces of rows, 4096 logits each in fp32, 8192 in 16 bits (2.1 and 4.2 million rows of 32000)
+ *   cache write and read           65535 blocks of one sequence (2.1 million new tokens)
+ *   attention                      65535 tiles of 32 rows of one key head (of 128 where four go side by side), times parts */
 
 /* Element types of these calls. */
 #define SZO_F32   0
@@ -349,7 +354,8 @@ int szo_kv_cache_read(const szo_kv_cache* cache /* host */, const szo_kv_tokens*
  * keys and values among it):
  *   out = softmax(scale q K^T) V over the positions that a query sees.  Query i of n of a sequence with `length` tokens
  *   stands at position p = length - n + i and sees positions [0, length), with `causal` up to p, with window > 0 from
- *   p - window + 1 on.  A query that sees nothing gives 0, and lse -inf.
+ *   p - window + 1 on.  A query that sees nothing gives 0, and lse -inf;
+ * so does one whose every score is -inf (an infinity in q).
  * q_heads is a multiple of kv_heads; query head h reads key head h / (q_heads / kv_heads).  What lies behind the length, or
  * in masked places, has no influence, NaN included.  Scores, statistics and sums are fp32; the weights of the values are
  * rounded to fp16 (11 significant bits, relative to the largest of the row), the output once to `type`. */
@@ -407,7 +413,7 @@ size_t szo_logprobs_workspace_bytes(const szo_logprobs_desc* desc /* host */);
  * [rows], either may be NULL):
  *   grad_logits = scale (grad_logp (1[v = target] - p) - grad_entropy p (log p + entropy))
  * from the forward's stats (and entropy, if grad_entropy is not NULL).  grad_logits: device, type of the logits, rows
- * grad_row_stride apart; may be the logits' own buffer.  The other outputs of the descriptor are not touched. */
+ * grad_row_stride apart; may be the logits' own buffer, with the logits' row_stride.  The other outputs of the descriptor are not touched. */
 int szo_token_logprobs_bwd(const szo_logprobs_desc* desc /* host */, const float* grad_logp, const float* grad_entropy,
                            void* grad_logits, int64_t grad_row_stride, void* stream);
 

@@ -214,8 +214,9 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
 // one step do not depend on each other.  The arguments that the first loads need come first, where they are in registers when a wave starts; the page of the
 // first block is read along with the lengths, for the case that it starts there.  Codes are asked for a step before they are used (two steps: 562 -> 596 us for a prompt of 8192,
 // registers run out).
-//   A prompt of 8192 tokens with 32 query and 8 key heads of 128, causal: 570 us, 965 TFLOP/s, bound by the issue of instructions: matrix products take 45 % of
-// the cycles, and a step has 182 vector instructions beside 16 products.  One token of each of 64 sequences of up to 8192: 107 us, 5.76 TB/s of the cache.
+//   A prompt of 8192 tokens with 32 query and 8 key heads of 128, causal: 577 us, 953 TFLOP/s, bound by the issue of instructions: matrix products take 44 % of
+// the cycles, and a step has 186 vector instructions beside 16 products.  One token of each of 64 sequences of up to 8192: 108 us, 5.73 TB/s of the cache.
+// 4096 tokens in bf16 with head dimensions of 64, 96, 128, 256: 124, 138, 168, 393 us (556, 748, 820, 699 TFLOP/s), in fp16 110, 140, 166, 383.
 template <int TYPE, int D, int WR, int WK, bool ONCE>
 __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
                                                                                    int max_pages, int bpp, int splits, int tiles, const AttnArgs a) {
@@ -518,9 +519,10 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
 //   With few workgroups a tile's cache is split over several, and a second kernel joins the parts.  That costs 2 us where a tile has few rows and 4 to 6
 // with 32, whose parts are 16 KiB each, and every workgroup 5 us to begin and to end: few rows go to up to 512 workgroups with a single block a wave (from 64
 // workgroups on with four), full tiles to 256 with four blocks a wave, and to twice as many of either only in caches of thousands.  us of parts 1, 2, 4, 8, 16, 32,
-// one token each: 1 sequence of 1000 10.3, 10.2, 8.6, 8.1, 8.1, 8.3; 1 of 8000 53, 33, 21, 14.7, 11.2, 9.6; 8 of 4000 35, 23, 17, 18, 20, 26; 16 of 8000 80, 49, 46,
-// 50, 56, 70; 32 of 1000 14, 18, 21; 64 of 500 to 8192 110, 106, 105.  64 tokens of one sequence (8 tiles for each key head) behind 2000 16.7, 15.8, 14.3, 18.6;
-// behind 8000 59, 38, 25, 24, 32; 200 tokens behind 4000 29, 32, 39, behind 8000 60, 47, 55.
+// one token each: 1 sequence of 1000 10.7, 10.6, 9.0, 8.5, 8.5, 8.6; 1 of 8000 54, 33, 21, 15.2, 11.8, 10.4; 8 of 4000 35, 24, 17, 18, 21, 27; 16 of 8000 81, 50, 46,
+// 51, 58, 74; 32 of 1000 14, 18, 21; 64 of 500 to 8192 111, 107, 106.  64 tokens of one sequence (8 tiles for each key head) behind 2000 17.2, 16.1, 14.7, 19.7;
+// behind 8000 60, 38, 25, 25, 34; 200 tokens, four waves a tile, behind 4000 29, 32, 39, behind 8000 60, 47, 55.  All with 32 query heads of 128 in bf16: the rule counts
+// blocks and tiles, and has not been measured for other head dimensions.
 //   Between 65 and 256 workgroups, a CU each, eight waves share a tile's cache of 1000 tokens or more instead of four (wk): 8 x 29 answers behind up to 2000
 // 20.3 -> 16.4 us, 200 tokens behind 2000 17.0 -> 15.5, behind 8000 47 -> 40; with fewer workgroups parts are better (one token behind 8000 10.2 -> 10.6),
 // and short tiles read enough at once when three quarters of the CUs have one (32 sequences of 1000 14.2 -> 15.2).

@@ -7,8 +7,8 @@
 // the maximum and the conversion.  Values lie transposed in the cache (the order of a matrix operand): whole blocks go through LDS, so that
 // both sides of the transposition are wide and contiguous.  A few tokens into a block that is there already take their bytes one by one: a decoding
 // step moves a few hundred bytes per head and is bound by latency, not by them.
-//   Eight prompts, 4096 tokens together, 32 heads of 128, from fp32: 34.7 us, 4.8 TB/s of what is read and written (a copy of 2 GiB runs at 4.85); one token to each of
-// 64 sequences, 8 heads: 4.7 us, four reads that wait for each other; 8192 tokens of 8 heads back as bf16: 9.9 us, 5.1 TB/s.
+//   Eight prompts, 4096 tokens together, 32 heads of 128, from fp32: 34.9 us, 4.8 TB/s of what is read and written (a copy of 2 GiB runs at 4.85); one token to each of
+// 64 sequences, 8 heads: 4.9 us, four reads that wait for each other; 8192 tokens of 8 heads back as bf16: 10.2 us, 4.9 TB/s.
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_kv.h"

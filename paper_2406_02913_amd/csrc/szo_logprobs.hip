@@ -8,6 +8,8 @@
 // few others reach it (of 32 groups, 31 logits for 20 alternatives): the threads whose maximum does look through their elements again, and what they
 // find is ranked.
 // With few rows a row is split over workgroups, whose parts a second kernel joins.
+//   Rows with NaN or infinities, with fewer finite logits than alternatives, or with more than 1024 that reach the bound are gone through once for each alternative instead,
+// element by element: with 5 of 32000 logits not masked and 20 alternatives 400 us for 16 rows (9 without a mask), 2330 for 4096 (97).
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_types.h"
@@ -307,10 +309,11 @@ __global__ void __launch_bounds__(1024) logp_loss_kernel(const float* __restrict
 struct GradArgs { szo_logprobs_desc d; const float *g_logp, *g_entropy; void* out; int64_t out_stride; int parts; };
 
 constexpr int kGradThreads = 256;
-constexpr int kGradChunks = 4;             // 16-byte pieces of a thread
+constexpr int kGradChunks = 4;             // 16-byte pieces of a thread, one after the other
 
 // dx = scale (g (1[v = target] - p) - h p (log p + H)), p from the row's maximum and sum: logits are read once and as much is written, 16 bytes a
-// lane, four on the way, several workgroups a row.  Bound by memory: 4096 rows of 32000 in bf16 96 us, 5.5 TB/s of both.
+// lane, several workgroups a row.  A thread's four pieces come one after the other: the output may be the input, so no load passes a store.  Bound by memory:
+// 4096 rows of 32000 in bf16 96 us, 5.5 TB/s of both.
 template <int TYPE>
 __global__ void __launch_bounds__(kGradThreads) token_logprobs_bwd_kernel(const GradArgs a) {
   typedef Chunk<TYPE> C;

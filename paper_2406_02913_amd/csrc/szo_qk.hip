@@ -148,8 +148,8 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkArgs arg
 // A group of lanes takes query heads or key heads, never both, so that it holds one side's weights and sums.  The weights' gradients: every lane
 // adds up its features over the heads and tokens of its workgroup, the workgroup adds its groups in LDS and leaves one partial per feature; a
 // second kernel adds those.  No atomics, so the order is fixed.  Small workgroups, five of them on a CU
-// by their registers (90): 4096 tokens of 32 + 32 heads of 128 in bf16 46 us (4.4 TB/s; a copy of 4 GB runs at 4.85), with both sides in every lane and workgroups of
-// 1024 threads, one on a CU, 58.
+// by their registers (90; the forms of fp32 inputs with 16-bit gradients keep 8 bytes a lane in memory for it, which has not been measured against four): 4096 tokens
+// of 32 + 32 heads of 128 in bf16 47 us (4.3 TB/s; a copy of 4 GB runs at 4.85), with both sides in every lane and workgroups of 1024 threads, one on a CU, 58.
 template <int IN, int OUT, int L, bool VEC>
 __global__ void __launch_bounds__(kThreads, 5) qk_norm_rope_bwd_kernel(const QkArgs args) {
   constexpr int kGroups = kThreads / L;
