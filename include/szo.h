@@ -270,6 +270,47 @@ int szo_workspace_init(void* workspace, void* stream);
 /* Largest size of a scale of logits or scores: beyond it scale * log2(e), which they are multiplied by, is infinite. */
 #define SZO_MOST_SCALE 2.35e38f
 
+/* Norms after and before a block, its gate and the residual stream: for each token
+ *   a = post(y)  (y itself without `post`),   h' = h_scale h + y_scale gate a,   x = pre(h')
+ * where a norm is (v - mean) / sqrt(var + eps) * weight + bias over the row, with mean 0 and var the mean square for SZO_NORM_RMS.
+ * y is what a block's last linear gives, h the residual stream, x what the next block's linears (or the head) take.  y NULL: no block in
+ * front (h' = h_scale h); h NULL: no stream yet (0); outputs that are NULL are not computed; weights that are NULL are 1, biases 0, a gate 1.  The gate is
+ * one row for every token, or one for all with gate_stride 0.  Sums and products in fp32, each output rounded once to its type, x from the unrounded h'.
+ * Squares are fp32: values above 1e19 give infinities.  An output may be an input's own buffer, with its type and stride. */
+#define SZO_NORM_RMS   0
+#define SZO_NORM_LAYER 1
+typedef struct szo_block_desc {
+  int64_t tokens;
+  int32_t width;                /* 1 to 16384                                                            */
+  int32_t y_type, h_type, x_type;     /* SZO_F32, SZO_BF16 or SZO_F16; h_type: of h and h_out            */
+  int32_t norm, post;           /* SZO_NORM_RMS or SZO_NORM_LAYER; 0 or 1                                */
+  float   eps, y_scale, h_scale;
+  int32_t reserved;             /* 0                                                                     */
+  const void *y, *h;            /* device [tokens, width]; strides of tokens count elements              */
+  const float *post_weight, *post_bias, *pre_weight, *pre_bias;    /* device fp32 [width]                */
+  const float* gate;            /* device fp32 [tokens, width], or [width] with gate_stride 0            */
+  void *h_out, *x_out;          /* device [tokens, width]                                                */
+  int64_t y_stride, h_stride, gate_stride, h_out_stride, x_out_stride;
+} szo_block_desc;
+
+/* Gradients of a scalar by the outputs (read; NULL: 0) and by the inputs (overwritten; NULL: not wanted; SZO_EINVAL for those of an input that
+ * is not there).  Types are those of the descriptor. */
+typedef struct szo_block_grads {
+  const void *x_out_grad, *h_out_grad;
+  void *y_grad, *h_grad;
+  float* gate_grad;             /* like the gate: with gate_stride 0 the sum over tokens                  */
+  float *post_weight_grad, *post_bias_grad, *pre_weight_grad, *pre_bias_grad;
+  int64_t x_out_stride, h_out_stride, y_stride, h_stride, gate_stride;
+  int64_t reserved;             /* 0                                                                     */
+} szo_block_grads;
+
+int szo_block_norm(const szo_block_desc* desc /* host */, void* stream);
+/* Backward of it from the same inputs (h as it was before the call; h_out and x_out are not read).  Sums over tokens are added up in a fixed
+ * order.  y_grad and h_grad may be the buffers of y and h, or of the outputs' gradients.  workspace: device, szo_block_workspace_bytes(desc), 16-byte aligned, for this
+ * call alone while it runs; may be NULL if no sum over tokens is wanted. */
+int szo_block_norm_bwd(const szo_block_desc* desc /* host */, const szo_block_grads* grads /* host */, void* workspace, void* stream);
+size_t szo_block_workspace_bytes(const szo_block_desc* desc /* host */);
+
 /* Queries and keys of a batch of tokens: for each token and head
  *   u = x * w / sqrt(mean(x^2) + eps)      (norm != 0; w = 1 where the weight is NULL; u = x without norm)
  *   out = u, its first rot_dim features turned pairwise by the angles of the token's position:

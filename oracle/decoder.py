@@ -1,5 +1,6 @@
 """What stands between a decoder block's linear layers and behind its head, in 64 bits and from the formulas: norms of queries and keys
-with the position rotation (and gradients), the 8-bit key/value cache, attention over it, token log probabilities (and gradients).
+with the position rotation (and gradients), norms around a block with its gate and the residual stream (and gradients), the 8-bit key/value cache, attention
+over it, token log probabilities (and gradients), from logits or from final states.
 numpy only, plain loops over blocks and sequences; nothing here is fast."""
 import numpy as np
 
@@ -37,6 +38,60 @@ def qk_norm_rope_bwd(x, w, eps, cos, sin, dout, interleaved=False, norm=True):
     r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
     h, u = x * r, g * (1.0 if w is None else w.astype(np.float64))
     return r * (u - h * (u * h).mean(-1, keepdims=True)), (g * h).sum((0, 1))
+
+
+# ---- norms around a block -------------------------------------------------------------------------
+def _unit(v, eps, layer):
+    """(normed rows, what they were multiplied by)"""
+    v = v - v.mean(-1, keepdims=True) if layer else v
+    r = 1.0 / np.sqrt((v * v).mean(-1, keepdims=True) + eps)
+    return v * r, r
+
+
+def _one(w, otherwise):
+    return otherwise if w is None else np.asarray(w, dtype=np.float64)
+
+
+def block_norm(y, h, eps, layer=False, post=False, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None, y_scale=1.0, h_scale=1.0):
+    """(residual stream behind the block, next block's input); y or h may be None."""
+    stream = h_scale * h.astype(np.float64) if h is not None else 0.0
+    if y is not None:
+        a = y.astype(np.float64)
+        if post:
+            a = _unit(a, eps, layer)[0] * _one(post_weight, 1.0) + _one(post_bias, 0.0)
+        stream = stream + y_scale * _one(gate, 1.0) * a
+    return stream, _unit(stream, eps, layer)[0] * _one(pre_weight, 1.0) + _one(pre_bias, 0.0)
+
+
+def _unit_bwd(u, unit, r, layer):
+    d = u - unit * (u * unit).mean(-1, keepdims=True)
+    return r * (d - u.mean(-1, keepdims=True) if layer else d)
+
+
+def block_norm_bwd(y, h, eps, gx, gh, layer=False, post=False, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None, y_scale=1.0, h_scale=1.0):
+    """Gradients by every input, as a dict; gx, gh: by the two outputs (None: 0)."""
+    stream, _ = block_norm(y, h, eps, layer, post, post_weight, post_bias, gate, pre_weight, pre_bias, y_scale, h_scale)
+    g, out = np.zeros_like(stream) if gh is None else gh.astype(np.float64), {}
+    if gx is not None:
+        gx = gx.astype(np.float64)
+        unit, r = _unit(stream, eps, layer)
+        out["pre_weight"], out["pre_bias"] = (gx * unit).sum(0), gx.sum(0)
+        g = g + _unit_bwd(gx * _one(pre_weight, 1.0), unit, r, layer)
+    out["h"] = h_scale * g
+    if y is None:
+        return out
+    a = y.astype(np.float64)
+    if post:
+        unit, r = _unit(a, eps, layer)
+        a = unit * _one(post_weight, 1.0) + _one(post_bias, 0.0)
+    into = y_scale * g * a
+    out["gate"] = into.sum(0) if gate is not None and gate.ndim == 1 else into
+    g = y_scale * g * _one(gate, 1.0)
+    if post:
+        out["post_weight"], out["post_bias"] = (g * unit).sum(0), g.sum(0)
+        g = _unit_bwd(g * _one(post_weight, 1.0), unit, r, layer)
+    out["y"] = g
+    return out
 
 
 # ---- 8-bit cache -----------------------------------------------------------------------------------

@@ -1,0 +1,547 @@
+// Norms after and before a block with its gate and the residual stream, forward and backward (definition: szo.h).
+//
+//   a = post(y),  h' = h_scale h + y_scale gate a,  x = pre(h');   a norm: unit = (v - mean) r,  r = 1 / sqrt(var + eps),  out = unit w + b
+//   (RMS norms: mean 0).  Backward, with u = gx w_pre and unit of h':
+//     gh' = gh_out + r (u - [mean u] - unit mean(u unit)),   dw = sum over tokens of gx unit,   db = sum of gx
+//     dh = h_scale gh',   dgate = y_scale a gh',   da = y_scale gate gh',   dy from da as gh' from gx
+//
+// Bound by memory: a row is read once and written once, and everything between stays in registers.  A row belongs to 1 to 16 waves, eight neighbouring
+// features of it to a thread (16 above 8192 features), so that a wave's loads are whole lines and a row's statistics are one exchange through LDS: the
+// variance comes from each wave's own mean and squares about it, joined as sums of squares about means are, which loses nothing where the mean is large.
+#include <algorithm>
+#include "szo_internal.h"
+#include "szo_types.h"
+
+namespace szo {
+namespace {
+
+constexpr int kMostWidth = 16384, kMostWaves = 16;
+constexpr int kSets = 5;             // sums over tokens: pre weight, pre bias, post weight, post bias, gate
+enum Set { kPreWeight, kPreBias, kPostWeight, kPostBias, kGate };
+
+struct BlockArgs {
+  szo_block_desc d;
+  szo_block_grads g;
+  float* partials;                   // [workgroups][sets][width]
+  int set_at[kSets], sets;           // place of each sum among the partials, -1: not wanted
+  int waves;                         // of a row
+};
+
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+
+// Eight features of a row: neighbours, or with VEC false a row's threads apart.
+template <bool VEC> struct Place {
+  int first, step, width;
+  __device__ __forceinline__ Place() : first(0), step(0), width(0) {}
+  __device__ __forceinline__ Place(int chunk, int thread, int threads, int width_)
+      : first(VEC ? (chunk * threads + thread) * 8 : chunk * 8 * threads + thread), step(VEC ? 1 : threads), width(width_) {}
+  __device__ __forceinline__ int at(int i) const { return first + i * step; }
+  __device__ __forceinline__ bool on(int i) const { return VEC ? first < width : at(i) < width; }
+};
+
+// As they lie in memory.  Loads and conversions are apart, so that the type, which is the same for the whole launch and not worth 27 kernels, is asked for
+// between them without waiting for the first of several loads.
+struct Raw { words4 a, b; };
+
+template <bool VEC>
+__device__ __forceinline__ Raw fetch(const void* base, int type, int64_t row, const Place<VEC>& p) {
+  Raw r = {};
+  if constexpr (VEC) {
+    if (base && p.first < p.width) {
+      const char* at = static_cast<const char*>(base) + (row + p.first) * (type == SZO_F32 ? 4 : 2);
+      r.a = *reinterpret_cast<const words4*>(at);
+      if (type == SZO_F32) r.b = *reinterpret_cast<const words4*>(at + 16);
+    }
+  } else {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = 0.f;
+      if (base && p.on(i)) {
+        const int64_t at = row + p.at(i);
+        v[i] = type == SZO_F32 ? static_cast<const float*>(base)[at]
+                               : type == SZO_BF16 ? (float)static_cast<const __bf16*>(base)[at] : (float)static_cast<const _Float16*>(base)[at];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { r.a[i] = __float_as_uint(v[i]); r.b[i] = __float_as_uint(v[4 + i]); }
+  }
+  return r;
+}
+
+template <bool VEC>
+__device__ __forceinline__ void widen(const Raw& r, int type, float (&v)[8]) {
+  if (!VEC || type == SZO_F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(r.a[i]); v[4 + i] = __uint_as_float(r.b[i]); }
+  } else if (type == SZO_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r.a[i] << 16); v[2 * i + 1] = __uint_as_float(r.a[i] & 0xFFFF0000u); }
+  } else {
+    const f16x8 h = __builtin_bit_cast(f16x8, r.a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+  }
+}
+
+template <bool VEC, int TYPE>
+__device__ __forceinline__ void put_as(void* base, int64_t row, const Place<VEC>& p, const float (&v)[8]) {
+  if constexpr (VEC) {
+    if (p.first < p.width) store_f32<TYPE, 8, true>(base, row + p.first, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p.on(i)) static_cast<typename TypeOf<TYPE>::type*>(base)[row + p.at(i)] = (typename TypeOf<TYPE>::type)v[i];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void put(void* base, int type, int64_t row, const Place<VEC>& p, const float (&v)[8]) {
+  if (!base) return;
+  if (type == SZO_F32) put_as<VEC, SZO_F32>(base, row, p, v);
+  else if (type == SZO_BF16) put_as<VEC, SZO_BF16>(base, row, p, v);
+  else put_as<VEC, SZO_F16>(base, row, p, v);
+}
+
+// A weight's or bias' features; `none` where there is none.
+template <bool VEC>
+__device__ __forceinline__ void factor(const float* base, int64_t row, const Place<VEC>& p, float none, float (&v)[8]) {
+  if (base) {
+    const Raw r = fetch<VEC>(base, SZO_F32, row, p);
+    widen<VEC>(r, SZO_F32, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = none;
+  }
+}
+
+// Where the waves of a row meet.  Every exchange of a pass over a row has a slot of its own, and a slot is written again one row later: at least one other
+// exchange, with its barrier, lies between (a kernel that makes a single exchange takes a single row).
+struct Meeting {
+  float (*slots)[kMostWaves][2];     // [exchange][wave]
+  int waves, wave, first;            // waves of a row, this one, first one of the row
+};
+
+// Sums of two values over a row.
+__device__ __forceinline__ void row_sums(const Meeting& m, int slot, float& a, float& b) {
+  a = lanes_sum<64>(a);
+  b = lanes_sum<64>(b);
+  if (m.waves == 1) return;
+  if (threadIdx.x % 64 == 0) { m.slots[slot][m.first + m.wave][0] = a; m.slots[slot][m.first + m.wave][1] = b; }
+  __syncthreads();
+  a = b = 0.f;
+  for (int w = 0; w < m.waves; ++w) { a += m.slots[slot][m.first + w][0]; b += m.slots[slot][m.first + w][1]; }
+}
+
+// Mean (0 for RMS norms) and 1 / sqrt(var + eps) of a row.  `count`: features of this wave.
+template <int CH, bool VEC>
+__device__ __forceinline__ void row_stats(const Meeting& m, int slot, const float (&v)[CH][8], const Place<VEC> (&at)[CH], bool layer, int width, float eps,
+                                          float& mean, float& r) {
+  float square = 0.f;
+  if (!layer) {
+    mean = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) square = fmaf(v[c][i], v[c][i], square);
+    float unused = 0.f;
+    row_sums(m, slot, square, unused);
+  } else {
+    float count = 0.f, sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { count += at[c].on(i) ? 1.f : 0.f; sum += v[c][i]; }
+    count = lanes_sum<64>(count);
+    mean = lanes_sum<64>(sum) / fmaxf(count, 1.f);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = at[c].on(i) ? v[c][i] - mean : 0.f;
+        square = fmaf(x, x, square);
+      }
+    square = lanes_sum<64>(square);
+    if (m.waves > 1) {
+      // a wave's count follows from the width: only the two others are exchanged, the counts are added up again from the places
+      if (threadIdx.x % 64 == 0) { m.slots[slot][m.first + m.wave][0] = mean; m.slots[slot][m.first + m.wave][1] = square; }
+      __syncthreads();
+      float all = 0.f;
+      for (int w = 0; w < m.waves; ++w) {
+        float n = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          // features of wave w in chunk c: neighbours with VEC, else eight runs of 64
+          if (VEC) n += (float)min(max(width - (c * m.waves + w) * 512, 0), 512);
+          else
+            for (int i = 0; i < 8; ++i) n += (float)min(max(width - ((c * 8 + i) * m.waves + w) * 64, 0), 64);
+        }
+        all = fmaf(n, m.slots[slot][m.first + w][0], all);
+      }
+      mean = all / (float)width;
+      square = 0.f;
+      for (int w = 0; w < m.waves; ++w) {
+        float n = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          if (VEC) n += (float)min(max(width - (c * m.waves + w) * 512, 0), 512);
+          else
+            for (int i = 0; i < 8; ++i) n += (float)min(max(width - ((c * 8 + i) * m.waves + w) * 64, 0), 64);
+        }
+        const float off = m.slots[slot][m.first + w][0] - mean;
+        square += fmaf(n * off, off, m.slots[slot][m.first + w][1]);
+      }
+    }
+  }
+  r = 1.f / sqrtf(square / (float)width + eps);
+}
+
+// unit = (v - mean) r, and 0 behind the row's end
+template <int CH, bool VEC>
+__device__ __forceinline__ void to_unit(float (&v)[CH][8], const Place<VEC> (&at)[CH], float mean, float r) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] = at[c].on(i) ? (v[c][i] - mean) * r : 0.f;
+}
+
+template <int CH, bool VEC>
+__device__ __forceinline__ void find_places(Place<VEC> (&p)[CH], int thread, int threads, int width) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c) p[c] = Place<VEC>(c, thread, threads, width);
+}
+
+template <int CH, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs args) {
+  __shared__ float slots[2][kMostWaves][2];
+  const szo_block_desc& d = args.d;
+  const int waves = args.waves, threads = waves * 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int row = wave / waves, thread = threadIdx.x - row * threads;
+  const Meeting m = {slots, waves, wave - row * waves, row * waves};
+  const int64_t token = (int64_t)blockIdx.x * (blockDim.x / threads) + row;
+  const bool there = token < d.tokens;                      // rows that are not still take part in the barriers
+  Place<VEC> p[CH];
+  find_places(p, thread, threads, there ? d.width : 0);
+  Raw y_raw[CH], h_raw[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    y_raw[c] = fetch<VEC>(d.y, d.y_type, token * d.y_stride, p[c]);
+    h_raw[c] = fetch<VEC>(d.h, d.h_type, token * d.h_stride, p[c]);
+  }
+  float y[CH][8], h[CH][8], w[8], b[8];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
+  if (d.y && d.post) {
+    float mean, r;
+    row_stats<CH, VEC>(m, 0, y, p, d.norm == SZO_NORM_LAYER, d.width, d.eps, mean, r);
+    to_unit<CH, VEC>(y, p, mean, r);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      factor<VEC>(d.post_weight, 0, p[c], 1.f, w);
+      factor<VEC>(d.post_bias, 0, p[c], 0.f, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[c][i] = fmaf(y[c][i], w[i], b[i]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    widen<VEC>(h_raw[c], d.h_type, h[c]);
+    factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[c][i] = d.y ? fmaf(d.y_scale * w[i], y[c][i], d.h_scale * h[c][i]) : d.h_scale * h[c][i];
+    put<VEC>(d.h_out, d.h_type, token * d.h_out_stride, p[c], h[c]);
+  }
+  if (!d.x_out) return;
+  float mean, r;
+  row_stats<CH, VEC>(m, 1, h, p, d.norm == SZO_NORM_LAYER, d.width, d.eps, mean, r);
+  to_unit<CH, VEC>(h, p, mean, r);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    factor<VEC>(d.pre_weight, 0, p[c], 1.f, w);
+    factor<VEC>(d.pre_bias, 0, p[c], 0.f, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[c][i] = fmaf(h[c][i], w[i], b[i]);
+    put<VEC>(d.x_out, d.x_type, token * d.x_out_stride, p[c], h[c]);
+  }
+}
+
+// A workgroup walks rows and keeps what it adds up over them in registers, eight features of up to five sums a thread; no atomics, so the order is fixed.
+template <int CH, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 : 1) block_norm_bwd_kernel(const BlockArgs args) {
+  __shared__ float slots[4][kMostWaves][2];
+  const szo_block_desc& d = args.d;
+  const szo_block_grads& g = args.g;
+  const int waves = args.waves, threads = waves * 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int rows = blockDim.x / threads, row = wave / waves, thread = threadIdx.x - row * threads;
+  const Meeting m = {slots, waves, wave - row * waves, row * waves};
+  const bool layer = d.norm == SZO_NORM_LAYER, post = d.y && d.post;
+  const float inverse = 1.f / (float)d.width;
+  float sums[kSets][CH][8];
+#pragma unroll
+  for (int s = 0; s < kSets; ++s)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sums[s][c][i] = 0.f;
+  for (int64_t first = (int64_t)blockIdx.x * rows; first < d.tokens; first += (int64_t)gridDim.x * rows) {
+    const int64_t token = first + row;
+    const bool there = token < d.tokens;
+    Place<VEC> p[CH];
+    find_places(p, thread, threads, there ? d.width : 0);
+    Raw y_raw[CH], h_raw[CH], gx_raw[CH], gh_raw[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      y_raw[c] = fetch<VEC>(d.y, d.y_type, token * d.y_stride, p[c]);
+      h_raw[c] = fetch<VEC>(g.x_out_grad ? d.h : nullptr, d.h_type, token * d.h_stride, p[c]);
+      gx_raw[c] = fetch<VEC>(g.x_out_grad, d.x_type, token * g.x_out_stride, p[c]);
+      gh_raw[c] = fetch<VEC>(g.h_out_grad, d.h_type, token * g.h_out_stride, p[c]);
+    }
+    float y[CH][8], gh[CH][8], w[8], b[8], y_r = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
+    if (post) {
+      float mean;
+      row_stats<CH, VEC>(m, 0, y, p, layer, d.width, d.eps, mean, y_r);
+      to_unit<CH, VEC>(y, p, mean, y_r);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) widen<VEC>(gh_raw[c], d.h_type, gh[c]);
+    if (g.x_out_grad) {
+      float h[CH][8], u[CH][8], mean, r, sum = 0.f, dot = 0.f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        widen<VEC>(h_raw[c], d.h_type, h[c]);
+        float a[8], gate[8];
+        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
+        factor<VEC>(post ? d.post_weight : nullptr, 0, p[c], 1.f, w);
+        factor<VEC>(post ? d.post_bias : nullptr, 0, p[c], 0.f, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          a[i] = fmaf(y[c][i], w[i], b[i]);
+          h[c][i] = d.y ? fmaf(d.y_scale * gate[i], a[i], d.h_scale * h[c][i]) : d.h_scale * h[c][i];
+        }
+      }
+      row_stats<CH, VEC>(m, 1, h, p, layer, d.width, d.eps, mean, r);
+      to_unit<CH, VEC>(h, p, mean, r);
+      if (!there) r = 0.f;                                  // with eps 0 it is infinite, and nothing times it would be NaN in the sums
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        widen<VEC>(gx_raw[c], d.x_type, u[c]);
+        factor<VEC>(d.pre_weight, 0, p[c], 1.f, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sums[kPreWeight][c][i] = fmaf(u[c][i], h[c][i], sums[kPreWeight][c][i]);
+          sums[kPreBias][c][i] += u[c][i];
+          u[c][i] *= w[i];
+          sum += u[c][i];
+          dot = fmaf(u[c][i], h[c][i], dot);
+        }
+      }
+      row_sums(m, 2, sum, dot);
+      sum = layer ? sum * inverse : 0.f;
+      dot *= inverse;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gh[c][i] = fmaf(r, u[c][i] - sum - h[c][i] * dot, gh[c][i]);
+    }
+    if (g.h_grad) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = d.h_scale * gh[c][i];
+        put<VEC>(g.h_grad, d.h_type, token * g.h_stride, p[c], w);
+      }
+    }
+    if (!d.y) continue;
+    // from here on gh is the gradient by what the residual stream was given, then by the norm's output, then by its input
+    float sum = 0.f, dot = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float gate[8], into[8];
+      factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
+      factor<VEC>(post ? d.post_weight : nullptr, 0, p[c], 1.f, w);
+      factor<VEC>(post ? d.post_bias : nullptr, 0, p[c], 0.f, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float t = d.y_scale * gh[c][i];
+        into[i] = t * fmaf(y[c][i], w[i], b[i]);
+        sums[kGate][c][i] += into[i];
+        gh[c][i] = t * gate[i];
+        sums[kPostWeight][c][i] = fmaf(gh[c][i], y[c][i], sums[kPostWeight][c][i]);
+        sums[kPostBias][c][i] += gh[c][i];
+        if (post) {
+          gh[c][i] *= w[i];
+          sum += gh[c][i];
+          dot = fmaf(gh[c][i], y[c][i], dot);
+        }
+      }
+      if (g.gate_grad && d.gate_stride) put<VEC>(g.gate_grad, SZO_F32, token * g.gate_stride, p[c], into);
+    }
+    if (post) {
+      row_sums(m, 3, sum, dot);
+      sum = layer ? sum * inverse : 0.f;
+      dot *= inverse;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gh[c][i] = y_r * (gh[c][i] - sum - y[c][i] * dot);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) put<VEC>(g.y_grad, d.y_type, token * g.y_stride, p[c], gh[c]);
+  }
+  if (!args.partials) return;
+  float* to = args.partials + ((int64_t)blockIdx.x * rows + row) * args.sets * d.width;
+  Place<VEC> whole[CH];
+  find_places(whole, thread, threads, d.width);
+#pragma unroll
+  for (int s = 0; s < kSets; ++s)
+    if (args.set_at[s] >= 0)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) put<VEC>(to, SZO_F32, (int64_t)args.set_at[s] * d.width, whole[c], sums[s][c]);
+}
+
+// 64 neighbouring sums per workgroup: 16 rows of threads walk the partials, then add each other up in order.
+__global__ void __launch_bounds__(1024) block_sums_kernel(const float* __restrict__ partials, int64_t width, int sets, int count, const BlockArgs args) {
+  __shared__ double rows[16][65];
+  const int column = threadIdx.x % 64, row = threadIdx.x / 64, set = blockIdx.y;
+  const int64_t i = (int64_t)blockIdx.x * 64 + column;
+  double s = 0.0;
+  if (i < width)
+#pragma unroll 4
+    for (int p = row; p < count; p += 16) s += (double)partials[((int64_t)p * sets + set) * width + i];
+  rows[row][column] = s;
+  __syncthreads();
+  for (int half = 8; half; half /= 2) {
+    if (row < half) rows[row][column] += rows[row + half][column];
+    __syncthreads();
+  }
+  if (row || i >= width) return;
+  float* const to[kSets] = {args.g.pre_weight_grad, args.g.pre_bias_grad, args.g.post_weight_grad, args.g.post_bias_grad, args.g.gate_grad};
+#pragma unroll
+  for (int k = 0; k < kSets; ++k)
+    if (args.set_at[k] == set) to[k][i] = (float)rows[0][column];
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostStride = (int64_t)1 << 40;
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / 1024;
+
+// Eight features a thread up to 512 threads, sixteen beyond: with 1024 threads a thread has 128 registers, and a backward's sums alone take 40 or 80.
+int chunks_of(int width) { return width <= 4096 ? 1 : 2; }
+int waves_of(int width) { return (width + 512 * chunks_of(width) - 1) / (512 * chunks_of(width)); }
+// Rows of a workgroup: it has 256 threads at least where rows have fewer.
+int rows_of(int waves) { return waves >= 4 ? 1 : 4 / waves; }
+
+// Workgroups of a backward: what the chip holds at a time.
+int64_t bwd_groups(const szo_block_desc* d) {
+  const int waves = waves_of(d->width), rows = rows_of(waves);
+  const int64_t most = 256 * std::max(1, (chunks_of(d->width) == 1 ? 16 : 8) / (waves * rows));
+  return std::max<int64_t>(1, std::min((d->tokens + rows - 1) / rows, most));
+}
+
+bool read_ok(const void* p, int64_t stride, int type) { return aligned_to(p, type_bytes(type)) && stride >= 0 && stride <= kMostStride; }
+// Rows that a call writes may not run into each other.
+bool written_ok(const void* p, int64_t stride, const szo_block_desc* d, int type) {
+  return !p || (read_ok(p, stride, type) && (d->tokens <= 1 || stride >= d->width));
+}
+bool vec_ok(const void* p, int64_t stride, int type) { return !p || (aligned_to(p, 16) && stride % (type == SZO_F32 ? 4 : 8) == 0); }
+
+int check(const szo_block_desc* d) {
+  if (!d || d->tokens < 0 || d->width <= 0 || !valid_type(d->y_type) || !valid_type(d->h_type) || !valid_type(d->x_type)) return SZO_EINVAL;
+  if ((d->norm != SZO_NORM_RMS && d->norm != SZO_NORM_LAYER) || (d->post & ~1) || d->reserved || !(d->eps >= 0.f)) return SZO_EINVAL;
+  if (d->width > kMostWidth) return SZO_EUNSUPPORTED;
+  if (d->tokens > 0 && !d->y && !d->h) return SZO_EINVAL;
+  if (!read_ok(d->y, d->y_stride, d->y_type) || !read_ok(d->h, d->h_stride, d->h_type) || !read_ok(d->gate, d->gate_stride, SZO_F32)) return SZO_EINVAL;
+  if (!aligned_to(d->post_weight, 4) || !aligned_to(d->post_bias, 4) || !aligned_to(d->pre_weight, 4) || !aligned_to(d->pre_bias, 4)) return SZO_EINVAL;
+  if (d->tokens > 0 && !d->y && d->gate) return SZO_EINVAL;              // an empty batch may have no addresses
+  return SZO_OK;
+}
+
+bool inputs_vec(const szo_block_desc* d) {
+  return d->width % 8 == 0 && vec_ok(d->y, d->y_stride, d->y_type) && vec_ok(d->h, d->h_stride, d->h_type) && vec_ok(d->gate, d->gate_stride, SZO_F32) &&
+         aligned_to(d->post_weight, 16) && aligned_to(d->post_bias, 16) && aligned_to(d->pre_weight, 16) && aligned_to(d->pre_bias, 16);
+}
+
+template <int CH, bool VEC, int THREADS>
+void launch(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+  const int threads = 64 * a.waves * rows_of(a.waves);
+  if (backward) block_norm_bwd_kernel<CH, VEC, THREADS><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+  else block_norm_kernel<CH, VEC, THREADS><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+}
+template <bool VEC>
+void launch_all(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+  if (a.d.width <= 4096) launch<1, VEC, 512>(a, groups, backward, s);
+  else if (a.d.width <= 8192) launch<2, VEC, 512>(a, groups, backward, s);
+  else launch<2, VEC, 1024>(a, groups, backward, s);
+}
+
+}  // namespace
+}  // namespace szo
+
+using namespace szo;
+
+extern "C" {
+
+int szo_block_norm(const szo_block_desc* d, void* stream) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!written_ok(d->h_out, d->h_out_stride, d, d->h_type) || !written_ok(d->x_out, d->x_out_stride, d, d->x_type)) return SZO_EINVAL;
+  if (d->tokens == 0 || (!d->h_out && !d->x_out)) return SZO_OK;
+  BlockArgs a = {};
+  a.d = *d;
+  a.waves = waves_of(d->width);
+  const int rows = rows_of(a.waves);
+  const int64_t groups = (d->tokens - 1) / rows + 1;
+  if (groups > kMostGroups) return SZO_EUNSUPPORTED;
+  const bool vec = inputs_vec(d) && vec_ok(d->h_out, d->h_out_stride, d->h_type) && vec_ok(d->x_out, d->x_out_stride, d->x_type);
+  vec ? launch_all<true>(a, groups, false, (hipStream_t)stream) : launch_all<false>(a, groups, false, (hipStream_t)stream);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
+size_t szo_block_workspace_bytes(const szo_block_desc* d) {
+  if (check(d) != SZO_OK || d->tokens == 0) return 16;
+  return sizeof(float) * kSets * (size_t)d->width * (size_t)(bwd_groups(d) * rows_of(waves_of(d->width)));
+}
+
+int szo_block_norm_bwd(const szo_block_desc* d, const szo_block_grads* g, void* workspace, void* stream) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!g || g->reserved) return SZO_EINVAL;
+  if (!read_ok(g->x_out_grad, g->x_out_stride, d->x_type) || !read_ok(g->h_out_grad, g->h_out_stride, d->h_type)) return SZO_EINVAL;
+  if (!written_ok(g->y_grad, g->y_stride, d, d->y_type) || !written_ok(g->h_grad, g->h_stride, d, d->h_type)) return SZO_EINVAL;
+  if (!aligned_to(g->gate_grad, 4) || (d->gate_stride && !written_ok(g->gate_grad, g->gate_stride, d, SZO_F32))) return SZO_EINVAL;
+  if (!aligned_to(g->pre_weight_grad, 4) || !aligned_to(g->pre_bias_grad, 4) || !aligned_to(g->post_weight_grad, 4) || !aligned_to(g->post_bias_grad, 4))
+    return SZO_EINVAL;
+  // a gradient of what has no part in the result is a mistake of the caller's, not zero
+  if (d->tokens > 0 && ((!d->y && g->y_grad) || (!d->h && g->h_grad) || (!d->gate && g->gate_grad) ||
+                        ((!d->y || !d->post) && (g->post_weight_grad || g->post_bias_grad)))) return SZO_EINVAL;
+  BlockArgs a = {};
+  a.d = *d;
+  a.g = *g;
+  a.waves = waves_of(d->width);
+  float* const wanted[kSets] = {g->pre_weight_grad, g->pre_bias_grad, g->post_weight_grad, g->post_bias_grad, d->gate_stride ? nullptr : g->gate_grad};
+  for (int k = 0; k < kSets; ++k) a.set_at[k] = wanted[k] ? a.sets++ : -1;
+  if (a.sets && (!workspace || !aligned_to(workspace, 16))) return SZO_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  if (d->tokens == 0) {
+    for (int k = 0; k < kSets; ++k)
+      if (wanted[k] && zero_words(wanted[k], d->width, s)) return SZO_ELAUNCH;
+    return SZO_OK;
+  }
+  a.partials = a.sets ? (float*)workspace : nullptr;
+  const bool vec = inputs_vec(d) && vec_ok(g->x_out_grad, g->x_out_stride, d->x_type) && vec_ok(g->h_out_grad, g->h_out_stride, d->h_type) &&
+                   vec_ok(g->y_grad, g->y_stride, d->y_type) && vec_ok(g->h_grad, g->h_stride, d->h_type) &&
+                   (!d->gate_stride || vec_ok(g->gate_grad, g->gate_stride, SZO_F32));
+  const int64_t groups = bwd_groups(d);
+  vec ? launch_all<true>(a, groups, true, s) : launch_all<false>(a, groups, true, s);
+  SZO_LAUNCH_CHECK();
+  if (a.sets) {
+    block_sums_kernel<<<dim3((unsigned)((d->width + 63) / 64), (unsigned)a.sets), 1024, 0, s>>>(a.partials, d->width, a.sets, (int)groups * rows_of(a.waves), a);
+    SZO_LAUNCH_CHECK();
+  }
+  return SZO_OK;
+}
+
+}  // extern "C"

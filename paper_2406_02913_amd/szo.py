@@ -24,6 +24,7 @@ FORMAT_UNIFORM, FORMAT_LUT = 0, 1
 F32, BF16, F16 = 0, 1, 2                  # element types of the calls between the linear layers
 KV_BLOCK = 32                             # tokens that share an exponent in the cache
 LOGPROBS_MAX_TOP = 32
+NORM_RMS, NORM_LAYER = 0, 1
 MOST_SCALE = 2.35e38                      # of logits and scores
 
 if not os.path.exists(LIB_PATH):
@@ -48,6 +49,17 @@ def _fields(kind, names):
 
 
 _I32, _I64, _PTR = C.c_int32, C.c_int64, C.c_void_p
+
+
+class BlockDesc(C.Structure):
+    _fields_ = (_fields(_I64, "tokens") + _fields(_I32, "width y_type h_type x_type norm post") + _fields(C.c_float, "eps y_scale h_scale") +
+                _fields(_I32, "reserved") + _fields(_PTR, "y h post_weight post_bias pre_weight pre_bias gate h_out x_out") +
+                _fields(_I64, "y_stride h_stride gate_stride h_out_stride x_out_stride"))
+
+
+class BlockGrads(C.Structure):
+    _fields_ = (_fields(_PTR, "x_out_grad h_out_grad y_grad h_grad gate_grad post_weight_grad post_bias_grad pre_weight_grad pre_bias_grad") +
+                _fields(_I64, "x_out_stride h_out_stride y_stride h_stride gate_stride reserved"))
 
 
 class QkDesc(C.Structure):
@@ -117,6 +129,9 @@ _SIGS = {
     "szo_kernel_timing": (C.c_int, [C.c_int]),
     "szo_kernel_timing_read": (C.c_int, [C.c_void_p, C.c_void_p]),
     "szo_kernel_timing_read2": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "szo_block_norm": (C.c_int, [_P(BlockDesc), C.c_void_p]),
+    "szo_block_norm_bwd": (C.c_int, [_P(BlockDesc), _P(BlockGrads), C.c_void_p, C.c_void_p]),
+    "szo_block_workspace_bytes": (C.c_size_t, [_P(BlockDesc)]),
     "szo_qk_norm_rope": (C.c_int, [_P(QkDesc), C.c_void_p]),
     "szo_qk_norm_rope_bwd": (C.c_int, [_P(QkDesc), _P(QkGrads), C.c_void_p, C.c_void_p]),
     "szo_qk_workspace_bytes": (C.c_size_t, [_P(QkDesc)]),
@@ -256,11 +271,15 @@ def new_workspace(device="cuda", nbytes=None):
 # ---- between the linear layers ------------------------------------------------------------------
 # A descriptor holds device pointers, so its tensors have to outlive it: it keeps them in `keep`.
 def _type(t):
+    return _type_of(t.dtype)
+
+
+def _type_of(dtype):
     import torch
     try:
-        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[t.dtype]
+        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[dtype]
     except KeyError:
-        raise ValueError(f"expected fp32, bf16 or fp16, got {t.dtype}") from None
+        raise ValueError(f"expected fp32, bf16 or fp16, got {dtype}") from None
 
 
 def _strided(t, shape):
@@ -284,6 +303,90 @@ def _room(workspace, need):
     if workspace is not None and workspace.nbytes < need:
         raise ValueError(f"a workspace of {workspace.nbytes} bytes, this call needs {need}")
     return _dev(workspace)
+
+
+def _rows(t, dtype, T, H):
+    """Pointer and stride of rows [T, H] of a type (None -> NULL); the last axis has to be contiguous."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (T, H) or (H > 1 and t.stride(1) != 1):
+        raise ValueError(f"expected a device tensor {dtype} {(T, H)} with contiguous rows, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr(), t.stride(0)
+
+
+def _gate(t, T, H):
+    """A gate [H] of all tokens (stride 0) or [T, H]."""
+    import torch
+    if t is not None and t.dim() == 1:
+        return _typed(t, torch.float32, (H,)), 0
+    return _rows(t, torch.float32, T, H)
+
+
+def make_block_desc(y, h, h_out=None, x_out=None, norm=NORM_RMS, post=None, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None,
+                    eps=1e-6, y_scale=1.0, h_scale=1.0, x_type=None):
+    """y, h [tokens, width] (one may be None), rows any distance apart; weights and biases fp32 [width]; gate fp32 [width] or [tokens, width].  `post` is on where a
+    weight or bias of it is given, unless said otherwise.  Without outputs: for the backward (x_type: torch type of the gradient by x_out, fp32, bf16 or fp16)."""
+    import torch
+    some = h if h is not None else y
+    if some is None:
+        raise ValueError("neither a block's output nor a residual stream")
+    T, H = some.shape
+    h_of = h.dtype if h is not None else h_out.dtype if h_out is not None else torch.float32
+    x_of = x_out.dtype if x_out is not None else x_type if x_type is not None else torch.bfloat16
+    y_of = y.dtype if y is not None else torch.float32
+    d = BlockDesc(T, H, *(_type_of(t) for t in (y_of, h_of, x_of)), norm, int((post_weight is not None or post_bias is not None) if post is None else post), eps, y_scale, h_scale, 0)
+    d.y, d.y_stride = _rows(y, y_of, T, H)
+    d.h, d.h_stride = _rows(h, h_of, T, H)
+    d.post_weight, d.post_bias, d.pre_weight, d.pre_bias = (_typed(t, torch.float32, (H,)) for t in (post_weight, post_bias, pre_weight, pre_bias))
+    d.gate, d.gate_stride = _gate(gate, T, H)
+    d.h_out, d.h_out_stride = _rows(h_out, h_of, T, H)
+    d.x_out, d.x_out_stride = _rows(x_out, x_of, T, H)
+    d.gated = None if gate is None else gate.dim()
+    d.x_given = x_out is not None or x_type is not None
+    d.types = y_of, h_of, x_of
+    d.keep = (y, h, h_out, x_out, post_weight, post_bias, gate, pre_weight, pre_bias)
+    return d
+
+
+def make_block_grads(desc, x_out_grad=None, h_out_grad=None, y_grad=None, h_grad=None, gate_grad=None, post_weight_grad=None, post_bias_grad=None,
+                     pre_weight_grad=None, pre_bias_grad=None):
+    """Gradients of what make_block_desc() was given, of the same shapes and types; None: 0 for those by the outputs, not wanted for the others.  A descriptor without
+    x_out and x_type takes the type of x_out_grad."""
+    import torch
+    T, H = desc.tokens, desc.width
+    y_of, h_of, x_of = desc.types
+    if x_out_grad is not None and not desc.x_given:
+        x_of = x_out_grad.dtype
+        desc.x_type, desc.types = _type(x_out_grad), (y_of, h_of, x_of)
+    if gate_grad is not None and gate_grad.dim() != desc.gated:
+        raise ValueError("a gradient of another shape than the gate")
+    g = BlockGrads()
+    g.x_out_grad, g.x_out_stride = _rows(x_out_grad, x_of, T, H)
+    g.h_out_grad, g.h_out_stride = _rows(h_out_grad, h_of, T, H)
+    g.y_grad, g.y_stride = _rows(y_grad, y_of, T, H)
+    g.h_grad, g.h_stride = _rows(h_grad, h_of, T, H)
+    g.gate_grad, g.gate_stride = _gate(gate_grad, T, H)
+    g.post_weight_grad, g.post_bias_grad, g.pre_weight_grad, g.pre_bias_grad = (
+        _typed(t, torch.float32, (H,)) for t in (post_weight_grad, post_bias_grad, pre_weight_grad, pre_bias_grad))
+    g.shape = T, H, tuple(desc.types), desc.gated
+    g.keep = (x_out_grad, h_out_grad, y_grad, h_grad, gate_grad, post_weight_grad, post_bias_grad, pre_weight_grad, pre_bias_grad)
+    return g
+
+
+def szo_block_norm(desc, stream=None):
+    _check("szo_block_norm", lib.szo_block_norm(C.byref(desc), _stream(stream)))
+
+
+def szo_block_norm_bwd(desc, grads, workspace=None, stream=None):
+    if grads.shape != (desc.tokens, desc.width, tuple(desc.types), desc.gated):
+        raise ValueError("gradients of other shapes or types than the descriptor's")
+    sums = (grads.pre_weight_grad, grads.pre_bias_grad, grads.post_weight_grad, grads.post_bias_grad, None if desc.gate_stride else grads.gate_grad)
+    need = lib.szo_block_workspace_bytes(C.byref(desc)) if any(sums) else 0
+    _check("szo_block_norm_bwd", lib.szo_block_norm_bwd(C.byref(desc), C.byref(grads), _room(workspace, need), _stream(stream)))
+
+
+def szo_block_workspace_bytes(desc):
+    return int(lib.szo_block_workspace_bytes(C.byref(desc)))
 
 
 def make_qk_desc(q, k, positions, cos_table, sin_table, q_out=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, norm=None):

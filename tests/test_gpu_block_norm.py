@@ -1,0 +1,248 @@
+"""Norms around a block with its gate and the residual stream, forward and backward, against the 64-bit definition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoder as od
+from paper_2406_02913_amd import szo
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": (2.0 ** -24, 0.0), "bf16": (2.0 ** -8, 0.0), "f16": (2.0 ** -11, 2.0 ** -25)}        # half a step; fp16 has a floor where it is subnormal
+U = 2.0 ** -24
+
+# tokens, width, layer norm, post, gate, types of y, h, x, layout
+CASES = [(1, 1, False, True, None, "f32", "f32", "f32", "plain"), (3, 5, True, True, "row", "f32", "f32", "f32", "plain"), (2, 8, True, False, "token", "bf16", "f32", "bf16", "plain"),
+         (9, 64, False, True, "row", "f32", "bf16", "bf16", "plain"), (17, 100, True, True, "token", "f16", "f16", "f32", "odd"), (5, 512, False, False, None, "f32", "f32", "bf16", "plain"),
+         (6, 520, True, True, "row", "bf16", "bf16", "bf16", "strided"), (7, 1000, False, True, "row", "f32", "f16", "f16", "plain"),
+         (3, 2056, True, True, "token", "f32", "f32", "f16", "strided"), (1500, 24, True, True, "row", "bf16", "f32", "f32", "plain"),
+         (4, 4096, False, True, "row", "f32", "f32", "bf16", "plain"), (3, 4104, True, True, "row", "f32", "bf16", "f32", "plain"),
+         (2, 5001, True, True, "token", "f32", "f32", "f32", "odd"), (700, 4096, True, True, "row", "bf16", "bf16", "bf16", "plain"),
+         (2, 8200, True, True, "row", "bf16", "f32", "f32", "plain"), (3, 16384, False, True, "token", "f32", "bf16", "bf16", "plain"),
+         (2, 12345, True, True, "row", "f16", "f32", "bf16", "plain")]
+
+
+def _np(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def _laid(x, layout):
+    """The same rows in one piece, at addresses that are no multiples of anything ("odd"), or apart ("strided", whole vectors)."""
+    if layout == "plain":
+        return x.contiguous()
+    T, H = x.shape
+    gap, off = (3, 1) if layout == "odd" else (8, 8)
+    room = torch.zeros(T * (H + gap) + off, dtype=x.dtype, device=x.device)
+    y = room[off:].view(T, H + gap)[:, :H]
+    y.copy_(x)
+    return y
+
+
+def _setup(case):
+    T, H, layer, post, gate, yt, ht, xt, layout = case
+    rng = np.random.default_rng(T * 31 + H)
+    dev = lambda a, t=torch.float32: torch.from_numpy(np.asarray(a)).to(t).to(DEV)         # noqa: E731
+    # rows of different strength, some with a mean far from 0
+    y = dev(rng.standard_normal((T, H)) * rng.uniform(0.1, 3, (T, 1)) + rng.integers(0, 2, (T, 1)) * 30, TYPES[yt])
+    h = dev(rng.standard_normal((T, H)) * 2 + rng.integers(0, 2, (T, 1)) * 10, TYPES[ht])
+    w = dict(pre_weight=dev(rng.uniform(0.5, 1.5, H)), pre_bias=dev(rng.standard_normal(H)) if layer else None)
+    if post:
+        w.update(post_weight=dev(rng.uniform(0.5, 1.5, H)), post_bias=dev(rng.standard_normal(H)) if layer else None)
+    if gate:
+        w["gate"] = dev(rng.standard_normal(H if gate == "row" else (T, H)))
+        if gate == "token":
+            w["gate"] = _laid(w["gate"], layout)
+    rest = dict(eps=1e-5, post=post, y_scale=0.7, h_scale=1.1)
+    return _laid(y, layout), _laid(h, layout), w, rest, rng, dev
+
+
+def _sizes(v, eps, layer):
+    """(r, unit, size that errors of unit are relative to): v minus a mean that was rounded, times r; 32 roundings at most on the way of any of them (8 products
+    after each other, six levels of lanes, sixteen waves, a quotient, a root)."""
+    unit, r = od._unit(v, eps, layer)
+    return r, unit, np.abs(unit) + (r * (np.abs(v) + np.abs(v).mean(-1, keepdims=True)) if layer else 0)
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_forward(case):
+    T, H, layer, post, gate, yt, ht, xt, layout = case
+    y, h, w, rest, _, _ = _setup(case)
+    h_out, x_out = _laid(torch.full((T, H), 7.0, dtype=TYPES[ht], device=DEV), layout), _laid(torch.full((T, H), 7.0, dtype=TYPES[xt], device=DEV), layout)
+    szo.szo_block_norm(szo.make_block_desc(y, h, h_out, x_out, norm=int(layer), **w, **rest))
+    wn = {n: _np(t) for n, t in w.items()}
+    want_h, want_x = od.block_norm(_np(y), _np(h), layer=layer, **wn, **rest)
+    one = lambda n, otherwise: otherwise if wn.get(n) is None else np.abs(wn[n])           # noqa: E731
+    a_size = np.abs(_np(y))
+    if post:
+        a_size = 32 * _sizes(_np(y), rest["eps"], layer)[2] * one("post_weight", 1.0) + 2 * one("post_bias", 0.0)
+    h_err = U * (abs(rest["y_scale"]) * one("gate", 1.0) * 4 * a_size + 4 * rest["h_scale"] * np.abs(_np(h)))
+    half, floor = HALF[ht]
+    assert np.all(np.abs(_np(h_out) - want_h) <= half * np.abs(want_h) + floor + h_err)
+    r, unit, size = _sizes(want_h, rest["eps"], layer)
+    # unit moves with the row: by its own error, the mean's and the size's
+    x_err = (r * (h_err + h_err.mean(-1, keepdims=True)) + np.abs(unit) * r * h_err.max(-1, keepdims=True) + 34 * U * size) * one("pre_weight", 1.0) + U * one("pre_bias", 0.0)
+    half, floor = HALF[xt]
+    assert np.all(np.abs(_np(x_out) - want_x) <= half * np.abs(want_x) + floor + x_err)
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_backward(case):
+    T, H, layer, post, gate, yt, ht, xt, layout = case
+    y, h, w, rest, rng, dev = _setup(case)
+    gx, gh = _laid(dev(rng.standard_normal((T, H)), TYPES[xt]), layout), _laid(dev(rng.standard_normal((T, H)), TYPES[ht]), layout)
+    d = szo.make_block_desc(y, h, norm=int(layer), x_type=TYPES[xt], **w, **rest)
+    out = {n + "_grad": None if t is None else _laid(torch.full_like(t, 7.0), layout) if n == "gate" and t.dim() == 2 else torch.full_like(t, 7.0) for n, t in w.items()}
+    out["y_grad"], out["h_grad"] = _laid(torch.full_like(y, 7.0), layout), _laid(torch.full_like(h, 7.0), layout)
+    g = szo.make_block_grads(d, x_out_grad=gx, h_out_grad=gh, **out)
+    room = torch.full((szo.szo_block_workspace_bytes(d),), 0xFF, dtype=torch.uint8, device=DEV)
+    szo.szo_block_norm_bwd(d, g, room)
+    wn = {n: _np(t) for n, t in w.items()}
+    want = od.block_norm_bwd(_np(y), _np(h), gx=_np(gx), gh=_np(gh), layer=layer, **wn, **rest)
+    # The same expressions of absolute values say what errors are relative to; 160 roundings on the longest way: two norms' statistics of up to 32, each
+    # in two places (units and their means), and some ten products and sums
+    one = lambda n: 1.0 if wn.get(n) is None else np.abs(wn[n])                            # noqa: E731
+    mean = lambda v: v.mean(-1, keepdims=True)                                             # noqa: E731
+    stream = od.block_norm(_np(y), _np(h), layer=layer, **wn, **rest)[0]
+    r, _, unit = _sizes(stream, rest["eps"], layer)
+    ys, hs = rest["y_scale"], rest["h_scale"]
+    a, yr = np.abs(_np(y)), None
+    if post:
+        yr, _, yunit = _sizes(a if not layer else _np(y), rest["eps"], layer)
+        a = yunit * one("post_weight") + (0 if wn["post_bias"] is None else np.abs(wn["post_bias"]))
+    # what the forward's own rounding of the stream does to the units: it is relative to the sizes of what was added
+    unit = unit + r * (ys * one("gate") * a + hs * np.abs(_np(h))) + np.abs(unit) * r * np.max(ys * one("gate") * a + hs * np.abs(_np(h)), -1, keepdims=True)
+    u = np.abs(_np(gx)) * one("pre_weight")
+    size = {"pre_weight": (np.abs(_np(gx)) * unit).sum(0), "pre_bias": np.abs(_np(gx)).sum(0)}
+    s = np.abs(_np(gh)) + r * (u + mean(u) + unit * mean(u * unit)) * (1 + r * np.max(ys * one("gate") * a + hs * np.abs(_np(h)), -1, keepdims=True))
+    size["h"] = hs * s
+    into = ys * s * a
+    size["gate"] = into.sum(0) if gate == "row" else into
+    s = ys * s * one("gate")
+    if post:
+        size["post_weight"], size["post_bias"] = (s * yunit).sum(0), s.sum(0)
+        s = s * one("post_weight")
+        s = yr * (s + mean(s) + yunit * mean(s * yunit)) * (1 + (np.abs(_np(y)).max(-1, keepdims=True) * yr if layer else 0))
+    size["y"] = s
+    for name, t in out.items():
+        if t is None:
+            continue
+        n = name[:-5]
+        half, floor = HALF[{torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}[t.dtype]]
+        off = np.abs(_np(t) - want[n])
+        assert np.all(off <= half * np.abs(want[n]) + floor + 160 * U * size[n]), (n, (off / (half * np.abs(want[n]) + floor + 160 * U * size[n])).max())
+
+
+def test_pieces_by_themselves():
+    rng = np.random.default_rng(5)
+    y, h = (torch.from_numpy(rng.standard_normal((4, 96))).float().to(DEV) for _ in range(2))
+    x = torch.empty_like(h)
+    szo.szo_block_norm(szo.make_block_desc(None, h, x_out=x))                         # the first norm of a model
+    np.testing.assert_allclose(_np(x), od.block_norm(None, _np(h), 1e-6)[1], rtol=40 * U, atol=40 * U)
+    out = torch.empty_like(h)
+    szo.szo_block_norm(szo.make_block_desc(y, None, h_out=out, y_scale=2.0))            # no stream yet
+    assert torch.equal(out, 2 * y)
+    szo.szo_block_norm(szo.make_block_desc(y, h, h_out=out))
+    assert torch.equal(out, y + h)
+    gx = torch.from_numpy(rng.standard_normal((4, 96))).float().to(DEV)
+    dh = torch.empty_like(h)
+    d = szo.make_block_desc(None, h)
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, x_out_grad=gx, h_grad=dh))
+    np.testing.assert_allclose(_np(dh), od.block_norm_bwd(None, _np(h), 1e-6, _np(gx), None)["h"], rtol=100 * U, atol=100 * U)
+    dy, gate = torch.empty_like(y), torch.full((96,), 0.5, device=DEV)
+    gate_grad = torch.empty_like(gate)
+    d = szo.make_block_desc(y, h, gate=gate)                                           # the sum alone
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, h_out_grad=gx, y_grad=dy, gate_grad=gate_grad), torch.empty(szo.szo_block_workspace_bytes(d), dtype=torch.uint8, device=DEV))
+    assert torch.equal(dy, 0.5 * gx)
+    np.testing.assert_allclose(_np(gate_grad), (_np(gx) * _np(y)).sum(0), rtol=8 * U, atol=32 * U)
+
+
+@pytest.mark.parametrize("norm", [szo.NORM_RMS, szo.NORM_LAYER])
+def test_in_place(norm):
+    rng = np.random.default_rng(6)
+    y, h = (torch.from_numpy(rng.standard_normal((33, 200))).float().to(DEV) for _ in range(2))
+    w = torch.from_numpy(rng.uniform(0.5, 1.5, 200)).float().to(DEV)
+    apart = torch.empty_like(h), torch.empty_like(h)
+    szo.szo_block_norm(szo.make_block_desc(y, h, *apart, norm=norm, post_weight=w, pre_weight=w))
+    y2, h2 = y.clone(), h.clone()
+    szo.szo_block_norm(szo.make_block_desc(y2, h2, h2, y2, norm=norm, post_weight=w, pre_weight=w))
+    assert torch.equal(h2, apart[0]) and torch.equal(y2, apart[1])
+    gx, gh = torch.randn_like(h), torch.randn_like(h)
+    d = szo.make_block_desc(y, h, norm=norm, post_weight=w, pre_weight=w)
+    dy, dh = torch.empty_like(y), torch.empty_like(h)
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, gx, gh, dy, dh))
+    gx2, gh2 = gx.clone(), gh.clone()
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, gx2, gh2, gx2, gh2))
+    assert torch.equal(gx2, dy) and torch.equal(gh2, dh)
+
+
+@pytest.mark.parametrize("width", [40, 3000])
+def test_zero_rows_and_nan_stay_in_their_rows(width):
+    h = torch.randn(6, width, device=DEV)
+    h[1], h[3, 7], h[4, 2] = 0, float("nan"), float("inf")
+    y, gx = torch.randn_like(h), torch.randn_like(h)
+    x, dh = torch.empty_like(h), torch.empty_like(h)
+    for eps in (1e-6, 0.0):
+        szo.szo_block_norm(szo.make_block_desc(None, h, x_out=x, eps=eps))
+        assert torch.isfinite(x[[0, 2, 5]]).all() and torch.isnan(x[3]).all() and torch.isnan(x[4, 2])
+        assert (x[1] == 0).all() if eps else torch.isnan(x[1]).all()
+        d = szo.make_block_desc(y, h, eps=eps)
+        szo.szo_block_norm_bwd(d, szo.make_block_grads(d, x_out_grad=gx, h_grad=dh))
+        assert torch.isfinite(dh[[0, 1, 2, 5]]).all() and torch.isnan(dh[3]).all()
+
+
+def test_rows_that_are_not_there_stay_out_of_sums_with_eps_0():
+    # 5 rows of one wave in workgroups of four
+    h, gx = torch.randn(5, 40, device=DEV), torch.randn(5, 40, device=DEV)
+    w, dw = torch.ones(40, device=DEV), torch.empty(40, device=DEV)
+    d = szo.make_block_desc(None, h, pre_weight=w, eps=0.0)
+    room = torch.empty(szo.szo_block_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, x_out_grad=gx, pre_weight_grad=dw), room)
+    want = od.block_norm_bwd(None, _np(h), 0.0, _np(gx), None)["pre_weight"]
+    np.testing.assert_allclose(_np(dw), want, rtol=0, atol=64 * U * 5 * 16)
+
+
+def test_no_tokens_give_no_sums():
+    h, dw = torch.empty(0, 16, device=DEV), torch.full((16,), 3.0, device=DEV)
+    d = szo.make_block_desc(None, h, pre_weight=torch.ones(16, device=DEV))
+    szo.szo_block_norm(d)
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, x_out_grad=h, pre_weight_grad=dw), torch.empty(16, dtype=torch.uint8, device=DEV))
+    assert (dw == 0).all()
+    gate, dgate, w = torch.ones(16, device=DEV), torch.full((16,), 3.0, device=DEV), torch.ones(16, device=DEV)
+    d = szo.make_block_desc(h, h, post_weight=w, gate=gate)
+    szo.szo_block_norm(d)
+    szo.szo_block_norm_bwd(d, szo.make_block_grads(d, h, h, h, h, gate_grad=dgate, post_weight_grad=dw.fill_(3.0)), torch.empty(16, dtype=torch.uint8, device=DEV))
+    assert (dw == 0).all() and (dgate == 0).all()
+
+
+def test_captured_and_replayed_beside_an_eager_run_on_another_stream():
+    torch.manual_seed(1)
+    y, h, gx, gh = (torch.randn(700, 512, device=DEV) for _ in range(4))
+    w, gate = torch.rand(512, device=DEV) + 0.5, torch.randn(512, device=DEV)
+
+    def call(stream=None):
+        out = [torch.empty_like(h) for _ in range(4)] + [torch.empty_like(w) for _ in range(3)]
+        d = szo.make_block_desc(y, h, out[0], out[1], post_weight=w, gate=gate, pre_weight=w)
+        g = szo.make_block_grads(d, gx, gh, out[2], out[3], out[4], post_weight_grad=out[5], pre_weight_grad=out[6])
+        room = torch.empty(szo.szo_block_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+        return out, lambda: (szo.szo_block_norm(d), szo.szo_block_norm_bwd(d, g, room))
+
+    want, run = call()
+    run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got, again = call()
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        again()
+    graph, (held, captured) = torch.cuda.CUDAGraph(), call()
+    with torch.cuda.graph(graph):
+        captured()
+    for _ in range(4):
+        for t in held:
+            t.fill_(9.0)
+        graph.replay()
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
