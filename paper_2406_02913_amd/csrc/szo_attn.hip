@@ -23,6 +23,7 @@ namespace szo {
 namespace {
 
 constexpr int kThreads = 256;              // of the joining kernel
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / 512;      // a launch counts its threads in 32 bits
 constexpr float kNone = -3.402823466e38f;  // running maximum of a row that has seen nothing: the lowest finite value, so that differences stay defined
 constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
 constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
@@ -40,6 +41,17 @@ struct AttnArgs {
   bool negate;                             // scale < 0: queries change sign
   float* partial;                          // [sequence][key head][wave tile][split] of part_floats()
   bool vec_q, vec_out;
+};
+
+// Sequences that share a prefix (szo_attn_shared).  Two kinds of units of work: tiles of rows of all of a group's sequences over parts of the shared blocks, and
+// tiles of a sequence's rows over parts of its own.  Both leave partial sums.
+struct SharedArgs {
+  const int32_t *group_start, *shared;
+  int groups, most_blocks;                 // most shared blocks
+  int tiles, wave_tiles, splits, rows_cap; // of the shared blocks: workgroups side by side over a group's rows, their waves, parts, rows kept per wave tile
+  int rows;                                // of a group that there are places for
+  int units, first_unit;                   // units of the shared blocks: tiles of all groups times parts; unit of the launch's first workgroups
+  int64_t own_at;                          // floats before the partial sums of sequences' own blocks
 };
 
 // A part's sums: rows_cap rows of head_dim numerators, then maximum (two floats) and denominator of each.  A multiple of 16 bytes, which rows are stored
@@ -172,26 +184,32 @@ struct Walk {
   }
 };
 
-// A lane's half of a row: finished, or as this split's partial sum.  Of WK waves each has the features 32 e .. + 31 with e = walker modulo WK.
+// A lane's half of a row as a partial sum: row `column` of rows_cap.  Of WK waves each has the features 32 e .. + 31 with e = walker modulo WK.
+template <int D, int WK>
+__device__ __forceinline__ void put_part(float* to, int rows_cap, const f32x16 (&o)[D / 32], float m, float m_exp, float l, int walker, int column, int half) {
+  float* mine = to + (int64_t)column * D;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) {
+    if (e % WK != walker) continue;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
+  }
+  if (half == 0 && walker == 0) {
+    to[(int64_t)rows_cap * D + 3 * column] = m;
+    to[(int64_t)rows_cap * D + 3 * column + 1] = m_exp;
+    to[(int64_t)rows_cap * D + 3 * column + 2] = l;
+  }
+}
+
+// Finished, or as this split's partial sum.
 template <int TYPE, int D, int WK>
 __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float m_exp, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
                                         int walker, int token, int q_head, int column, int half) {
   const szo_attn_desc& d = a.d;
   if (a.splits > 1) {
-    float* to = a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * part_floats(a.rows_cap, D);
-    float* mine = to + (int64_t)column * D;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-      if (e % WK != walker) continue;
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(mine + 32 * e + 2 * i + 4 * half) = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
-    }
-    if (half == 0 && walker == 0) {
-      to[(int64_t)a.rows_cap * D + 3 * column] = m;
-      to[(int64_t)a.rows_cap * D + 3 * column + 1] = m_exp;
-      to[(int64_t)a.rows_cap * D + 3 * column + 2] = l;
-    }
+    put_part<D, WK>(a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * part_floats(a.rows_cap, D), a.rows_cap, o, m, m_exp, l,
+                    walker, column, half);
     return;
   }
   const float by = inverse_sum(l);
@@ -209,6 +227,40 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
   if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, m_exp, l);
 }
 
+// The group that a sequence is of, and what it shares.  Every lane of the wave asks for one and the same sequence.
+struct GroupOf {
+  int index, first, blocks;                // its number, its first sequence; blocks of 32 tokens that are shared, 0: none
+  int start;                               // first token of its first sequence
+  __device__ __forceinline__ GroupOf(const SharedArgs& sh, const AttnArgs& a, const int32_t* q_start, int sequence, int lane) : index(0), first(0), blocks(0), start(0) {
+    for (int k = 0; k < sh.groups; k += 64) {
+      const bool in = k + lane < sh.groups;
+      const int from = in ? sh.group_start[k + lane] : 0, to = in ? sh.group_start[k + lane + 1] : 0x7FFFFFFF, tokens = in ? sh.shared[k + lane] : 0;
+      const uint64_t before = __ballot(to <= sequence);
+      if (before == ~0ull) continue;
+      const int c = __popcll(before);      // ends ascend, so these are the first ones
+      index = k + c;
+      first = __builtin_amdgcn_readlane(from, c);
+      blocks = shared_blocks(sh, a, __builtin_amdgcn_readlane(tokens, c));
+      if (k + c >= sh.groups || first < 0 || first > sequence) blocks = 0;
+      break;
+    }
+    if (blocks) start = max(q_start[first], 0);
+  }
+  // Whole blocks among the first `tokens` that the page table has room for.
+  static __device__ __forceinline__ int shared_blocks(const SharedArgs& sh, const AttnArgs& a, int tokens) {
+    return a.d.cache.pages == 0 ? 0 : (int)min((int64_t)min(max(tokens, 0) / kKvBlock, sh.most_blocks), (int64_t)a.d.cache.max_pages * a.blocks_per_page);
+  }
+};
+// Whether the rows of a sequence that ends before token `stop` have places in the tiles of its group's shared blocks; else it goes over all of its blocks itself.
+__device__ __forceinline__ bool covered(const SharedArgs& sh, const AttnArgs& a, const GroupOf& g, int stop) {
+  return g.blocks > 0 && (int64_t)(stop - g.start) * a.group <= sh.rows;
+}
+
+__device__ __forceinline__ int wave_min(int v) {
+  for (int by = 32; by; by /= 2) v = min(v, __shfl_xor(v, by));
+  return v;
+}
+
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
 //   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
 // one step do not depend on each other.  The arguments that the first loads need come first, where they are in registers when a wave starts; the page of the
@@ -217,45 +269,119 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
 //   A prompt of 8192 tokens with 32 query and 8 key heads of 128, causal: 577 us, 953 TFLOP/s, bound by the issue of instructions: matrix products take 44 % of
 // the cycles, and a step has 186 vector instructions beside 16 products.  One token of each of 64 sequences of up to 8192: 108 us, 5.73 TB/s of the cache.
 // 4096 tokens in bf16 with head dimensions of 64, 96, 128, 256: 124, 138, 168, 393 us (556, 748, 820, 699 TFLOP/s), in fp16 110, 140, 166, 383.
-template <int TYPE, int D, int WR, int WK, bool ONCE>
-__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
-                                                                                   int max_pages, int bpp, int splits, int tiles, const AttnArgs a) {
+//   SHARED: units of work of sequences that share prefixes, one after the other with the key heads side by side; what a unit's rows are and which blocks they go over
+// is all that differs.
+template <int TYPE, int D, int WR, int WK, bool ONCE, bool SHARED>
+__device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table, int max_pages, int bpp, int splits, int tiles,
+                                          const AttnArgs& a, const SharedArgs& sh) {
   constexpr int E = D / 32;
   const szo_attn_desc& d = a.d;
   const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), column = lane % 32, half = lane / 32;
   // key heads vary fastest: workgroups are dealt out to the 8 XCDs in turn, so the row tiles of one key head share an L2
-  const int head = blockIdx.x, sequence = blockIdx.z;
-  const int split = splits == 1 ? 0 : blockIdx.y % splits;
-  const int tile = tiles - 1 - (splits == 1 ? blockIdx.y : blockIdx.y / splits);          // later rows see more: they start first
-  const int wave_tile = tile * WR + wave % WR, walker = WK == 1 ? 0 : wave / WR;
-  const int32_t* table = page_table + (int64_t)sequence * max_pages;
-  const int whole = lengths[sequence], guess = max_pages > walker / bpp ? table[walker / bpp] : -1;
-  const int start = max(q_start[sequence], 0), stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);      // differences of both fit
-  const int n = max(0, min(stop - start, d.max_q));
-  const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
-  const int rows = n * a.group, first_row = wave_tile * 32;
-  if (tile * WR * 32 >= rows) return;                    // the workgroup as a whole
-  const int behind = max(whole, 0) - (stop - start);     // position of the sequence's first query
+  int head = blockIdx.x, sequence = blockIdx.z, split, tile;
+  int unit = 0;
+  bool together = false;                   // SHARED: rows of a whole group over its shared blocks
+  if constexpr (SHARED) {
+    const int at = blockIdx.x / d.cache.kv_heads;
+    head = blockIdx.x - at * d.cache.kv_heads;
+    unit = sh.first_unit + at;
+    together = unit < sh.units;
+    const int parts = together ? sh.splits : splits, per = (together ? sh.tiles : tiles) * parts, within = together ? unit : unit - sh.units;
+    sequence = within / per;               // the group, for now, if together
+    tile = (within - sequence * per) / parts;
+    split = within - sequence * per - tile * parts;
+    splits = parts;
+  } else {
+    split = splits == 1 ? 0 : blockIdx.y % splits;
+    tile = tiles - 1 - (splits == 1 ? blockIdx.y : blockIdx.y / splits);          // later rows see more: they start first
+  }
+  const int wave_tile = tile * WR + wave % WR, walker = WK == 1 ? 0 : wave / WR, first_row = wave_tile * 32, row = first_row + column;
   // First position of the window of a query at `position`: 0 where the window is wider; no difference leaves 32 bits.  What a wave has in common is kept in scalar
   // registers (a prompt of 8192 636 us otherwise, 577 so).
   auto window_from = [&](int position) { return d.window > 0 ? max(position + 1, d.window) - d.window : 0; };
-
-  // this lane's row
-  const int row = first_row + column, query = row / a.group, q_head = head * a.group + row % a.group;
-  const bool valid = row < rows;
-  const int see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
-  const int see_from = window_from(behind + query);
+  const int32_t* table;
+  float* part = nullptr;
+  int guess = -1, start, query, q_head, see_to, see_from, see_all, see_all_from, lo, hi;
+  bool valid;
   Query<TYPE, D> q;
-  q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
+  if (SHARED && together) {
+    const int group = sequence, first = max(sh.group_start[group], 0), last = min(sh.group_start[group + 1], d.cache.sequences);
+    const int blocks = GroupOf::shared_blocks(sh, a, sh.shared[group]);
+    if (first >= last || blocks == 0) return;
+    table = page_table + (int64_t)first * max_pages;
+    start = max(q_start[first], 0);
+    const int stop = max((int)min((int64_t)q_start[last], d.tokens), 0);
+    const int rows = (int)min((int64_t)max(stop - start, 0) * a.group, (int64_t)sh.rows);
+    if (tile * WR * 32 >= rows) return;                  // the workgroup as a whole
+    // the sequence of this lane's row: those of the tile's tokens are gone through one by one
+    const int token = start + row / a.group, token_first = start + first_row / a.group, token_last = start + (min(first_row + 32, rows) - 1) / a.group;
+    int own_start = 0, own_stop = 0, whole = 0;
+    bool found = false, done = false;
+    for (int k = first; k < last && !done; k += 64) {
+      const int i = k + lane;
+      const int from = i < last ? q_start[i] : 0x7FFFFFFF, to = i < last ? max((int)min((int64_t)q_start[i + 1], d.tokens), 0) : 0x7FFFFFFF;
+      const int tokens = i < last ? lengths[i] : 0;
+      const uint64_t before = __ballot(to <= token_first);
+      if (before == ~0ull) continue;
+      for (int c = __popcll(before); c < 64 && !done; ++c) {
+        const int from_c = max(__builtin_amdgcn_readlane(from, c), 0), to_c = __builtin_amdgcn_readlane(to, c);
+        done = from_c > token_last;
+        const bool mine = !done && token >= from_c && token < to_c;
+        own_start = mine ? from_c : own_start;
+        own_stop = mine ? to_c : own_stop;
+        whole = mine ? __builtin_amdgcn_readlane(tokens, c) : whole;
+        found |= mine;
+      }
+    }
+    query = token - own_start;
+    q_head = head * a.group + row % a.group;
+    valid = row < rows && found && query < d.max_q;
+    const int behind = max(whole, 0) - (own_stop - own_start);
+    const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
+    see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
+    see_from = window_from(behind + query);
+    start = own_start;
+    const int reach = -wave_min(valid ? -see_to : 0);
+    lo = uniform(wave_min(valid ? see_from : 0x7FFFFFFF)) / kKvBlock;
+    hi = uniform(min(blocks, reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0));
+    see_all = uniform(wave_min(valid ? see_to : 0x7FFFFFFF));
+    see_all_from = uniform(-wave_min(valid ? -see_from : 0));
+    part = a.partial + ((((int64_t)group * d.cache.kv_heads + head) * sh.wave_tiles + wave_tile) * splits + split) * part_floats(sh.rows_cap, D);
+    q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
+  } else {
+    table = page_table + (int64_t)sequence * max_pages;
+    const int whole = lengths[sequence];
+    if constexpr (!SHARED) guess = max_pages > walker / bpp ? table[walker / bpp] : -1;
+    start = max(q_start[sequence], 0);
+    const int stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);      // differences of both fit
+    const int n = max(0, min(stop - start, d.max_q));
+    const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
+    const int rows = n * a.group;
+    if (tile * WR * 32 >= rows) return;                    // the workgroup as a whole
+    const int behind = max(whole, 0) - (stop - start);     // position of the sequence's first query
 
-  // blocks that some row of the wave sees, the part of them that is this split's, and this wave's share of that
-  const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
-  const int reach = first_row >= rows || d.cache.pages == 0 ? 0 : d.causal ? min(length, pos_last + 1) : length;
-  const int lo = uniform(window_from(pos_first)) / kKvBlock, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
+    // this lane's row
+    query = row / a.group, q_head = head * a.group + row % a.group;
+    valid = row < rows;
+    see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
+    see_from = window_from(behind + query);
+    q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
+
+    // blocks that some row of the wave sees
+    const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
+    const int reach = first_row >= rows || d.cache.pages == 0 ? 0 : d.causal ? min(length, pos_last + 1) : length;
+    lo = uniform(window_from(pos_first)) / kKvBlock, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
+    see_all = d.causal ? min(length, pos_first + 1) : length;     // tokens before this one are seen by every row, but for the window
+    see_all_from = uniform(window_from(pos_last));
+    if constexpr (SHARED) {
+      const GroupOf g(sh, a, q_start, sequence, lane);
+      if (covered(sh, a, g, stop)) lo = max(lo, uniform(g.blocks));
+      part = a.partial + sh.own_at + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles * WR + wave_tile) * splits + split) * part_floats(a.rows_cap, D);
+    }
+  }
+  // the part of the blocks that is this split's, and this wave's share of that
   const int share = splits == 1 ? max(hi - lo, 0) : (max(hi - lo, 0) + splits - 1) / splits;
   const int j0 = lo + split * share + walker, j1 = min(hi, lo + (split + 1) * share);
-  const int see_all = d.causal ? min(length, pos_first + 1) : length;     // tokens before this one are seen by every row, but for the window
-  const int see_all_from = uniform(window_from(pos_last));
 
   f32x16 o[E], s = {};
   float m = kNone, m_exp = 0.f, l = 0.f;
@@ -267,7 +393,7 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
   if (j0 < j1) {
     // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
     Walk walk(j0, bpp);
-    int now = j0 == walker ? walk.on(d.cache, guess, head, bpp) : walk.at(d.cache, table, head, bpp), next = now;
+    int now = !SHARED && j0 == walker ? walk.on(d.cache, guess, head, bpp) : walk.at(d.cache, table, head, bpp), next = now;
     if (j0 + WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
     auto known = [](int b) { return max(b, 0); };
     auto scores = [&](const Raw<D>& k) {
@@ -457,30 +583,59 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kern
       }
     }
   }
-  if (valid) put_row<TYPE, D, WK>(a, o, m, m_exp, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
+  if constexpr (SHARED) {
+    if (valid) put_part<D, WK>(part, together ? sh.rows_cap : a.rows_cap, o, m, m_exp, l, walker, column, half);
+  } else {
+    if (valid) put_row<TYPE, D, WK>(a, o, m, m_exp, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
+  }
+}
+
+template <int TYPE, int D, int WR, int WK, bool ONCE>
+__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_walk_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
+                                                                                   int max_pages, int bpp, int splits, int tiles, const AttnArgs a) {
+  attn_walk<TYPE, D, WR, WK, ONCE, false>(q_start, lengths, page_table, max_pages, bpp, splits, tiles, a, SharedArgs{});
+}
+template <int TYPE, int D, int WR, int WK>
+__global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_shared_kernel(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table,
+                                                                                     int max_pages, int bpp, int splits, int tiles, const AttnArgs a, const SharedArgs sh) {
+  attn_walk<TYPE, D, WR, WK, false, true>(q_start, lengths, page_table, max_pages, bpp, splits, tiles, a, sh);
 }
 
 // Joins the parts of a row, four features of it at a time, by G neighbouring lanes: each takes every G-th part and they add each other up by row
 // permutations.  One lane, up to four parts on the way, for up to five parts and for full tiles, 16 lanes otherwise (1 sequence of 8000 in 32 parts 12.4 -> 10.5 us,
 // 32 rows of it in 8 parts 18.7 -> 19.2).  Workgroups go over sequences, key heads, wave tiles and a tile's pieces.
-template <int TYPE, int D, int G>
-__global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
+//   SHARED: the parts of its group's shared blocks come before those of its own.
+template <int TYPE, int D, int G, bool SHARED>
+__device__ __forceinline__ void attn_join(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs& a, const SharedArgs& sh) {
   const szo_attn_desc& d = a.d;
   const int wave_tile = blockIdx.x % wave_tiles, head = blockIdx.y, sequence = blockIdx.z;
-  const float* from = partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
+  const float* from = partial + (SHARED ? sh.own_at : 0) + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
   const int start = max(q_start[sequence], 0), stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
   const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
   const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
   const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
+  const float* shared_from = nullptr;
+  int shared_parts = 0, shared_column = 0;
+  if constexpr (SHARED) {
+    const GroupOf g(sh, a, q_start, sequence, threadIdx.x % 64);
+    if (covered(sh, a, g, stop)) {
+      const int place = (start - g.start + query) * a.group + row % a.group;
+      shared_parts = sh.splits;
+      shared_column = place % 32;
+      shared_from = a.partial + (((int64_t)g.index * gridDim.y + head) * sh.wave_tiles + place / 32) * sh.splits * part_floats(sh.rows_cap, D);
+    }
+  }
   if (column >= rows) return;                  // G lanes at once
   float m = kNone, m_exp = 0.f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int kAhead = G == 1 ? 4 : 2;
 #pragma unroll kAhead
-  for (int s = g; s < splits; s += G) {
-    const float* part = from + (int64_t)s * part_floats(rows_cap, D);
-    const float* stats = part + (int64_t)rows_cap * D + 3 * column;
+  for (int s = g; s < splits + shared_parts; s += G) {
+    const bool of_group = SHARED && s < shared_parts;
+    const int cap = of_group ? sh.rows_cap : rows_cap, at = of_group ? shared_column : column;
+    const float* part = of_group ? shared_from + (int64_t)s * part_floats(cap, D) : from + (int64_t)(s - shared_parts) * part_floats(cap, D);
+    const float* stats = part + (int64_t)cap * D + 3 * at;
     const float ms = stats[0], es = stats[1], ls = stats[2];
-    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)at * D + f);
     const float over = (ms - m) + (es - m_exp), keep_half = half_of(fminf(-over, 0.f)), add_half = half_of(fminf(over, 0.f));
     const float keep = keep_half * keep_half, add = add_half * add_half;
     l = fmaf(l * keep_half, keep_half, ls * add_half * add_half);
@@ -507,6 +662,16 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_st
   else store_f32<TYPE, 4, false>(d.out, at, y);
   if (d.lse && f == 0)
     d.lse[(int64_t)(start + query) * d.q_heads + q_head] = log_sum(m, m_exp, l);
+}
+
+template <int TYPE, int D, int G>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
+  attn_join<TYPE, D, G, false>(q_start, partial, wave_tiles, splits, rows_cap, a, SharedArgs{});
+}
+template <int TYPE, int D, int G>
+__global__ void __launch_bounds__(kThreads) attn_shared_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a,
+                                                                    const SharedArgs sh) {
+  attn_join<TYPE, D, G, true>(q_start, partial, wave_tiles, splits, rows_cap, a, sh);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -621,6 +786,120 @@ int launch_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
   }
 }
 
+// ---- sequences that share a prefix -----------------------------------------------------------------------------------
+
+struct SharedPlan { int rows, wr, tiles, splits, rows_cap, own_tiles, own_splits, own_cap; };
+
+SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
+  SharedPlan p;
+  const int64_t group = d->q_heads / d->cache.kv_heads, heads = d->cache.kv_heads;
+  auto blocks_of = [](int64_t tokens) { return (std::max<int64_t>(tokens, 1) + kKvBlock - 1) / kKvBlock; };
+  // rows of all of a group's sequences over the shared blocks
+  const int64_t rows = std::min<int64_t>(d->tokens, (int64_t)d->max_q * g->max_sequences) * group;
+  const int64_t held = std::min<int64_t>(d->tokens * group / 32 + g->groups, g->groups * ((rows + 31) / 32)) * heads;      // tiles that hold something, about
+  const int64_t blocks = blocks_of(d->window > 0 ? std::min<int64_t>(g->max_shared, (int64_t)d->window + d->max_q) : g->max_shared);
+  p.rows = (int)rows;
+  p.wr = held >= 2048 ? 4 : 1;
+  p.tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
+  p.rows_cap = (int)std::min<int64_t>(32, rows);
+  const int64_t most = p.wr == 4 ? 1 : std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(held, 1), (blocks + 7) / 8));
+  p.splits = (int)std::min<int64_t>(most, 64);
+  // a sequence's rows over its own blocks
+  const int64_t own_rows = (int64_t)d->max_q * group, own_held = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((own_rows + 31) / 32)) * heads;
+  const int64_t own_blocks = blocks_of((int64_t)d->max_len - g->max_shared);
+  p.own_tiles = (int)((own_rows + 31) / 32);
+  p.own_cap = (int)std::min<int64_t>(32, own_rows);
+  p.own_splits = (int)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(own_held, 1), (own_blocks + 7) / 8)), 64);
+  return p;
+}
+
+// Whether anything is shared at all: else every sequence goes by itself.
+bool shares(const szo_attn_groups* g) { return g->groups > 0 && g->max_sequences > 0 && g->max_shared >= kKvBlock; }
+
+int check(const szo_attn_desc* d, const szo_attn_groups* g) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!g || g->groups < 0 || g->max_sequences < 0 || g->max_shared < 0 || g->reserved) return SZO_EINVAL;
+  if (nothing(d) || !shares(g)) return SZO_OK;
+  if (!g->group_start || !g->shared || !aligned_to(g->group_start, 4) || !aligned_to(g->shared, 4)) return SZO_EINVAL;
+  const szo_kv_cache& c = d->cache;
+  if (std::min<int64_t>(d->tokens, (int64_t)d->max_q * g->max_sequences) * (d->q_heads / c.kv_heads) > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
+  const SharedPlan p = plan_of(d, g);
+  const int64_t units = (int64_t)g->groups * p.tiles * p.splits, own = (int64_t)c.sequences * p.own_tiles * p.own_splits;
+  if ((units + own) * c.kv_heads > kMostGroups || (int64_t)p.own_tiles * 64 > 0x7FFFFFFF || c.sequences > 65535) return SZO_EUNSUPPORTED;
+  return SZO_OK;
+}
+
+size_t shared_floats(const szo_attn_desc* d, const szo_attn_groups* g, const SharedPlan& p) {
+  return (size_t)g->groups * d->cache.kv_heads * p.tiles * p.wr * p.splits * part_floats(p.rows_cap, d->cache.head_dim);
+}
+size_t own_floats(const szo_attn_desc* d, const SharedPlan& p) {
+  return (size_t)d->cache.sequences * d->cache.kv_heads * p.own_tiles * p.own_splits * part_floats(p.own_cap, d->cache.head_dim);
+}
+
+template <int TYPE, int D, int WR, int WK>
+int launch_shared(const AttnArgs& a, const SharedArgs& sh, int64_t units, hipStream_t s) {
+  constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 3) * sizeof(float);
+  static std::atomic<uint64_t> raised{0};
+  if (lds > 64 * 1024) {
+    const int rc = set_lds_limit_once(raised, (const void*)attn_shared_kernel<TYPE, D, WR, WK>, lds);
+    if (rc != SZO_OK) return rc;
+  }
+  attn_shared_kernel<TYPE, D, WR, WK><<<dim3((unsigned)(units * a.d.cache.kv_heads)), 64 * WR * WK, lds, s>>>(
+      a.d.q_start, a.d.cache.lengths, a.d.cache.page_table, a.d.cache.max_pages, a.blocks_per_page, a.splits, a.tiles, a, sh);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
+template <int TYPE, int D, int G>
+int join_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
+  const int pieces = (a.rows_cap * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
+  const dim3 grid((unsigned)(a.tiles * pieces), (unsigned)a.d.cache.kv_heads, (unsigned)a.d.cache.sequences);
+  attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, a.tiles, a.splits, a.rows_cap, a, sh);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
+template <int TYPE, int D>
+int launch_shared_all(const AttnArgs& a, SharedArgs sh, const SharedPlan& p, hipStream_t s) {
+  const int64_t own = (int64_t)a.d.cache.sequences * a.tiles * a.splits;
+  int rc;
+  if (p.wr == 4) {
+    rc = launch_shared<TYPE, D, 4, 1>(a, sh, sh.units, s);
+    if (rc != SZO_OK) return rc;
+    sh.first_unit = sh.units;
+    rc = launch_shared<TYPE, D, 1, 4>(a, sh, own, s);
+  } else {
+    rc = launch_shared<TYPE, D, 1, 4>(a, sh, sh.units + own, s);
+  }
+  if (rc != SZO_OK) return rc;
+  return sh.splits + a.splits < 6 || a.rows_cap > 16 ? join_shared<TYPE, D, 1>(a, sh, s) : join_shared<TYPE, D, 16>(a, sh, s);
+}
+
+template <int TYPE>
+int launch_shared_dim(const AttnArgs& a, const SharedArgs& sh, const SharedPlan& p, hipStream_t s) {
+  switch (a.d.cache.head_dim) {
+    case 64: return launch_shared_all<TYPE, 64>(a, sh, p, s);
+    case 96: return launch_shared_all<TYPE, 96>(a, sh, p, s);
+    case 128: return launch_shared_all<TYPE, 128>(a, sh, p, s);
+    default: return launch_shared_all<TYPE, 256>(a, sh, p, s);
+  }
+}
+
+// What both calls tell their kernels.
+AttnArgs args_of(const szo_attn_desc* d, void* workspace) {
+  AttnArgs a = {};
+  a.d = *d;
+  a.group = d->q_heads / d->cache.kv_heads;
+  a.blocks_per_page = d->cache.page_tokens / kKvBlock;
+  a.to_log2 = (d->scale < 0.f ? -d->scale : d->scale) * 1.44269504088896341f;
+  a.negate = d->scale < 0.f;
+  a.partial = (float*)workspace;
+  a.vec_q = aligned_to(d->q, 16) && d->q_token_stride % 8 == 0 && d->q_head_stride % 8 == 0;
+  a.vec_out = aligned_to(d->out, 8) && d->out_token_stride % 4 == 0 && d->out_head_stride % 4 == 0;
+  return a;
+}
+
 }  // namespace
 }  // namespace szo
 
@@ -653,19 +932,44 @@ int szo_attn_cached(const szo_attn_desc* d, void* workspace, void* stream) {
   if (nothing(d)) return SZO_OK;
   const Plan p = plan_of(d);
   if (p.splits > 1 && (!workspace || !aligned_to(workspace, 16))) return SZO_EINVAL;
-  AttnArgs a = {};
-  a.d = *d;
-  a.group = d->q_heads / d->cache.kv_heads;
-  a.blocks_per_page = d->cache.page_tokens / kKvBlock;
+  AttnArgs a = args_of(d, workspace);
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.rows_cap = p.rows_cap;
-  a.to_log2 = (d->scale < 0.f ? -d->scale : d->scale) * 1.44269504088896341f;
-  a.negate = d->scale < 0.f;
-  a.partial = (float*)workspace;
-  a.vec_q = aligned_to(d->q, 16) && d->q_token_stride % 8 == 0 && d->q_head_stride % 8 == 0;
-  a.vec_out = aligned_to(d->out, 8) && d->out_token_stride % 4 == 0 && d->out_head_stride % 4 == 0;
   return d->type == SZO_BF16 ? launch_dim<SZO_BF16>(a, p, (hipStream_t)stream) : launch_dim<SZO_F16>(a, p, (hipStream_t)stream);
+}
+
+size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* d, const szo_attn_groups* g) {
+  if (check(d, g) != SZO_OK || nothing(d)) return 16;
+  if (!shares(g)) return szo_attn_workspace_bytes(d);
+  const SharedPlan p = plan_of(d, g);
+  return (shared_floats(d, g, p) + own_floats(d, p)) * sizeof(float);
+}
+
+int szo_attn_shared(const szo_attn_desc* d, const szo_attn_groups* g, void* workspace, void* stream) {
+  const int rc = check(d, g);
+  if (rc != SZO_OK) return rc;
+  if (nothing(d)) return SZO_OK;
+  if (!shares(g)) return szo_attn_cached(d, workspace, stream);
+  if (!workspace || !aligned_to(workspace, 16)) return SZO_EINVAL;
+  const SharedPlan p = plan_of(d, g);
+  AttnArgs a = args_of(d, workspace);
+  a.tiles = p.own_tiles;
+  a.splits = p.own_splits;
+  a.rows_cap = p.own_cap;
+  SharedArgs sh = {};
+  sh.group_start = g->group_start;
+  sh.shared = g->shared;
+  sh.groups = g->groups;
+  sh.most_blocks = g->max_shared / kKvBlock;
+  sh.tiles = p.tiles;
+  sh.wave_tiles = p.tiles * p.wr;
+  sh.splits = p.splits;
+  sh.rows_cap = p.rows_cap;
+  sh.rows = p.rows;
+  sh.units = g->groups * p.tiles * p.splits;
+  sh.own_at = (int64_t)shared_floats(d, g, p);
+  return d->type == SZO_BF16 ? launch_shared_dim<SZO_BF16>(a, sh, p, (hipStream_t)stream) : launch_shared_dim<SZO_F16>(a, sh, p, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -90,6 +90,10 @@ class AttnDesc(C.Structure):
                 _fields(_I64, "out_token_stride out_head_stride") + _fields(_PTR, "lse"))
 
 
+class AttnGroups(C.Structure):
+    _fields_ = _fields(_I32, "groups max_sequences max_shared reserved") + _fields(_PTR, "group_start shared")
+
+
 class LogprobsDesc(C.Structure):
     _fields_ = (_fields(_I64, "rows vocab row_stride") + _fields(_I32, "type top") + _fields(C.c_float, "scale") + _fields(_I32, "reserved") +
                 _fields(_PTR, "logits targets logp entropy stats top_logp top_index loss_acc") + _fields(C.c_double, "loss_scale"))
@@ -139,6 +143,8 @@ _SIGS = {
     "szo_kv_cache_read": (C.c_int, [_P(KvCache), _P(KvTokens), C.c_void_p]),
     "szo_attn_cached": (C.c_int, [_P(AttnDesc), C.c_void_p, C.c_void_p]),
     "szo_attn_plan": (C.c_int, [_P(AttnDesc), C.c_void_p]),
+    "szo_attn_shared": (C.c_int, [_P(AttnDesc), _P(AttnGroups), C.c_void_p, C.c_void_p]),
+    "szo_attn_shared_workspace_bytes": (C.c_size_t, [_P(AttnDesc), _P(AttnGroups)]),
     "szo_attn_workspace_bytes": (C.c_size_t, [_P(AttnDesc)]),
     "szo_token_logprobs": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p]),
     "szo_logprobs_workspace_bytes": (C.c_size_t, [_P(LogprobsDesc)]),
@@ -526,6 +532,26 @@ def szo_attn_plan(desc):
     plan = (C.c_int32 * 4)()
     _check("szo_attn_plan", lib.szo_attn_plan(C.byref(desc), plan))
     return tuple(plan)
+
+
+def make_attn_groups(group_start, shared, max_sequences, max_shared):
+    """group_start i32 [groups + 1]: first sequence of each group; shared i32 [groups]: leading tokens that its sequences have in common.  Most sequences of a
+    group and most shared tokens, which the split of the work goes by."""
+    import torch
+    n = shared.shape[0]
+    g = AttnGroups(n, max_sequences, max_shared, 0, _typed(group_start, torch.int32, (n + 1,)), _typed(shared, torch.int32, (n,)))
+    g.keep = (group_start, shared)
+    return g
+
+
+def szo_attn_shared(desc, groups, workspace=None, stream=None):
+    """workspace: of szo_attn_shared_workspace_bytes() for this very pair."""
+    room = _room(workspace, lib.szo_attn_shared_workspace_bytes(C.byref(desc), C.byref(groups)))
+    _check("szo_attn_shared", lib.szo_attn_shared(C.byref(desc), C.byref(groups), room, _stream(stream)))
+
+
+def szo_attn_shared_workspace_bytes(desc, groups):
+    return int(lib.szo_attn_shared_workspace_bytes(C.byref(desc), C.byref(groups)))
 
 
 def make_logprobs_desc(logits, targets=None, logp=None, entropy=None, stats=None, top_logp=None, top_index=None, scale=1.0, loss_acc=None, loss_scale=1.0):
