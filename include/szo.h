@@ -475,6 +475,37 @@ size_t szo_logprobs_workspace_bytes(const szo_logprobs_desc* desc /* host */);
 int szo_token_logprobs_bwd(const szo_logprobs_desc* desc /* host */, const float* grad_logp, const float* grad_entropy,
                            void* grad_logits, int64_t grad_row_stride, void* stream);
 
+/* Log probabilities of given tokens straight from the final states: logits = x weight^T of a head that is not quantised (a tied embedding), softmax cross entropy
+ * of them, in tiles of the vocabulary; the logits are never in memory.
+ *   logp = scale logits_target - log sum exp(scale logits)
+ * Targets, ignored ones, infinities and NaN count as in szo_token_logprobs, and so do logp, stats and loss_acc.  Products of 16-bit values with sums in fp32. */
+typedef struct szo_head_desc {
+  int64_t rows, vocab;
+  int32_t width, type;          /* width a multiple of 64 up to 65536; SZO_BF16 or SZO_F16: of x and weight */
+  float   scale;                /* 1 / temperature, > 0 and at most SZO_MOST_SCALE                       */
+  int32_t reserved;             /* 0                                                                     */
+  const void *x, *weight;       /* device [rows, width], [vocab, width], 16-byte aligned                 */
+  int64_t x_stride, weight_stride;      /* multiples of 8, up to 2^22                                    */
+  const int32_t* targets;       /* device [rows]; NULL: every target ignored                             */
+  float* logp;                  /* device [rows], or NULL                                                */
+  float* stats;                 /* device [rows, 2]: largest logit, sum of exp(scale (x - largest)), or NULL; read by the backward */
+  double* loss_acc;             /* device double or NULL: loss_acc += loss_scale * sum of -logp over the rows with a target (logp may then not be NULL) */
+  double loss_scale;
+} szo_head_desc;
+/* workspace: device, szo_head_workspace_bytes(desc) for this very descriptor, 16-byte aligned, for this call alone while it runs.  SZO_EUNSUPPORTED: widths and strides
+ * other than those named, a vocabulary above 2^30, 2^23 tiles of 256 vocabulary entries and 64 to 256 rows. */
+int szo_head_logprobs(const szo_head_desc* desc /* host */, void* workspace, void* stream);
+size_t szo_head_workspace_bytes(const szo_head_desc* desc /* host */);
+/* Gradients by x and by the weight of a scalar whose gradient by logp is grad_logp (device fp32 [rows]), from the forward's stats:
+ *   d = scale grad_logp (1[v = target] - p),   x_grad = d weight,   weight_grad = d^T x
+ * The logits are computed again, piece by piece of the vocabulary; d is rounded to the type (fp16: times a power of two that the largest gradient sets).  x_grad and weight_grad (device,
+ * of the type, rows x_grad_stride and weight_grad_stride apart, 2-byte aligned; either may be NULL) are overwritten and may be the buffers of x and weight.  Rows whose target
+ * is ignored have gradient 0 and no part in weight_grad, whatever they hold.  workspace: szo_head_bwd_workspace_bytes(desc), up to 256 MiB for a piece of d and
+ * what sums of x_grad take. */
+int szo_head_logprobs_bwd(const szo_head_desc* desc /* host */, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad,
+                          int64_t weight_grad_stride, void* workspace, void* stream);
+size_t szo_head_bwd_workspace_bytes(const szo_head_desc* desc /* host */);
+
 /* ---- one-time set-up on the host (no GPU needed; deterministic) ------------------------- */
 
 /* Number of TCSR tiles of an [N,K] matrix: ceil(N/64) * (K/64).  0 if K % 64 != 0. */

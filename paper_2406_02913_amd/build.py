@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libszo.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 HIP_SOURCES = ["szo_kernels.hip", "szo_gemm.hip", "szo_smallm.hip", "szo_split.hip", "szo_onepass.hip", "szo_qk.hip", "szo_kvcache.hip",
-               "szo_attn.hip", "szo_logprobs.hip", "szo_block.hip"]
+               "szo_attn.hip", "szo_logprobs.hip", "szo_block.hip", "szo_head.hip"]
 HOST_SOURCES = ["szo_host.cpp"]
 
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -1,0 +1,561 @@
+// Log probabilities of given tokens from final states x [rows, width] and a head's weight [vocab, width], and their gradients (definition: szo.h).
+//
+//   logits = x W^T;   logp_t = c logits_t,target - log sum_v exp(c logits_tv)
+//   d_tv = c g_t (1[v = target] - p_tv),   dx = d W,   dW = d^T x
+//
+// The logits stay in the registers of the tile that computes them: a tile of 256 vocabulary entries reduces them to a row's maximum and sum of exponentials (and the target's
+// logit, where it has it), and a small kernel joins the tiles of a row.  The backward computes them again, turns them into d, rounded to 16 bits, and multiplies that
+// twice.  d is in memory for a piece of the vocabulary at a time.  Three products of the same size, bound by the matrix cores for many rows and by one pass
+// over the weight for few.
+#include <algorithm>
+#include "szo_product.h"
+
+namespace szo {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kTileV = 256, kThreads = 512;
+constexpr size_t kPieceBytes = (size_t)256 << 20;        // of d, at most
+constexpr int64_t kMostGroups = 0xFFFFFFFFll / kThreads, kMostSmallGroups = 0xFFFFFFFFll / 256;      // a launch counts its threads in 32 bits
+
+struct HeadArgs {
+  szo_head_desc d;
+  int tiles_v, tiles_t;
+  float2* parts;                     // [rows][tiles_v]: maximum, sum
+  float* hit;                        // [rows]: the target's logit
+  // backward
+  int64_t first_v, piece_v;          // of this piece of the vocabulary; its columns
+  int64_t pitch;                     // columns of d in memory, a multiple of 256
+  int64_t rows64;                    // rows, rounded up to a multiple of 64
+  uint16_t* grad;                    // d [rows64][pitch]
+  const float* row_grad;             // [rows]: scale * gradient * lift, 0 where the target is ignored
+  const float* lift;                 // [2]: the power of two that d is multiplied by, and its inverse
+  const uint16_t* x_copy;            // x [rows64][width], rows without a target 0
+  float* sums;                       // x_grad in parts [splits][rows][width]
+  int splits, steps, add;            // parts of a piece, 64-wide steps of it, whether to add to what is there
+  void* out;
+  int64_t out_stride;
+  int out_vec;
+};
+
+__device__ __forceinline__ float groups_max(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+#endif
+  return v;
+}
+__device__ __forceinline__ float groups_sum(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+#endif
+  return v;
+}
+
+template <int TYPE>
+__device__ __forceinline__ uint2 rounded4(const f32x4& v, float by) {
+  typedef typename TypeOf<TYPE>::type T;
+  typedef T four __attribute__((ext_vector_type(4)));
+  const four h = {(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
+  return __builtin_bit_cast(uint2, h);
+}
+
+// Logits of a tile: vocabulary entries of [v0, v0 + 256) by rows of [t0, t0 + BT).
+template <int TYPE, int BT, int WI, int WJ> using LogitTile = Tile<TYPE, false, false, kTileV, BT, WI, WJ>;
+
+template <int TYPE, int BT, int WI, int WJ>
+__device__ __forceinline__ void logits_of(LogitTile<TYPE, BT, WI, WJ>& tile, const HeadArgs& a, int64_t v0, int64_t t0, lds_at lds, int wave, int lane) {
+  const szo_head_desc& d = a.d;
+  const Operand w = {static_cast<const uint16_t*>(d.weight) + v0 * d.weight_stride, d.weight_stride, min((int64_t)kTileV, d.vocab - v0), d.width};
+  const Operand x = {static_cast<const uint16_t*>(d.x) + t0 * d.x_stride, d.x_stride, min((int64_t)BT, d.rows - t0), d.width};
+  tile.run(w, x, d.width / kStep, lds, wave, lane);
+}
+
+template <int TYPE, int BT, int WI, int WJ>
+__global__ void __launch_bounds__(kThreads, 2) head_stats_kernel(const HeadArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  typedef LogitTile<TYPE, BT, WI, WJ> L;
+  const szo_head_desc& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  tile_of(blockIdx.x, a.tiles_v, a.tiles_t, ti, tj);
+  const int64_t v0 = (int64_t)ti * kTileV, t0 = (int64_t)tj * BT;
+  L tile;
+  logits_of<TYPE, BT, WI, WJ>(tile, a, v0, t0, (lds_at)lds, wave, lane);
+  __syncthreads();
+  float2* const meet = reinterpret_cast<float2*>(lds);                 // [WI][BT]
+  const float by = d.scale * kLog2e;
+  const int mine = wi * (kTileV / WI) + 4 * (lane >> 4);              // this lane's first entry
+  const int there = (int)min((int64_t)kTileV, d.vocab - v0);
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int column = wj * (BT / WJ) + 16 * j + (lane & 15);
+    const int64_t token = t0 + column;
+    const int64_t target = token < d.rows && d.targets ? d.targets[token] : -1;
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (mine + 16 * i + k >= there) tile.sum[i][j][k] = -__builtin_inff();
+        most = fmaxf(most, tile.sum[i][j][k]);
+      }
+    const int at = (int)(target - v0 - mine);
+    if (target >= v0 && target < v0 + there && at >= 0 && at < 16 * L::TI && (at & 15) < 4) {
+#pragma unroll
+      for (int i = 0; i < L::TI; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (at == 16 * i + k) a.hit[token] = tile.sum[i][j][k];
+    }
+    most = groups_max(most);
+    const float base = most == -__builtin_inff() ? 0.f : most;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += __builtin_amdgcn_exp2f((tile.sum[i][j][k] - base) * by);
+    sum = groups_sum(sum);
+    if (lane < 16) meet[wi * BT + column] = make_float2(most, sum);
+  }
+  __syncthreads();
+  for (int column = threadIdx.x; column < BT; column += kThreads) {
+    if (t0 + column >= d.rows) break;
+    float most = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WI; ++w) most = fmaxf(most, meet[w * BT + column].x);
+    const float base = most == -__builtin_inff() ? 0.f : most;
+#pragma unroll
+    for (int w = 0; w < WI; ++w) sum += meet[w * BT + column].y * __builtin_amdgcn_exp2f((meet[w * BT + column].x - base) * by);
+    a.parts[(t0 + column) * a.tiles_v + ti] = make_float2(most, sum);
+  }
+}
+
+// A wave joins the tiles of a row.
+__global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
+  const szo_head_desc& d = a.d;
+  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  const int lane = threadIdx.x & 63;
+  if (row >= d.rows) return;
+  const float2* parts = a.parts + row * a.tiles_v;
+  const float by = d.scale * kLog2e;
+  float most = -__builtin_inff(), sum = 0.f;
+#pragma unroll 4
+  for (int i = lane; i < a.tiles_v; i += 64) {
+    const float2 p = parts[i];
+    const float up = fmaxf(most, p.x), base = up == -__builtin_inff() ? 0.f : up;
+    sum = sum * __builtin_amdgcn_exp2f((most - base) * by) + p.y * __builtin_amdgcn_exp2f((p.x - base) * by);
+    most = up;
+  }
+  const float top = lanes_max<64>(most), base = top == -__builtin_inff() ? 0.f : top;
+  sum = lanes_sum<64>(sum * __builtin_amdgcn_exp2f((most - base) * by));
+  if (lane) return;
+  if (d.stats) { d.stats[2 * row] = top; d.stats[2 * row + 1] = sum; }
+  if (!d.logp) return;
+  const int64_t target = d.targets ? d.targets[row] : -1;
+  float logp = 0.f;
+  if (target >= 0 && target < d.vocab) logp = sum == 0.f ? -__builtin_inff() : (a.hit[row] - top) * d.scale - logf(sum);
+  d.logp[row] = logp;
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------------------
+
+// scale * gradient of each row, lifted for fp16 by the power of two that takes the largest to 2^13 .. 2^14: with |1 - p| <= 1 nothing overflows, and what is
+// 2^-27 of the largest still has all its bits.
+__global__ void __launch_bounds__(1024) head_rows_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* lift) {
+  __shared__ float part[16];
+  float most = 0.f;
+  auto of = [&](int64_t i) {
+    const int64_t t = d.targets ? d.targets[i] : -1;
+    return t >= 0 && t < d.vocab ? grad[i] * d.scale : 0.f;
+  };
+  for (int64_t i = threadIdx.x; i < d.rows; i += 1024) {
+    const float g = fabsf(of(i));
+    if (g < __builtin_inff()) most = fmaxf(most, g);
+  }
+  most = lanes_max<64>(most);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) most = fmaxf(most, part[w]);
+  const int up = d.type == SZO_F16 && most > 0.f ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
+  const float by = __builtin_amdgcn_ldexpf(1.f, up);
+  for (int64_t i = threadIdx.x; i < d.rows; i += 1024) row_grad[i] = of(i) * by;
+  if (threadIdx.x == 0) { lift[0] = by; lift[1] = __builtin_amdgcn_ldexpf(1.f, -up); }
+}
+
+// x with rows that have no target as 0: they may hold anything, and 0 times infinity would reach the weight's gradient.
+__global__ void __launch_bounds__(256) head_copy_kernel(const szo_head_desc d, int64_t rows64, uint16_t* out) {
+  const int per = d.width / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per, at = i % per * 8;
+  if (row >= rows64) return;
+  const int64_t target = row < d.rows && d.targets ? d.targets[row] : -1;
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (target >= 0 && target < d.vocab) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + row * d.x_stride + at);
+  *reinterpret_cast<uint4*>(out + row * d.width + at) = v;
+}
+
+// Rows of nothing.
+__global__ void __launch_bounds__(256) head_zero_kernel(uint16_t* out, int64_t rows, int64_t stride, int width) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / width;
+  if (row < rows) out[row * stride + i % width] = 0;
+}
+
+template <int TYPE, int BT, int WI, int WJ>
+__global__ void __launch_bounds__(kThreads, 2) head_grad_kernel(const HeadArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  typedef LogitTile<TYPE, BT, WI, WJ> L;
+  const szo_head_desc& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  tile_of(blockIdx.x, a.tiles_v, a.tiles_t, ti, tj);
+  const int64_t v0 = a.first_v + (int64_t)ti * kTileV, t0 = (int64_t)tj * BT;
+  L tile;
+  logits_of<TYPE, BT, WI, WJ>(tile, a, v0, t0, (lds_at)lds, wave, lane);
+  const float by = d.scale * kLog2e;
+  const int mine = wi * (kTileV / WI) + 4 * (lane >> 4);
+  const int there = (int)min((int64_t)kTileV, d.vocab - v0);
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t token = t0 + wj * (BT / WJ) + 16 * j + (lane & 15);
+    if (token >= a.rows64) continue;
+    const bool in = token < d.rows;
+    const float g = in ? a.row_grad[token] : 0.f, most = in ? d.stats[2 * token] : 0.f, sum = in ? d.stats[2 * token + 1] : 1.f;
+    const int64_t target = in && d.targets ? d.targets[token] : -1;
+    const bool none = target < 0 || target >= d.vocab || sum == 0.f;
+    const int hit = target >= v0 && target < v0 + there ? (int)(target - v0) - mine : -1;
+    const float share = g / sum;
+    uint16_t* const to = a.grad + token * a.pitch + (v0 - a.first_v) + mine;
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i) {
+      f32x4 y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float p = share * __builtin_amdgcn_exp2f((tile.sum[i][j][k] - most) * by);
+        const float v = hit == 16 * i + k ? g - p : -p;
+        y[k] = none || mine + 16 * i + k >= there ? 0.f : v;
+      }
+      *reinterpret_cast<uint2*>(to + 16 * i) = rounded4<TYPE>(y, 1.f);
+    }
+  }
+}
+
+// dx of a tile: features [k0, k0 + 256) by rows [t0, t0 + BT), over a part of the piece's vocabulary.
+template <int TYPE, int BT, int WI, int WJ>
+__global__ void __launch_bounds__(kThreads, 2) head_x_grad_kernel(const HeadArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  typedef Tile<TYPE, true, false, 256, BT, WI, WJ> L;
+  const szo_head_desc& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
+  const int tiles_k = (d.width + 255) / 256, per = tiles_k * a.tiles_t, split = blockIdx.x / per;
+  int ti, tj;
+  tile_of(blockIdx.x - split * per, tiles_k, a.tiles_t, ti, tj);
+  const int k0 = ti * 256, share = (a.steps + a.splits - 1) / a.splits, from = split * share, steps = min(share, a.steps - from);
+  const int64_t t0 = (int64_t)tj * BT, r0 = (int64_t)from * kStep;
+  L tile;
+  if (steps > 0) {
+    const Operand w = {static_cast<const uint16_t*>(d.weight) + (a.first_v + r0) * d.weight_stride + k0, d.weight_stride, d.width - k0, a.piece_v - r0};
+    const Operand g = {a.grad + t0 * a.pitch + r0, a.pitch, min((int64_t)BT, a.rows64 - t0), a.pitch - r0};
+    tile.run(w, g, steps, (lds_at)lds, wave, lane);
+  } else {
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i)
+#pragma unroll
+      for (int j = 0; j < L::TJ; ++j) tile.sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float by = a.lift[1];
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t token = t0 + wj * (BT / WJ) + 16 * j + (lane & 15);
+    if (token >= d.rows) continue;
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i) {
+      const int k = k0 + wi * (256 / WI) + 16 * i + 4 * (lane >> 4);
+      if (k >= d.width) continue;
+      if (a.sums) {
+        float4* const to = reinterpret_cast<float4*>(a.sums + ((int64_t)split * d.rows + token) * d.width + k);
+        float4 v = make_float4(tile.sum[i][j][0], tile.sum[i][j][1], tile.sum[i][j][2], tile.sum[i][j][3]);
+        if (a.add) {
+          const float4 had = *to;
+          v.x += had.x; v.y += had.y; v.z += had.z; v.w += had.w;
+        }
+        *to = v;
+      } else {
+        uint16_t* const to = static_cast<uint16_t*>(a.out) + token * a.out_stride + k;
+        const uint2 v = rounded4<TYPE>(tile.sum[i][j], by);
+        if (a.out_vec) *reinterpret_cast<uint2*>(to) = v;
+        else { to[0] = (uint16_t)v.x; to[1] = (uint16_t)(v.x >> 16); to[2] = (uint16_t)v.y; to[3] = (uint16_t)(v.y >> 16); }
+      }
+    }
+  }
+}
+
+// The parts of dx, added up in order.
+template <int TYPE>
+__global__ void __launch_bounds__(256) head_x_sum_kernel(const HeadArgs a) {
+  const szo_head_desc& d = a.d;
+  const int per = d.width / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per, k = i % per * 4;
+  if (row >= d.rows) return;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < a.splits; ++p) {
+    const float4 v = *reinterpret_cast<const float4*>(a.sums + ((int64_t)p * d.rows + row) * d.width + k);
+    s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+  }
+  uint16_t* const to = static_cast<uint16_t*>(a.out) + row * a.out_stride + k;
+  const uint2 v = rounded4<TYPE>(s, a.lift[1]);
+  if (a.out_vec) *reinterpret_cast<uint2*>(to) = v;
+  else { to[0] = (uint16_t)v.x; to[1] = (uint16_t)(v.x >> 16); to[2] = (uint16_t)v.y; to[3] = (uint16_t)(v.y >> 16); }
+}
+
+// dW of a tile: features [k0, k0 + 256) by vocabulary entries [v0, v0 + 256) of the piece.
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads, 2) head_weight_grad_kernel(const HeadArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  typedef Tile<TYPE, true, true, 256, 256, 2, 4> L;
+  const szo_head_desc& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
+  int ti, tj;
+  tile_of(blockIdx.x, (d.width + 255) / 256, a.tiles_v, ti, tj);
+  const int k0 = ti * 256;
+  const int64_t v0 = (int64_t)tj * 256;
+  const Operand x = {a.x_copy + k0, d.width, d.width - k0, a.rows64};
+  const Operand g = {a.grad + v0, a.pitch, a.pitch - v0, a.rows64};
+  L tile;
+  tile.run(x, g, (int)(a.rows64 / kStep), (lds_at)lds, wave, lane);
+  const float by = a.lift[1];
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t v = v0 + wj * 64 + 16 * j + (lane & 15);
+    if (v >= a.piece_v) continue;
+#pragma unroll
+    for (int i = 0; i < L::TI; ++i) {
+      const int k = k0 + wi * 128 + 16 * i + 4 * (lane >> 4);
+      if (k >= d.width) continue;
+      uint16_t* const to = static_cast<uint16_t*>(a.out) + (a.first_v + v) * a.out_stride + k;
+      const uint2 y = rounded4<TYPE>(tile.sum[i][j], by);
+      if (a.out_vec) *reinterpret_cast<uint2*>(to) = y;
+      else { to[0] = (uint16_t)y.x; to[1] = (uint16_t)(y.x >> 16); to[2] = (uint16_t)y.y; to[3] = (uint16_t)(y.y >> 16); }
+    }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostStride = 1 << 22;
+
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+int64_t tiles_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+int row_tile(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+
+int check(const szo_head_desc* d) {
+  if (!d || d->rows < 0 || d->vocab < 0 || d->width < 0 || (d->type != SZO_BF16 && d->type != SZO_F16) || d->reserved) return SZO_EINVAL;
+  if (!(d->scale > 0.f && d->scale <= SZO_MOST_SCALE)) return SZO_EINVAL;
+  if (d->width == 0 || d->width % 64 || d->width > 65536 || d->vocab > (1 << 30) || d->rows > 0x7FFFFFFF) return SZO_EUNSUPPORTED;
+  if (d->x_stride < 0 || d->weight_stride < 0 || (d->vocab > 1 && d->weight_stride < d->width)) return SZO_EINVAL;
+  if (d->x_stride > kMostStride || d->weight_stride > kMostStride || d->x_stride % 8 || d->weight_stride % 8) return SZO_EUNSUPPORTED;
+  if ((d->rows && !d->x) || (d->vocab && !d->weight) || !aligned_to(d->x, 16) || !aligned_to(d->weight, 16)) return SZO_EINVAL;
+  if (!aligned_to(d->targets, 4) || !aligned_to(d->logp, 4) || !aligned_to(d->stats, 4) || !aligned_to(d->loss_acc, 8)) return SZO_EINVAL;
+  if (tiles_of(d->vocab, kTileV) * tiles_of(d->rows, row_tile(d->rows)) > kMostGroups) return SZO_EUNSUPPORTED;
+  return SZO_OK;
+}
+
+// A launch of a kernel whose workgroup takes `bytes` of LDS.
+template <typename F, typename... Args>
+int launch(F* kernel, std::atomic<uint64_t>& raised, size_t bytes, int64_t groups, hipStream_t s, const Args&... args) {
+  const int rc = set_lds_limit_once(raised, (const void*)kernel, bytes);
+  if (rc != SZO_OK) return rc;
+  kernel<<<dim3((unsigned)groups), kThreads, bytes, s>>>(args...);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
+template <int TYPE, int BT, int WI, int WJ>
+int logit_launch(const HeadArgs& a, bool backward, hipStream_t s) {
+  static std::atomic<uint64_t> raised[2] = {{0}, {0}};
+  const int64_t groups = (int64_t)a.tiles_v * a.tiles_t;
+  return backward ? launch(head_grad_kernel<TYPE, BT, WI, WJ>, raised[1], LogitTile<TYPE, BT, WI, WJ>::kLds, groups, s, a)
+                  : launch(head_stats_kernel<TYPE, BT, WI, WJ>, raised[0], LogitTile<TYPE, BT, WI, WJ>::kLds, groups, s, a);
+}
+template <int TYPE>
+int logit_launch(const HeadArgs& a, bool backward, hipStream_t s) {
+  switch (row_tile(a.d.rows)) {
+    case 64: return logit_launch<TYPE, 64, 4, 2>(a, backward, s);
+    case 128: return logit_launch<TYPE, 128, 4, 2>(a, backward, s);
+    default: return logit_launch<TYPE, 256, 2, 4>(a, backward, s);
+  }
+}
+
+template <int TYPE, int BT, int WI, int WJ>
+int x_grad_launch(const HeadArgs& a, hipStream_t s) {
+  static std::atomic<uint64_t> raised{0};
+  const int64_t groups = tiles_of(a.d.width, 256) * a.tiles_t * a.splits;
+  return launch(head_x_grad_kernel<TYPE, BT, WI, WJ>, raised, Tile<TYPE, true, false, 256, BT, WI, WJ>::kLds, groups, s, a);
+}
+template <int TYPE>
+int x_grad_launch(const HeadArgs& a, hipStream_t s) {
+  switch (row_tile(a.d.rows)) {
+    case 64: return x_grad_launch<TYPE, 64, 4, 2>(a, s);
+    case 128: return x_grad_launch<TYPE, 128, 4, 2>(a, s);
+    default: return x_grad_launch<TYPE, 256, 2, 4>(a, s);
+  }
+}
+
+template <int TYPE>
+int weight_grad_launch(const HeadArgs& a, hipStream_t s) {
+  static std::atomic<uint64_t> raised{0};
+  return launch(head_weight_grad_kernel<TYPE>, raised, Tile<TYPE, true, true, 256, 256, 2, 4>::kLds, tiles_of(a.d.width, 256) * a.tiles_v, s, a);
+}
+
+// A backward: columns of d that are in memory at a time, parts of dx, and where things lie in the workspace.
+struct Plan {
+  int64_t rows64, pitch;
+  int pieces, splits;
+  size_t grad_at, copy_at, sums_at, rows_at, lift_at, bytes;
+};
+Plan plan_of(const szo_head_desc* d) {
+  Plan p;
+  p.rows64 = tiles_of(d->rows, 64) * 64;
+  const int64_t all = tiles_of(d->vocab, kTileV), fit = std::max<int64_t>(1, (int64_t)(kPieceBytes / 2) / (p.rows64 * kTileV));       // tiles of columns
+  p.pieces = (int)tiles_of(all, std::min(all, fit));
+  p.pitch = tiles_of(all, p.pieces) * kTileV;
+  const int64_t tiles = tiles_of(d->width, 256) * tiles_of(d->rows, row_tile(d->rows));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, p.pitch / kStep / 8));
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t was = at; at = up16(at + n); return was; };
+  p.grad_at = take((size_t)p.rows64 * p.pitch * 2);
+  p.copy_at = take((size_t)p.rows64 * d->width * 2);
+  p.sums_at = take(p.pieces > 1 || p.splits > 1 ? (size_t)p.splits * d->rows * d->width * sizeof(float) : 0);
+  p.rows_at = take((size_t)d->rows * sizeof(float));
+  p.lift_at = take(2 * sizeof(float));
+  p.bytes = at;
+  return p;
+}
+
+template <int TYPE>
+int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad, int64_t weight_grad_stride, char* room, hipStream_t s) {
+  const szo_head_desc& d = a.d;
+  head_rows_kernel<<<1, 1024, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.lift_at));
+  SZO_LAUNCH_CHECK();
+  if (weight_grad) {
+    head_copy_kernel<<<dim3((unsigned)tiles_of(p.rows64 * (d.width / 8), 256)), 256, 0, s>>>(d, p.rows64, (uint16_t*)(room + p.copy_at));
+    SZO_LAUNCH_CHECK();
+  }
+  a.rows64 = p.rows64;
+  a.pitch = p.pitch;
+  a.grad = (uint16_t*)(room + p.grad_at);
+  a.row_grad = (const float*)(room + p.rows_at);
+  a.lift = (const float*)(room + p.lift_at);
+  a.x_copy = (const uint16_t*)(room + p.copy_at);
+  a.splits = p.splits;
+  float* const sums = p.pieces > 1 || p.splits > 1 ? (float*)(room + p.sums_at) : nullptr;
+  auto vec = [](const void* q, int64_t stride) { return aligned_to(q, 8) && stride % 4 == 0; };
+  int rc = SZO_OK;
+  for (int piece = 0; piece < p.pieces; ++piece) {
+    a.first_v = (int64_t)piece * p.pitch;
+    a.piece_v = std::min(p.pitch, d.vocab - a.first_v);
+    a.tiles_v = (int)tiles_of(a.piece_v, kTileV);
+    a.steps = (int)tiles_of(a.piece_v, kStep);
+    rc = logit_launch<TYPE>(a, true, s);
+    if (rc != SZO_OK) return rc;
+    if (x_grad) {                            // before the weight's, which may overwrite the piece's rows of the weight
+      a.out = x_grad;
+      a.out_stride = x_grad_stride;
+      a.out_vec = vec(x_grad, x_grad_stride);
+      a.sums = sums;
+      a.add = piece > 0;
+      rc = x_grad_launch<TYPE>(a, s);
+      if (rc != SZO_OK) return rc;
+    }
+    if (weight_grad) {
+      a.out = weight_grad;
+      a.out_stride = weight_grad_stride;
+      a.out_vec = vec(weight_grad, weight_grad_stride);
+      rc = weight_grad_launch<TYPE>(a, s);
+      if (rc != SZO_OK) return rc;
+    }
+  }
+  if (x_grad && sums) {
+    a.sums = sums;
+    a.out = x_grad;
+    a.out_stride = x_grad_stride;
+    a.out_vec = vec(x_grad, x_grad_stride);
+    head_x_sum_kernel<TYPE><<<dim3((unsigned)tiles_of(d.rows * (d.width / 4), 256)), 256, 0, s>>>(a);
+    SZO_LAUNCH_CHECK();
+  }
+  return SZO_OK;
+}
+
+size_t parts_bytes(const szo_head_desc* d) { return up16((size_t)d->rows * tiles_of(d->vocab, kTileV) * sizeof(float2)); }
+
+}  // namespace
+}  // namespace szo
+
+using namespace szo;
+
+extern "C" {
+
+size_t szo_head_workspace_bytes(const szo_head_desc* d) {
+  if (check(d) != SZO_OK || d->rows == 0) return 16;
+  return parts_bytes(d) + up16((size_t)d->rows * sizeof(float));
+}
+
+int szo_head_logprobs(const szo_head_desc* d, void* workspace, void* stream) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (d->loss_acc && !d->logp) return SZO_EINVAL;
+  if (d->rows == 0) return SZO_OK;
+  if (d->vocab == 0 || !workspace || !aligned_to(workspace, 16)) return SZO_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  HeadArgs a = {};
+  a.d = *d;
+  a.tiles_v = (int)tiles_of(d->vocab, kTileV);
+  a.tiles_t = (int)tiles_of(d->rows, row_tile(d->rows));
+  a.parts = (float2*)workspace;
+  a.hit = (float*)((char*)workspace + parts_bytes(d));
+  const int done = d->type == SZO_BF16 ? logit_launch<SZO_BF16>(a, false, s) : logit_launch<SZO_F16>(a, false, s);
+  if (done != SZO_OK) return done;
+  head_join_kernel<<<dim3((unsigned)tiles_of(d->rows, 4)), 256, 0, s>>>(a);
+  SZO_LAUNCH_CHECK();
+  return d->loss_acc ? add_token_loss(d->logp, d->targets, d->rows, d->vocab, d->loss_scale, d->loss_acc, s) : SZO_OK;
+}
+
+size_t szo_head_bwd_workspace_bytes(const szo_head_desc* d) {
+  if (check(d) != SZO_OK || d->rows == 0 || d->vocab == 0) return 16;
+  return plan_of(d).bytes;
+}
+
+int szo_head_logprobs_bwd(const szo_head_desc* d, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad, int64_t weight_grad_stride,
+                          void* workspace, void* stream) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!aligned_to(x_grad, 2) || !aligned_to(weight_grad, 2) || !aligned_to(grad_logp, 4)) return SZO_EINVAL;
+  if ((x_grad && d->rows > 1 && x_grad_stride < d->width) || (weight_grad && d->vocab > 1 && weight_grad_stride < d->width)) return SZO_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  if (d->rows == 0 || d->vocab == 0) {
+    void* const out = d->rows ? x_grad : weight_grad;
+    const int64_t rows = d->rows ? d->rows : d->vocab, stride = d->rows ? x_grad_stride : weight_grad_stride, groups = tiles_of(rows * d->width, 256);
+    if (!out || rows == 0) return SZO_OK;
+    if (groups > kMostSmallGroups) return SZO_EUNSUPPORTED;
+    head_zero_kernel<<<dim3((unsigned)groups), 256, 0, s>>>((uint16_t*)out, rows, stride, d->width);
+    SZO_LAUNCH_CHECK();
+    return SZO_OK;
+  }
+  if (!d->stats || !grad_logp || !workspace || !aligned_to(workspace, 16)) return SZO_EINVAL;
+  if (!x_grad && !weight_grad) return SZO_OK;
+  if (tiles_of(tiles_of(d->rows, 64) * 64 * d->width, 4 * 256) > kMostSmallGroups) return SZO_EUNSUPPORTED;
+  HeadArgs a = {};
+  a.d = *d;
+  a.tiles_t = (int)tiles_of(d->rows, row_tile(d->rows));
+  const Plan p = plan_of(d);
+  if (tiles_of(d->width, 256) * a.tiles_t * p.splits > kMostGroups || tiles_of(d->width, 256) * (p.pitch / kTileV) > kMostGroups) return SZO_EUNSUPPORTED;
+  return d->type == SZO_BF16 ? backward<SZO_BF16>(a, p, grad_logp, x_grad, x_grad_stride, weight_grad, weight_grad_stride, (char*)workspace, s)
+                             : backward<SZO_F16>(a, p, grad_logp, x_grad, x_grad_stride, weight_grad, weight_grad_stride, (char*)workspace, s);
+}
+
+}  // extern "C"

@@ -121,6 +121,9 @@ bool stream_is_capturing(hipStream_t stream);
 // Sets n 32-bit words to zero with a small kernel (defined in szo_kernels.hip).
 int zero_words(void* p, int n, hipStream_t stream);
 
+// loss_acc[0] += scale * sum of -logp over the rows whose target is in [0, vocab) (defined in szo_logprobs.hip).
+int add_token_loss(const float* logp, const int32_t* targets, int64_t rows, int64_t vocab, double scale, double* loss_acc, hipStream_t stream);
+
 // Wave-wide sum in a fixed order (64 lanes): halves, then rows of 16, 8, 4, 2, 1 lanes added to each other; result valid in every
 // lane.  By lane swaps and row rotations, which stay in registers: the same sums by shuffles are six round trips through LDS, of two
 // permutations each, one after the other: 0.3 us at the end of kernels that take five.  (A row rotated by 4, 2 or 1 pairs the lanes that an exclusive or

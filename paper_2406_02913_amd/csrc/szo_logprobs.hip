@@ -306,6 +306,16 @@ __global__ void __launch_bounds__(1024) logp_loss_kernel(const float* __restrict
   *loss_acc += scale * s;
 }
 
+}  // namespace
+
+int add_token_loss(const float* logp, const int32_t* targets, int64_t rows, int64_t vocab, double scale, double* loss_acc, hipStream_t s) {
+  logp_loss_kernel<<<1, 1024, 0, s>>>(logp, targets, rows, vocab, scale, loss_acc);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
+
+namespace {
+
 struct GradArgs { szo_logprobs_desc d; const float *g_logp, *g_entropy; void* out; int64_t out_stride; int parts; };
 
 constexpr int kGradThreads = 256;
@@ -408,11 +418,7 @@ int szo_token_logprobs(const szo_logprobs_desc* d, void* workspace, void* stream
   else if (d->type == SZO_BF16) launch<SZO_BF16>(a, p, s);
   else launch<SZO_F16>(a, p, s);
   SZO_LAUNCH_CHECK();
-  if (d->loss_acc) {
-    logp_loss_kernel<<<1, 1024, 0, s>>>(d->logp, d->targets, d->rows, d->vocab, d->loss_scale, d->loss_acc);
-    SZO_LAUNCH_CHECK();
-  }
-  return SZO_OK;
+  return d->loss_acc ? add_token_loss(d->logp, d->targets, d->rows, d->vocab, d->loss_scale, d->loss_acc, s) : SZO_OK;
 }
 
 int szo_token_logprobs_bwd(const szo_logprobs_desc* d, const float* grad_logp, const float* grad_entropy, void* grad_logits, int64_t grad_row_stride,

@@ -1,0 +1,229 @@
+// Products of 16-bit matrices in tiles of BI x BJ for a workgroup of eight waves, C[i][j] = sum over r of A(i, r) B(j, r), sums in fp32 registers.
+//
+// Either operand lies in memory with r contiguous ("rows": a row of A is an i) or with i (j) contiguous ("columns": a row is an r).  A step takes 64 of r.  Its
+// operands go from memory to LDS without passing through registers, 16 bytes a lane and 1 KiB an instruction, two steps' worth held; lanes choose what they
+// read, since a load puts them side by side in LDS:
+//   rows     [row][64 of r]: the eight 16-byte pieces of a row are exchanged by (row / 2) mod 8, so that 16 lanes that read one piece of 16 rows touch every bank once
+//   columns  [r][256 of i], two r to an instruction: 16-wide groups are exchanged in pairs in odd r, pairs of r lie 64 bytes and eights of them 128 further than they are
+//            long, so that the four 32-byte pieces each of two groups of 16 lanes, which the transposing LDS read asks for together, lie in different banks
+// A half step's operands are read into registers while the other half's products run: after the one barrier of a step no wave has to wait for LDS.
+#pragma once
+#include "szo_internal.h"
+#include "szo_types.h"
+
+namespace szo {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uint8_t* lds_at;
+typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
+
+template <int TYPE> struct Product;
+template <> struct Product<SZO_BF16> {
+  typedef bf16x8 vec;
+  static __device__ __forceinline__ f32x4 add(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Product<SZO_F16> {
+  typedef f16x8 vec;
+  static __device__ __forceinline__ f32x4 add(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+constexpr int kStep = 64;                  // of r
+constexpr int kPairBytes = 1024 + 64;      // columns: two r of 256, and what pairs are apart
+
+// An operand as it lies in memory: `stride` elements from row to row.  rows: r runs from 0 to `length`, `count` rows from `base` on.  columns: `length` rows from `base`
+// on, of which `count` elements are there (256 are read: what is behind them reaches only sums that nobody stores).
+struct Operand {
+  const uint16_t* base;
+  int64_t stride;
+  int64_t count, length;
+};
+
+template <bool COLUMNS, int SIZE> constexpr int stage_bytes() { return COLUMNS ? 32 * kPairBytes + 8 * 128 : SIZE * kStep * 2; }
+
+// One operand of a workgroup's tile: its loads to LDS and its reads from there.
+template <bool COLUMNS, int SIZE, int PER>           // PER: 16-wide groups of a wave
+struct Side {
+  static constexpr int kLoads = SIZE / 64;           // of a wave and step
+  static constexpr int kStage = stage_bytes<COLUMNS, SIZE>();
+  static_assert(!COLUMNS || SIZE == 256, "columns are laid out for 256");
+  uint32_t from[kLoads];                             // bytes from the step's first row or column
+  uint32_t lds;                                      // where this wave's loads go, in a stage
+  lds_at read[2];                                    // rows: of the two halves of a step; columns: of even and odd groups
+  uint64_t base;
+  uint32_t pitch;                                    // bytes of a row
+  int64_t left;                                      // bytes (rows) or rows (columns) behind `base`
+  int64_t count;
+
+  // `wave_first`: first of this wave's SIZE values
+  __device__ __forceinline__ Side(const Operand& o, lds_at stages, int wave, int wave_first, int lane) {
+    pitch = (uint32_t)(o.stride * 2);
+    base = (uint64_t)(uintptr_t)o.base;
+    count = o.count;
+    if constexpr (COLUMNS) {
+      left = o.length;
+      const uint32_t r = (uint32_t)lane >> 5, piece = ((uint32_t)lane & 31u) ^ (2u * r);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) from[i] = (uint32_t)(2 * (wave * kLoads + i) + (int)r) * pitch + 16u * piece;
+      lds = (uint32_t)(uintptr_t)stages + (uint32_t)(wave * kLoads) * kPairBytes + (uint32_t)wave * 128u;       // kLoads is 4: pairs 4 w .. + 3
+      // lane p of sixteen: 8 bytes of row 8 g + p / 4; the row's pair is 4 g + p / 8
+      const int g = lane >> 4, p = lane & 15, odd = p >> 2 & 1;
+      const lds_at at = stages + (4 * g + (p >> 3)) * kPairBytes + g * 128 + odd * 512 + (p & 3) * 8 + wave_first * 2;
+      read[0] = at + odd * 32;
+      read[1] = at - odd * 32;
+    } else {
+      left = ((o.count - 1) * o.stride + o.length) * 2;
+      // rows of an instruction: eight, the same eight of sixteen for all of a wave's
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t row = (uint32_t)(((wave >> 1) * kLoads + i) * 16 + (wave & 1) * 8 + (lane >> 3));
+        from[i] = row * pitch + 16u * (((uint32_t)lane & 7u) ^ (row >> 1 & 7u));
+      }
+      lds = (uint32_t)(uintptr_t)stages + (uint32_t)((wave >> 1) * kLoads * 16 + (wave & 1) * 8) * 128u;
+      const int row = wave_first + (lane & 15), swizzle = (lane & 15) >> 1;
+      read[0] = stages + row * 128 + (((lane >> 4) ^ swizzle) << 4);
+      read[1] = stages + row * 128 + ((((lane >> 4) + 4) ^ swizzle) << 4);
+    }
+  }
+
+  // Loads of the next step; addresses out of bounds read as zero.  In assembly: behind the compiler's own form it waits for all of them at every LDS read.
+  __device__ __forceinline__ void load(int stage) {
+    uint32_t bytes;
+    if constexpr (COLUMNS) bytes = left <= 0 ? 0u : (uint32_t)min(left - 1, (int64_t)kStep - 1) * pitch + (uint32_t)count * 2u;
+    else bytes = left <= 0 ? 0u : (uint32_t)left;
+    const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00027000u};
+    const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + (uint32_t)(stage * kStage)));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    // m0 is no register that values are allocated to, which the compiler warns of; named all the same.  Wait states: a vector instruction may have written the
+    // descriptor just before.
+    if constexpr (kLoads == 4) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %1, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %2, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %3, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %4, %5, 0 offen lds" ::
+                   "s"(to), "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "s"(rsrc), "i"(COLUMNS ? kPairBytes : 2048) : "memory", "scc", "m0");
+    } else if constexpr (kLoads == 2) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %1, %3, 0 offen lds\n\ts_add_u32 m0, m0, %4\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %2, %3, 0 offen lds" ::
+                   "s"(to), "v"(from[0]), "v"(from[1]), "s"(rsrc), "i"(2048) : "memory", "scc", "m0");
+    } else {
+      static_assert(kLoads == 1, "64, 128 or 256");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(from[0]), "s"(rsrc) : "memory", "scc", "m0");
+    }
+#pragma clang diagnostic pop
+    if constexpr (COLUMNS) {
+      base += (uint64_t)pitch * kStep;
+      left -= kStep;
+    } else {
+      base += kStep * 2;
+      left -= kStep * 2;
+    }
+  }
+
+  // Group t of 16, half h of a step: a lane's eight of r.
+  template <int TYPE>
+  __device__ __forceinline__ typename Product<TYPE>::vec fragment(int stage, int half, int t) const {
+    typedef typename Product<TYPE>::vec vec;
+    typedef __attribute__((address_space(3))) const vec* vec_at;
+    if constexpr (COLUMNS) {
+      typedef short short4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) short4_t* four_at;
+      const lds_at at = read[t & 1] + (stage * kStage + half * (16 * kPairBytes + 4 * 128) + t * 32);
+      struct { uint64_t lo, hi; } both;
+      both.lo = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((four_at)at));
+      both.hi = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((four_at)(at + 2 * kPairBytes)));
+      return __builtin_bit_cast(vec, both);
+    } else {
+      return *(vec_at)(read[half] + (stage * kStage + t * 2048));
+    }
+  }
+};
+
+// The tile's sums: a lane has C[16 ti + 4 (lane / 16) + 0..3][16 tj + lane % 16] of its wave's part.  `steps` > 0 steps.
+template <int TYPE, bool A_COLUMNS, bool B_COLUMNS, int BI, int BJ, int WI, int WJ>
+struct Tile {
+  static constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
+  static constexpr int kLds = 2 * (stage_bytes<A_COLUMNS, BI>() + stage_bytes<B_COLUMNS, BJ>());
+  static_assert(WI * WJ == 8 && kLds <= 160 * 1024, "eight waves, one workgroup's LDS");
+  typedef typename Product<TYPE>::vec vec;
+  f32x4 sum[TI][TJ];
+
+  __device__ __forceinline__ void run(const Operand& a_op, const Operand& b_op, int steps, lds_at lds, int wave, int lane) {
+    Side<A_COLUMNS, BI, TI> a(a_op, lds, wave, wave / WJ * (BI / WI), lane);
+    Side<B_COLUMNS, BJ, TJ> b(b_op, lds + 2 * stage_bytes<A_COLUMNS, BI>(), wave, wave % WJ * (BJ / WJ), lane);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    vec x[2][TI], y[2][TJ];
+    auto take = [&](int stage, int half) {
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) y[half][j] = b.template fragment<TYPE>(stage, half, j);
+#pragma unroll
+      for (int i = 0; i < TI; ++i) x[half][i] = a.template fragment<TYPE>(stage, half, i);
+    };
+    auto multiply = [&](int half) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) sum[i][j] = Product<TYPE>::add(x[half][i], y[half][j], sum[i][j]);
+    };
+    // LDS reads between products, so that neither waits for a row of the other
+    auto interleave = [] {
+      constexpr int reads = TI * (A_COLUMNS ? 2 : 1) + TJ * (B_COLUMNS ? 2 : 1);
+#pragma unroll
+      for (int k = 0; k < reads; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, TI * TJ / reads, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, TI * TJ - TI * TJ / reads * reads, 0);
+    };
+    a.load(0);
+    b.load(0);
+    if (steps > 1) {
+      a.load(1);
+      b.load(1);
+      if constexpr (Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+      else if constexpr (Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+      else asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    asm volatile("s_barrier" ::: "memory");
+    take(0, 0);
+    auto step = [&](int stage, int at) {
+      take(stage, 1);
+      multiply(0);
+      interleave();
+      // every wave has read the stage, and the next one has arrived for all of them
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (at + 2 < steps) {
+        a.load(stage);
+        b.load(stage);
+      }
+      take(stage ^ 1, 0);                  // behind the last step: what lies there, for nothing
+      multiply(1);
+      interleave();
+    };
+    int at = 0;
+    for (; at + 1 < steps; at += 2) {
+      step(0, at);
+      step(1, at + 1);
+    }
+    if (at < steps) step(0, at);
+  }
+};
+
+// Workgroup -> tile.  Workgroups are dealt out to the 8 XCDs in turn: each gets a run of tiles of its own, in columns of four, so that the 32 tiles that its CUs work on
+// share 4 + 8 operands in its L2.
+__device__ __forceinline__ void tile_of(int id, int tiles_i, int tiles_j, int& i, int& j) {
+  const int all = tiles_i * tiles_j, each = all / 8, more = all % 8, xcd = id % 8, at = id / 8;
+  const int n = xcd * each + min(xcd, more) + at;            // xcd < more have one more
+  const int band = n / (4 * tiles_j), first = band * 4, high = min(4, tiles_i - first), within = n - band * 4 * tiles_j;
+  j = within / high;
+  i = first + within % high;
+}
+
+}  // namespace szo

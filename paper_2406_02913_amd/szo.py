@@ -99,6 +99,11 @@ class LogprobsDesc(C.Structure):
                 _fields(_PTR, "logits targets logp entropy stats top_logp top_index loss_acc") + _fields(C.c_double, "loss_scale"))
 
 
+class HeadDesc(C.Structure):
+    _fields_ = (_fields(_I64, "rows vocab") + _fields(_I32, "width type") + _fields(C.c_float, "scale") + _fields(_I32, "reserved") + _fields(_PTR, "x weight") +
+                _fields(_I64, "x_stride weight_stride") + _fields(_PTR, "targets logp stats loss_acc") + _fields(C.c_double, "loss_scale"))
+
+
 _P = C.POINTER
 _SIGS = {
     "szo_linear_fwd": (C.c_int, [_P(LinearDesc), C.c_uint64, C.c_uint64, C.c_int, C.c_float, C.c_void_p]),
@@ -149,6 +154,10 @@ _SIGS = {
     "szo_token_logprobs": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p]),
     "szo_logprobs_workspace_bytes": (C.c_size_t, [_P(LogprobsDesc)]),
     "szo_token_logprobs_bwd": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "szo_head_logprobs": (C.c_int, [_P(HeadDesc), C.c_void_p, C.c_void_p]),
+    "szo_head_workspace_bytes": (C.c_size_t, [_P(HeadDesc)]),
+    "szo_head_logprobs_bwd": (C.c_int, [_P(HeadDesc), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "szo_head_bwd_workspace_bytes": (C.c_size_t, [_P(HeadDesc)]),
     "szo_last_hip_error": (C.c_int, []),
     "szo_version": (C.c_int, []),
 }
@@ -588,6 +597,47 @@ def szo_token_logprobs_bwd(desc, grad_logp, grad_entropy, grad_logits, stream=No
         raise ValueError("expected a gradient of the logits' shape and type")
     _check("szo_token_logprobs_bwd", lib.szo_token_logprobs_bwd(C.byref(desc), _typed(grad_logp, torch.float32, (R,)), _typed(grad_entropy, torch.float32, (R,)),
                                                                 grad_logits.data_ptr(), grad_logits.stride(0), _stream(stream)))
+
+
+def make_head_desc(x, weight, targets=None, logp=None, stats=None, scale=1.0, loss_acc=None, loss_scale=1.0):
+    """x [rows, width], weight [vocab, width], bf16 or fp16, rows any multiple of 8 apart; targets i32 [rows]; outputs that are None are not computed."""
+    import torch
+    R, K = x.shape
+    V = weight.shape[0]
+    d = HeadDesc(R, V, K, _type(x), scale, 0)
+    d.x, d.x_stride = _rows(x, x.dtype, R, K)
+    d.weight, d.weight_stride = _rows(weight, x.dtype, V, K)
+    d.targets, d.logp = _typed(targets, torch.int32, (R,)), _typed(logp, torch.float32, (R,))
+    d.stats = _typed(stats, torch.float32, (R, 2))
+    d.loss_acc = None if loss_acc is None else _typed(loss_acc, torch.float64, loss_acc.shape)
+    d.loss_scale = loss_scale
+    d.dtype = x.dtype
+    d.keep = (x, weight, targets, logp, stats, loss_acc)
+    return d
+
+
+def szo_head_logprobs(desc, workspace=None, stream=None):
+    """workspace: of szo_head_workspace_bytes() for this very descriptor."""
+    room = _room(workspace, lib.szo_head_workspace_bytes(C.byref(desc)))
+    _check("szo_head_logprobs", lib.szo_head_logprobs(C.byref(desc), room, _stream(stream)))
+
+
+def szo_head_workspace_bytes(desc):
+    return int(lib.szo_head_workspace_bytes(C.byref(desc)))
+
+
+def szo_head_logprobs_bwd(desc, grad_logp, x_grad=None, weight_grad=None, workspace=None, stream=None):
+    """grad_logp fp32 [rows]; x_grad and weight_grad like x and weight (or None: not wanted), or these themselves."""
+    import torch
+    R, V, K = desc.rows, desc.vocab, desc.width
+    xp, xs = _rows(x_grad, desc.dtype, R, K)
+    wp, ws = _rows(weight_grad, desc.dtype, V, K)
+    room = _room(workspace, lib.szo_head_bwd_workspace_bytes(C.byref(desc)))
+    _check("szo_head_logprobs_bwd", lib.szo_head_logprobs_bwd(C.byref(desc), _typed(grad_logp, torch.float32, (R,)), xp, xs, wp, ws, room, _stream(stream)))
+
+
+def szo_head_bwd_workspace_bytes(desc):
+    return int(lib.szo_head_bwd_workspace_bytes(C.byref(desc)))
 
 
 # ---- host set-up -----------------------------------------------------------------------------
