@@ -6,7 +6,7 @@
 //   rows     [row][64 of r]: the eight 16-byte pieces of a row are exchanged by (row / 2) mod 8, so that 16 lanes that read one piece of 16 rows touch every bank once
 //   columns  [r][256 of i], two r to an instruction: 16-wide groups are exchanged in pairs in odd r, pairs of r lie 64 bytes and eights of them 128 further than they are
 //            long, so that the four 32-byte pieces each of two groups of 16 lanes, which the transposing LDS read asks for together, lie in different banks
-// A half step's operands are read into registers while the other half's products run: after the one barrier of a step no wave has to wait for LDS.
+// Fragments are read from LDS a few groups of products before they are used, across the one barrier of a step.
 #pragma once
 #include "szo_internal.h"
 #include "szo_types.h"
@@ -46,24 +46,24 @@ struct Side {
   static constexpr int kLoads = SIZE / 64;           // of a wave and step
   static constexpr int kStage = stage_bytes<COLUMNS, SIZE>();
   static_assert(!COLUMNS || SIZE == 256, "columns are laid out for 256");
-  uint32_t from[kLoads];                             // bytes from the step's first row or column
+  uint32_t from, apart;                              // bytes from the step's first row or column to this lane's first 16, and from one load to the next
   uint32_t lds;                                      // where this wave's loads go, in a stage
   lds_at read[2];                                    // rows: of the two halves of a step; columns: of even and odd groups
   uint64_t base;
   uint32_t pitch;                                    // bytes of a row
-  int64_t left;                                      // bytes (rows) or rows (columns) behind `base`
-  int64_t count;
+  int left;                                          // bytes (rows) or rows (columns) behind `base`
+  uint32_t row_bytes;                                // columns: of a row, those that are there
 
   // `wave_first`: first of this wave's SIZE values
   __device__ __forceinline__ Side(const Operand& o, lds_at stages, int wave, int wave_first, int lane) {
     pitch = (uint32_t)(o.stride * 2);
     base = (uint64_t)(uintptr_t)o.base;
-    count = o.count;
+    row_bytes = (uint32_t)(o.count * 2);
     if constexpr (COLUMNS) {
-      left = o.length;
+      left = (int)o.length;
       const uint32_t r = (uint32_t)lane >> 5, piece = ((uint32_t)lane & 31u) ^ (2u * r);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) from[i] = (uint32_t)(2 * (wave * kLoads + i) + (int)r) * pitch + 16u * piece;
+      from = (uint32_t)(2 * wave * kLoads + (int)r) * pitch + 16u * piece;
+      apart = 2 * pitch;
       lds = (uint32_t)(uintptr_t)stages + (uint32_t)(wave * kLoads) * kPairBytes + (uint32_t)wave * 128u;       // kLoads is 4: pairs 4 w .. + 3
       // lane p of sixteen: 8 bytes of row 8 g + p / 4; the row's pair is 4 g + p / 8
       const int g = lane >> 4, p = lane & 15, odd = p >> 2 & 1;
@@ -71,55 +71,48 @@ struct Side {
       read[0] = at + odd * 32;
       read[1] = at - odd * 32;
     } else {
-      left = ((o.count - 1) * o.stride + o.length) * 2;
+      left = (int)(((o.count - 1) * o.stride + o.length) * 2);
       // rows of an instruction: eight, the same eight of sixteen for all of a wave's
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t row = (uint32_t)(((wave >> 1) * kLoads + i) * 16 + (wave & 1) * 8 + (lane >> 3));
-        from[i] = row * pitch + 16u * (((uint32_t)lane & 7u) ^ (row >> 1 & 7u));
-      }
-      lds = (uint32_t)(uintptr_t)stages + (uint32_t)((wave >> 1) * kLoads * 16 + (wave & 1) * 8) * 128u;
-      const int row = wave_first + (lane & 15), swizzle = (lane & 15) >> 1;
-      read[0] = stages + row * 128 + (((lane >> 4) ^ swizzle) << 4);
-      read[1] = stages + row * 128 + ((((lane >> 4) + 4) ^ swizzle) << 4);
+      const uint32_t first = (uint32_t)((wave >> 1) * kLoads * 16 + (wave & 1) * 8), row = first + ((uint32_t)lane >> 3);
+      from = row * pitch + 16u * (((uint32_t)lane & 7u) ^ (row >> 1 & 7u));
+      apart = 16 * pitch;
+      lds = (uint32_t)(uintptr_t)stages + first * 128u;
+      const int at = wave_first + (lane & 15), swizzle = (lane & 15) >> 1;
+      read[0] = stages + at * 128 + (((lane >> 4) ^ swizzle) << 4);
+      read[1] = stages + at * 128 + ((((lane >> 4) + 4) ^ swizzle) << 4);
     }
   }
 
-  // Loads of the next step; addresses out of bounds read as zero.  In assembly: behind the compiler's own form it waits for all of them at every LDS read.
+  // Loads of the next step, which is there; addresses out of bounds read as zero.  In assembly: behind the compiler's own form it waits for all of them at every LDS
+  // read, and kept apart the loads' addresses would take registers that the main loop has not got.
   __device__ __forceinline__ void load(int stage) {
-    uint32_t bytes;
-    if constexpr (COLUMNS) bytes = left <= 0 ? 0u : (uint32_t)min(left - 1, (int64_t)kStep - 1) * pitch + (uint32_t)count * 2u;
-    else bytes = left <= 0 ? 0u : (uint32_t)left;
-    const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00027000u};
-    const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds + (uint32_t)(stage * kStage)));
+    const uint32_t bytes = COLUMNS ? (uint32_t)min(left - 1, kStep - 1) * pitch + row_bytes : (uint32_t)left;
+    const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32), bytes, 0x00027000u};
+    const uint32_t to = lds + (uint32_t)(stage * kStage);
+    uint32_t at;
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
     // m0 is no register that values are allocated to, which the compiler warns of; named all the same.  Wait states: a vector instruction may have written the
     // descriptor just before.
     if constexpr (kLoads == 4) {
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
-                   "buffer_load_dwordx4 %1, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %2, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %3, %5, 0 offen lds\n\ts_add_u32 m0, m0, %6\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %4, %5, 0 offen lds" ::
-                   "s"(to), "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "s"(rsrc), "i"(COLUMNS ? kPairBytes : 2048) : "memory", "scc", "m0");
+      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
+                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(COLUMNS ? kPairBytes : 2048) : "memory", "scc", "m0");
     } else if constexpr (kLoads == 2) {
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
-                   "buffer_load_dwordx4 %1, %3, 0 offen lds\n\ts_add_u32 m0, m0, %4\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %2, %3, 0 offen lds" ::
-                   "s"(to), "v"(from[0]), "v"(from[1]), "s"(rsrc), "i"(2048) : "memory", "scc", "m0");
+      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
+                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(2048) : "memory", "scc", "m0");
     } else {
       static_assert(kLoads == 1, "64, 128 or 256");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(from[0]), "s"(rsrc) : "memory", "scc", "m0");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(from), "s"(rsrc) : "memory", "scc", "m0");
     }
 #pragma clang diagnostic pop
-    if constexpr (COLUMNS) {
-      base += (uint64_t)pitch * kStep;
-      left -= kStep;
-    } else {
-      base += kStep * 2;
-      left -= kStep * 2;
-    }
+    base += COLUMNS ? (uint64_t)pitch * kStep : (uint64_t)(kStep * 2);
+    left -= COLUMNS ? kStep : kStep * 2;
   }
 
   // Group t of 16, half h of a step: a lane's eight of r.
@@ -157,56 +150,53 @@ struct Tile {
     for (int i = 0; i < TI; ++i)
 #pragma unroll
       for (int j = 0; j < TJ; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    vec x[2][TI], y[2][TJ];
-    auto take = [&](int stage, int half) {
+    // A step is kGroups groups of TJ products, one fragment of A each.  A's are read kAhead groups before they are used, B's for the second half during the first; the
+    // stage's last read is then issued kAhead groups before its end, where the barrier stands, and the next stage's first reads run beside the last groups.
+    constexpr int kGroups = 2 * TI, kAhead = 3;
+    vec x[kAhead + 1], y[2][TJ];
+    auto read_a = [&](int stage, int g) { x[g % (kAhead + 1)] = a.template fragment<TYPE>(stage, g / TI, g % TI); };
+    auto read_b = [&](int stage, int half, int j) { y[half][j] = b.template fragment<TYPE>(stage, half, j); };
+    static_assert(kGroups % (kAhead + 1) == 0, "a step begins with the ring's first place");
+    auto step = [&](int stage, int at) {
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) y[half][j] = b.template fragment<TYPE>(stage, half, j);
+      for (int g = 0; g < kGroups; ++g) {
+        if (g == kGroups - kAhead) {
+          // every wave has read the stage, and the next one has arrived for all of them
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          if (at + 2 < steps) {
+            a.load(stage);
+            b.load(stage);
+          }
+        }
+        if (g < kGroups - kAhead) read_a(stage, g + kAhead);
+        else read_a(stage ^ 1, g + kAhead - kGroups);        // behind the last step: what lies there, for nothing
 #pragma unroll
-      for (int i = 0; i < TI; ++i) x[half][i] = a.template fragment<TYPE>(stage, half, i);
-    };
-    auto multiply = [&](int half) {
+        for (int j = 0; j < TJ; ++j) {
+          if (g == j * (TI / 2) / TJ) read_b(stage, 1, j);
+          if (g == kGroups - kAhead + j * 2 / TJ) read_b(stage ^ 1, 0, j);
+        }
 #pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) sum[i][j] = Product<TYPE>::add(x[half][i], y[half][j], sum[i][j]);
-    };
-    // LDS reads between products, so that neither waits for a row of the other
-    auto interleave = [] {
-      constexpr int reads = TI * (A_COLUMNS ? 2 : 1) + TJ * (B_COLUMNS ? 2 : 1);
-#pragma unroll
-      for (int k = 0; k < reads; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, TI * TJ / reads, 0);
+        for (int j = 0; j < TJ; ++j) sum[g % TI][j] = Product<TYPE>::add(x[g % (kAhead + 1)], y[g / TI][j], sum[g % TI][j]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, TI * TJ - TI * TJ / reads * reads, 0);
     };
     a.load(0);
     b.load(0);
     if (steps > 1) {
       a.load(1);
       b.load(1);
-      if constexpr (Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-      else if constexpr (Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+      constexpr int loads = Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads;
+      if constexpr (loads == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+      else if constexpr (loads == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
       else asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     asm volatile("s_barrier" ::: "memory");
-    take(0, 0);
-    auto step = [&](int stage, int at) {
-      take(stage, 1);
-      multiply(0);
-      interleave();
-      // every wave has read the stage, and the next one has arrived for all of them
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (at + 2 < steps) {
-        a.load(stage);
-        b.load(stage);
-      }
-      take(stage ^ 1, 0);                  // behind the last step: what lies there, for nothing
-      multiply(1);
-      interleave();
-    };
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) read_b(0, 0, j);
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) read_a(0, g);
     int at = 0;
     for (; at + 1 < steps; at += 2) {
       step(0, at);
@@ -216,12 +206,12 @@ struct Tile {
   }
 };
 
-// Workgroup -> tile.  Workgroups are dealt out to the 8 XCDs in turn: each gets a run of tiles of its own, in columns of four, so that the 32 tiles that its CUs work on
-// share 4 + 8 operands in its L2.
+// Workgroup -> tile.  Workgroups are dealt out to the 8 XCDs in turn: each gets a run of tiles of its own, in columns of eight, so that the 32 tiles that its CUs work on
+// share 8 + 4 operands in its L2.
 __device__ __forceinline__ void tile_of(int id, int tiles_i, int tiles_j, int& i, int& j) {
   const int all = tiles_i * tiles_j, each = all / 8, more = all % 8, xcd = id % 8, at = id / 8;
   const int n = xcd * each + min(xcd, more) + at;            // xcd < more have one more
-  const int band = n / (4 * tiles_j), first = band * 4, high = min(4, tiles_i - first), within = n - band * 4 * tiles_j;
+  const int band = n / (8 * tiles_j), first = band * 8, high = min(8, tiles_i - first), within = n - band * 8 * tiles_j;
   j = within / high;
   i = first + within % high;
 }
