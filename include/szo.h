@@ -426,18 +426,18 @@ int szo_attn_plan(const szo_attn_desc* desc /* host */, int32_t* plan /* host, 4
 
 /* The same attention for sequences that share prefixes: candidate answers behind one prompt, continuations of one, questions behind the same examples.
  * Sequences group_start[g] to group_start[g + 1] - 1 form a group, and the first shared[g] tokens of every one of them are the same, on the pages that the page
- * table names for them all (or on copies: those of the group's first sequence are read).  Rows of all of a group's sequences go over the shared blocks together, so that these
- * are read once for the group, each sequence's rows over its own, and both are joined; the result is that of szo_attn_cached up to the order of sums.  Of
+ * table names for them all (or on copies: those of the group's first sequence are read).  Tiles of 32 rows (tokens times query heads of a key head) of a group's sequences go
+ * over the shared blocks together and then over each one's own; the result is that of szo_attn_cached up to the order of sums.  Of
  * shared[g] whole blocks of 32 tokens count, max_shared tokens at most; tokens behind a sequence's length and masked ones have no influence here either.  Sequences
- * of no group, and those of a group whose rows do not fit max_sequences times max_q tokens, are computed by themselves. */
+ * of no group share nothing. */
 typedef struct szo_attn_groups {
-  int32_t groups, max_sequences;/* most sequences of a group                                             */
+  int32_t groups, max_sequences;/* most sequences of a group: a hint                                     */
   int32_t max_shared, reserved; /* most shared tokens                                                    */
   const int32_t* group_start;   /* device [groups + 1], ascending from 0 to sequences                    */
   const int32_t* shared;        /* device [groups]                                                       */
 } szo_attn_groups;
 /* workspace: device, szo_attn_shared_workspace_bytes(desc, groups) for this very pair, 16-byte aligned, for this call alone while it runs.  SZO_EUNSUPPORTED as for
- * szo_attn_cached, and beyond 2^23 workgroups: tiles of 32 rows of a group times groups and parts, and of a sequence times sequences and parts, times key heads. */
+ * szo_attn_cached, for more than 2^30 rows (tokens times query heads of a key head), and beyond 2^23 - 1 tiles times parts and key heads. */
 int szo_attn_shared(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */, void* workspace, void* stream);
 size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */);
 

@@ -25,6 +25,7 @@ namespace {
 constexpr int kThreads = 256;              // of the joining kernel
 constexpr int64_t kMostGroups = 0xFFFFFFFFll / 512;      // a launch counts its threads in 32 bits
 constexpr float kNone = -3.402823466e38f;  // running maximum of a row that has seen nothing: the lowest finite value, so that differences stay defined
+constexpr float kAbsent = __builtin_inff();      // in place of a maximum: a tile's row that is nobody's
 constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
 constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
 // The denominator is held times 2^40 beside that.  Its largest term is the one of the block with exponent e that sets the maximum, 2^(51 - e), from 2^-73 (with the slack)
@@ -43,15 +44,24 @@ struct AttnArgs {
   bool vec_q, vec_out;
 };
 
-// Sequences that share a prefix (szo_attn_shared).  Two kinds of units of work: tiles of rows of all of a group's sequences over parts of the shared blocks, and
-// tiles of a sequence's rows over parts of its own.  Both leave partial sums.
+// floor(v / d) for 0 <= v < 2^31: with 2^(l - 1) < d <= 2^l and m = ceil(2^(31 + l) / d) it is v m / 2^(31 + l), exactly.
+struct Divisor {
+  uint32_t m;
+  int l;
+  __device__ __forceinline__ int of(int v) const { return (int)(__umulhi(2u * (uint32_t)v, m) >> l); }
+};
+Divisor divisor(int64_t d) {
+  int l = 0;
+  while (((int64_t)1 << l) < d) ++l;
+  return {(uint32_t)((((uint64_t)1 << (31 + l)) + (uint64_t)d - 1) / (uint64_t)d), l};
+}
+
+// Sequences that share a prefix (szo_attn_shared): tiles of 32 rows of a group's sequences go over the blocks that these share, and then over each one's own.
 struct SharedArgs {
   const int32_t *group_start, *shared;
   int groups, most_blocks;                 // most shared blocks
-  int tiles, wave_tiles, splits, rows_cap; // of the shared blocks: workgroups side by side over a group's rows, their waves, parts, rows kept per wave tile
-  int rows;                                // of a group that there are places for
-  int units, first_unit;                   // units of the shared blocks: tiles of all groups times parts; unit of the launch's first workgroups
-  int64_t own_at;                          // floats before the partial sums of sequences' own blocks
+  int tiles, splits;                       // tiles of rows, with and without any; parts of a tile's blocks
+  Divisor by_group, by_page;               // by query heads of a key head, by blocks of a page
 };
 
 // A part's sums: rows_cap rows of head_dim numerators, then maximum (two floats) and denominator of each.  A multiple of 16 bytes, which rows are stored
@@ -207,7 +217,7 @@ template <int TYPE, int D, int WK>
 __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D / 32], float m, float m_exp, float l, int sequence, int head, int64_t tiles, int wave_tile, int split,
                                         int walker, int token, int q_head, int column, int half) {
   const szo_attn_desc& d = a.d;
-  if (a.splits > 1) {
+  if (a.splits > 1) {                                     // not with SHARED, which has parts of its own
     put_part<D, WK>(a.partial + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles + wave_tile) * a.splits + split) * part_floats(a.rows_cap, D), a.rows_cap, o, m, m_exp, l,
                     walker, column, half);
     return;
@@ -227,39 +237,117 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
   if (d.lse && half == 0 && walker == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, m_exp, l);
 }
 
-// The group that a sequence is of, and what it shares.  Every lane of the wave asks for one and the same sequence.
-struct GroupOf {
-  int index, first, blocks;                // its number, its first sequence; blocks of 32 tokens that are shared, 0: none
-  int start;                               // first token of its first sequence
-  __device__ __forceinline__ GroupOf(const SharedArgs& sh, const AttnArgs& a, const int32_t* q_start, int sequence, int lane) : index(0), first(0), blocks(0), start(0) {
-    for (int k = 0; k < sh.groups; k += 64) {
-      const bool in = k + lane < sh.groups;
-      const int from = in ? sh.group_start[k + lane] : 0, to = in ? sh.group_start[k + lane + 1] : 0x7FFFFFFF, tokens = in ? sh.shared[k + lane] : 0;
-      const uint64_t before = __ballot(to <= sequence);
-      if (before == ~0ull) continue;
-      const int c = __popcll(before);      // ends ascend, so these are the first ones
-      index = k + c;
-      first = __builtin_amdgcn_readlane(from, c);
-      blocks = shared_blocks(sh, a, __builtin_amdgcn_readlane(tokens, c));
-      if (k + c >= sh.groups || first < 0 || first > sequence) blocks = 0;
-      break;
+// The batch's starts and lengths, lane by lane, where they fit: what is looked up in them needs no round trip to memory then.
+struct Batch {
+  int first, stop, length;                 // first token; lane i: token behind sequence i, its length
+  bool fits;
+  __device__ __forceinline__ Batch(const AttnArgs& a, const int32_t* q_start, const int32_t* lengths, int lane) : first(0), stop(0), length(0) {
+    const int sequences = a.d.cache.sequences;
+    fits = sequences <= 64;
+    if (fits) {
+      first = clamped(a, q_start[0]);
+      stop = clamped(a, q_start[min(lane, sequences - 1) + 1]);
+      if (lengths) length = lengths[min(lane, sequences - 1)];
     }
-    if (blocks) start = max(q_start[first], 0);
   }
-  // Whole blocks among the first `tokens` that the page table has room for.
-  static __device__ __forceinline__ int shared_blocks(const SharedArgs& sh, const AttnArgs& a, int tokens) {
-    return a.d.cache.pages == 0 ? 0 : (int)min((int64_t)min(max(tokens, 0) / kKvBlock, sh.most_blocks), (int64_t)a.d.cache.max_pages * a.blocks_per_page);
+  static __device__ __forceinline__ int clamped(const AttnArgs& a, int at) { return max((int)min((int64_t)at, a.d.tokens), 0); }
+  __device__ __forceinline__ int start_of(const AttnArgs& a, const int32_t* q_start, int sequence) const {
+    if (!fits) return clamped(a, q_start[sequence]);
+    const int before = __shfl(stop, max(sequence - 1, 0));
+    return sequence ? before : first;
+  }
+  __device__ __forceinline__ int length_of(const int32_t* lengths, int sequence) const { return fits ? __shfl(length, sequence) : lengths[sequence]; }
+};
+
+// Which rows a tile has.  Tiles go through the groups one after the other, and through what lies before the first and behind the last one as groups that share nothing: with
+// group e of these (0: before the first) beginning at row r, its tiles are r / 32 + e and following, which leaves room for the last, partly filled one of each.
+struct GroupTile {
+  int first, last;                         // the group's sequences; first == last: no rows
+  int start, rows, first_row;              // its first token, its rows, the tile's first row among them
+  int blocks;                              // that its sequences share
+  __device__ __forceinline__ GroupTile(const SharedArgs& sh, const AttnArgs& a, const Batch& batch, const int32_t* q_start, int tile, int lane)
+      : first(0), last(0), start(0), rows(0), first_row(0), blocks(0) {
+    int e = -1, tokens = 0, stop = 0;
+    for (int k = 0;; k += 64) {
+      const int i = k + lane;
+      const int sequence = i == 0 ? 0 : i <= sh.groups + 1 ? min(max(sh.group_start[i - 1], 0), a.d.cache.sequences) : a.d.cache.sequences;
+      const int at = batch.start_of(a, q_start, sequence);
+      const int common = i >= 1 && i <= sh.groups ? sh.shared[i - 1] : 0;
+      const int c = __popcll(__ballot(i <= sh.groups + 1 && at * a.group / 32 + i <= tile));            // they ascend: the first c
+      if (c > 0) {
+        e = k + c - 1;
+        first = __builtin_amdgcn_readlane(sequence, c - 1);
+        start = __builtin_amdgcn_readlane(at, c - 1);
+        tokens = __builtin_amdgcn_readlane(common, c - 1);
+      }
+      if (c < 64) {
+        last = __builtin_amdgcn_readlane(sequence, c);
+        stop = __builtin_amdgcn_readlane(at, c);
+        break;
+      }
+    }
+    if (e < 0) { last = first; return; }
+    rows = max(stop - start, 0) * a.group;
+    first_row = (tile - (start * a.group / 32 + e)) * 32;
+    blocks = a.d.cache.pages == 0 ? 0 : (int)min((int64_t)min(max(tokens, 0) / kKvBlock, sh.most_blocks), (int64_t)a.d.cache.max_pages * a.blocks_per_page);
+  }
+  __device__ __forceinline__ bool empty() const { return first >= last || first_row >= rows; }
+};
+
+// What a tile goes over: the shared blocks (slot -1), then the own ones of each sequence that has rows in it; lane k has those of slot k.
+struct Segments {
+  int shared_first, shared_count, sequence;          // the shared ones, read by the page table's row of this sequence
+  int own_sequence, own_first, own_count, own_page;  // this lane's slot; where the first of its blocks lies, so that entering a segment waits for no page table
+  __device__ __forceinline__ int count(int slot) const { return slot < 0 ? shared_count : __builtin_amdgcn_readlane(own_count, slot); }
+};
+struct SegmentWalk {
+  int slot, left, block, page_at, sub, per_page;     // blocks of the segment from this one on, the block's number in its sequence and where it lies
+  bool entered;                                      // at a slot's first block
+  const int32_t* table;
+  __device__ __forceinline__ void enter(const Segments& g, int at, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    int n = g.count(slot);
+    while (at >= n) { at -= n; n = g.count(++slot); }          // blocks asked for are there
+    left = n - at;
+    block = (slot < 0 ? g.shared_first : __builtin_amdgcn_readlane(g.own_first, slot)) + at;
+    table = page_table + (int64_t)(slot < 0 ? g.sequence : __builtin_amdgcn_readlane(g.own_sequence, slot)) * max_pages;
+    page_at = by_page.of(block);
+    sub = block - page_at * per_page;
+    entered = slot >= 0 && at == 0;
+  }
+  __device__ __forceinline__ void step(const Segments& g, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    entered = false;
+    if (--left > 0) {
+      ++block;
+      if (++sub == per_page) { sub = 0; ++page_at; }
+    } else {
+      ++slot;
+      enter(g, 0, page_table, max_pages, by_page);
+    }
+  }
+  __device__ __forceinline__ int at(const Segments& g, const szo_kv_cache& c, int head) const {
+    const int page = entered ? __builtin_amdgcn_readlane(g.own_page, slot) : table[page_at];
+    return (uint32_t)page >= (uint32_t)c.pages ? -1 : (page * c.kv_heads + head) * per_page + sub;
   }
 };
-// Whether the rows of a sequence that ends before token `stop` have places in the tiles of its group's shared blocks; else it goes over all of its blocks itself.
-__device__ __forceinline__ bool covered(const SharedArgs& sh, const AttnArgs& a, const GroupOf& g, int stop) {
-  return g.blocks > 0 && (int64_t)(stop - g.start) * a.group <= sh.rows;
-}
 
-__device__ __forceinline__ int wave_min(int v) {
-  for (int by = 32; by; by /= 2) v = min(v, __shfl_xor(v, by));
-  return v;
+// A value of all lanes: largest, sum.
+template <int CTRL> __device__ __forceinline__ int lane_permuted(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false); }
+template <typename F>
+__device__ __forceinline__ int wave_of(int v, F f) {
+  v = f(v, lane_permuted<0xB1>(v));
+  v = f(v, lane_permuted<0x4E>(v));
+  v = f(v, lane_permuted<0x141>(v));
+  v = f(v, lane_permuted<0x140>(v));
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto s = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = f((int)s[0], (int)s[1]);
+  s = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = f((int)s[0], (int)s[1]);
+#endif
+  return uniform(v);
 }
+__device__ __forceinline__ int wave_max(int v) { return wave_of(v, [](int a, int b) { return max(a, b); }); }
+__device__ __forceinline__ int wave_add(int v) { return wave_of(v, [](int a, int b) { return a + b; }); }
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
 //   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
@@ -269,119 +357,135 @@ __device__ __forceinline__ int wave_min(int v) {
 //   A prompt of 8192 tokens with 32 query and 8 key heads of 128, causal: 577 us, 953 TFLOP/s, bound by the issue of instructions: matrix products take 44 % of
 // the cycles, and a step has 186 vector instructions beside 16 products.  One token of each of 64 sequences of up to 8192: 108 us, 5.73 TB/s of the cache.
 // 4096 tokens in bf16 with head dimensions of 64, 96, 128, 256: 124, 138, 168, 393 us (556, 748, 820, 699 TFLOP/s), in fp16 110, 140, 166, 383.
-//   SHARED: units of work of sequences that share prefixes, one after the other with the key heads side by side; what a unit's rows are and which blocks they go over
-// is all that differs.
+//   SHARED: a tile has rows of several sequences of a group, and goes over the blocks that these share and then over each one's own, where the others' rows are masked.
 template <int TYPE, int D, int WR, int WK, bool ONCE, bool SHARED>
 __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t* lengths, const int32_t* page_table, int max_pages, int bpp, int splits, int tiles,
                                           const AttnArgs& a, const SharedArgs& sh) {
   constexpr int E = D / 32;
   const szo_attn_desc& d = a.d;
   const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), column = lane % 32, half = lane / 32;
-  // key heads vary fastest: workgroups are dealt out to the 8 XCDs in turn, so the row tiles of one key head share an L2
-  int head = blockIdx.x, sequence = blockIdx.z, split, tile;
-  int unit = 0;
-  bool together = false;                   // SHARED: rows of a whole group over its shared blocks
-  if constexpr (SHARED) {
-    const int at = blockIdx.x / d.cache.kv_heads;
-    head = blockIdx.x - at * d.cache.kv_heads;
-    unit = sh.first_unit + at;
-    together = unit < sh.units;
-    const int parts = together ? sh.splits : splits, per = (together ? sh.tiles : tiles) * parts, within = together ? unit : unit - sh.units;
-    sequence = within / per;               // the group, for now, if together
-    tile = (within - sequence * per) / parts;
-    split = within - sequence * per - tile * parts;
-    splits = parts;
-  } else {
-    split = splits == 1 ? 0 : blockIdx.y % splits;
-    tile = tiles - 1 - (splits == 1 ? blockIdx.y : blockIdx.y / splits);          // later rows see more: they start first
-  }
-  const int wave_tile = tile * WR + wave % WR, walker = WK == 1 ? 0 : wave / WR, first_row = wave_tile * 32, row = first_row + column;
+  // What a wave's rows are and which blocks they go over.
+  int head, sequence = 0, split, wave_tile, start, query, q_head, see_to, see_from, see_all, see_all_from, j0, j1, guess = -1;
+  bool valid;
+  const int32_t* table = nullptr;
+  Query<TYPE, D> q;
+  int my_slot = -1, slots = 1;             // SHARED: of this lane's row, of the tile
+  Segments segments = {};
+  const int walker = WK == 1 ? 0 : wave / WR;
   // First position of the window of a query at `position`: 0 where the window is wider; no difference leaves 32 bits.  What a wave has in common is kept in scalar
   // registers (a prompt of 8192 636 us otherwise, 577 so).
   auto window_from = [&](int position) { return d.window > 0 ? max(position + 1, d.window) - d.window : 0; };
-  const int32_t* table;
-  float* part = nullptr;
-  int guess = -1, start, query, q_head, see_to, see_from, see_all, see_all_from, lo, hi;
-  bool valid;
-  Query<TYPE, D> q;
-  if (SHARED && together) {
-    const int group = sequence, first = max(sh.group_start[group], 0), last = min(sh.group_start[group + 1], d.cache.sequences);
-    const int blocks = GroupOf::shared_blocks(sh, a, sh.shared[group]);
-    if (first >= last || blocks == 0) return;
-    table = page_table + (int64_t)first * max_pages;
-    start = max(q_start[first], 0);
-    const int stop = max((int)min((int64_t)q_start[last], d.tokens), 0);
-    const int rows = (int)min((int64_t)max(stop - start, 0) * a.group, (int64_t)sh.rows);
-    if (tile * WR * 32 >= rows) return;                  // the workgroup as a whole
-    // the sequence of this lane's row: those of the tile's tokens are gone through one by one
-    const int token = start + row / a.group, token_first = start + first_row / a.group, token_last = start + (min(first_row + 32, rows) - 1) / a.group;
-    int own_start = 0, own_stop = 0, whole = 0;
-    bool found = false, done = false;
-    for (int k = first; k < last && !done; k += 64) {
-      const int i = k + lane;
-      const int from = i < last ? q_start[i] : 0x7FFFFFFF, to = i < last ? max((int)min((int64_t)q_start[i + 1], d.tokens), 0) : 0x7FFFFFFF;
-      const int tokens = i < last ? lengths[i] : 0;
-      const uint64_t before = __ballot(to <= token_first);
-      if (before == ~0ull) continue;
-      for (int c = __popcll(before); c < 64 && !done; ++c) {
-        const int from_c = max(__builtin_amdgcn_readlane(from, c), 0), to_c = __builtin_amdgcn_readlane(to, c);
-        done = from_c > token_last;
-        const bool mine = !done && token >= from_c && token < to_c;
-        own_start = mine ? from_c : own_start;
-        own_stop = mine ? to_c : own_stop;
-        whole = mine ? __builtin_amdgcn_readlane(tokens, c) : whole;
-        found |= mine;
-      }
-    }
-    query = token - own_start;
-    q_head = head * a.group + row % a.group;
-    valid = row < rows && found && query < d.max_q;
-    const int behind = max(whole, 0) - (own_stop - own_start);
-    const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
-    see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
-    see_from = window_from(behind + query);
-    start = own_start;
-    const int reach = -wave_min(valid ? -see_to : 0);
-    lo = uniform(wave_min(valid ? see_from : 0x7FFFFFFF)) / kKvBlock;
-    hi = uniform(min(blocks, reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0));
-    see_all = uniform(wave_min(valid ? see_to : 0x7FFFFFFF));
-    see_all_from = uniform(-wave_min(valid ? -see_from : 0));
-    part = a.partial + ((((int64_t)group * d.cache.kv_heads + head) * sh.wave_tiles + wave_tile) * splits + split) * part_floats(sh.rows_cap, D);
-    q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
-  } else {
+  if constexpr (!SHARED) {
+    // key heads vary fastest: workgroups are dealt out to the 8 XCDs in turn, so the row tiles of one key head share an L2
+    head = blockIdx.x, sequence = blockIdx.z;
+    split = splits == 1 ? 0 : blockIdx.y % splits;
+    const int tile = tiles - 1 - (splits == 1 ? blockIdx.y : blockIdx.y / splits);          // later rows see more: they start first
+    wave_tile = tile * WR + wave % WR;
     table = page_table + (int64_t)sequence * max_pages;
     const int whole = lengths[sequence];
-    if constexpr (!SHARED) guess = max_pages > walker / bpp ? table[walker / bpp] : -1;
+    guess = max_pages > walker / bpp ? table[walker / bpp] : -1;
     start = max(q_start[sequence], 0);
     const int stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);      // differences of both fit
     const int n = max(0, min(stop - start, d.max_q));
     const int length = (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
-    const int rows = n * a.group;
+    const int rows = n * a.group, first_row = wave_tile * 32;
     if (tile * WR * 32 >= rows) return;                    // the workgroup as a whole
     const int behind = max(whole, 0) - (stop - start);     // position of the sequence's first query
 
     // this lane's row
+    const int row = first_row + column;
     query = row / a.group, q_head = head * a.group + row % a.group;
     valid = row < rows;
     see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
     see_from = window_from(behind + query);
     q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
 
-    // blocks that some row of the wave sees
+    // blocks that some row of the wave sees, the part of them that is this split's, and this wave's share of that
     const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
     const int reach = first_row >= rows || d.cache.pages == 0 ? 0 : d.causal ? min(length, pos_last + 1) : length;
-    lo = uniform(window_from(pos_first)) / kKvBlock, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
+    const int lo = uniform(window_from(pos_first)) / kKvBlock, hi = reach > 0 ? (reach + kKvBlock - 1) / kKvBlock : 0;
+    const int share = splits == 1 ? max(hi - lo, 0) : (max(hi - lo, 0) + splits - 1) / splits;
+    j0 = lo + split * share + walker, j1 = min(hi, lo + (split + 1) * share);
     see_all = d.causal ? min(length, pos_first + 1) : length;     // tokens before this one are seen by every row, but for the window
     see_all_from = uniform(window_from(pos_last));
-    if constexpr (SHARED) {
-      const GroupOf g(sh, a, q_start, sequence, lane);
-      if (covered(sh, a, g, stop)) lo = max(lo, uniform(g.blocks));
-      part = a.partial + sh.own_at + ((((int64_t)sequence * d.cache.kv_heads + head) * tiles * WR + wave_tile) * splits + split) * part_floats(a.rows_cap, D);
+  } else {
+    const int unit = blockIdx.x / d.cache.kv_heads;
+    head = blockIdx.x - unit * d.cache.kv_heads;
+    const int tile = unit / splits;
+    split = unit - tile * splits;
+    wave_tile = tile * WR + wave % WR;
+    const Batch batch(a, q_start, lengths, lane);
+    const GroupTile g(sh, a, batch, q_start, wave_tile, lane);
+    if (g.empty()) return;                                 // all waves that meet have the same tile
+    const int row = g.first_row + column, of_start = sh.by_group.of(row), token = g.start + of_start;
+    const int token_first = g.start + sh.by_group.of(g.first_row), token_last = g.start + sh.by_group.of(min(g.first_row + 32, g.rows) - 1);
+    q_head = head * a.group + row - of_start * a.group;
+    q.load(d.q, (int64_t)token * d.q_token_stride + (int64_t)q_head * d.q_head_stride, row < g.rows, a.vec_q, a.negate, half);
+    // The sequences that have rows in the tile, 64 side by side; those that have go to slots, one lane each (at most 32, since each has a token).
+    int slot_start = 0, slot_last = 0, slot_behind = 0, slot_length = 0;       // this lane's slot: first token, last query that counts, position of the first one, length
+    int reach = 0, first_seen = -0x7FFFFFFF, all_to = -0x7FFFFFFF, all_from = 0;      // of all slots: largest, and smallest with the sign changed
+    uint64_t begins = 0;                                                      // columns at which a slot begins
+    slots = 0;
+    for (int k = g.first; k < g.last; k += 64) {
+      const bool in = k + lane < g.last;
+      const int i = min(k + lane, g.last - 1);
+      const int from = batch.start_of(a, q_start, i), to = batch.start_of(a, q_start, i + 1), whole = batch.length_of(lengths, i);
+      bool mine = in && to > from && to > token_first && from <= token_last;
+      const uint64_t mask = __ballot(mine);
+      const int place = slots + __popcll(mask & ((1ull << lane) - 1));
+      mine = mine && place < 32;
+      const int query_first = max(token_first, from) - from, query_last = min(min(token_last, to - 1) - from, d.max_q - 1);
+      const int behind = max(whole, 0) - (to - from);
+      const int length = d.cache.pages == 0 ? 0 : (int)max((int64_t)0, min((int64_t)whole, (int64_t)max_pages * bpp * kKvBlock));
+      const int see_last = d.causal ? min(length, behind + query_last + 1) : length, window = window_from(behind + query_first);
+      const int own_first = max(g.blocks, window / kKvBlock);
+      const bool some = mine && query_first <= query_last;                    // not all of them left out
+      const int own_count = some && see_last > 0 ? max((see_last + kKvBlock - 1) / kKvBlock - own_first, 0) : 0;
+      if (some) {
+        reach = max(reach, see_last);
+        first_seen = max(first_seen, -window);
+        all_to = max(all_to, -(d.causal ? min(length, behind + query_first + 1) : length));
+        all_from = max(all_from, window_from(behind + query_last));
+      }
+      // to the slots' lanes; lanes without one send to a lane that has none
+      const int to_lane = 4 * (mine ? place : 63), here = __popcll(mask);
+      const bool taken = lane >= slots && lane < slots + here;
+      auto put = [&](int& at, int v) {
+        const int got = __builtin_amdgcn_ds_permute(to_lane, v);
+        at = taken ? got : at;
+      };
+      put(segments.own_sequence, i);
+      put(segments.own_first, own_first);
+      put(segments.own_count, own_count);
+      put(slot_start, from);
+      put(slot_last, query_last);
+      put(slot_behind, behind);
+      put(slot_length, length);
+      begins |= __ballot(__builtin_amdgcn_ds_permute(4 * (mine ? max((from - g.start) * a.group - g.first_row, 0) : 63), mine ? 1 : 0) == 1);
+      slots = min(slots + here, 32);
+      if (__any(in && from > token_last)) break;
     }
+    const int at = max(__popcll(begins & ((2ull << column) - 1)) - 1, 0);
+    start = __shfl(slot_start, at);
+    query = token - start;
+    const int length = __shfl(slot_length, at), position = __shfl(slot_behind, at) + query;
+    valid = slots > 0 && row < g.rows && query >= 0 && query <= __shfl(slot_last, at);
+    my_slot = at;
+    see_to = !valid ? 0 : d.causal ? min(length, position + 1) : length;
+    see_from = window_from(position);
+    reach = wave_max(reach);
+    see_all = -wave_max(all_to);
+    see_all_from = wave_max(all_from);
+    segments.own_page = lane < slots && segments.own_count > 0 ? page_table[(int64_t)segments.own_sequence * max_pages + sh.by_page.of(segments.own_first)] : -1;
+    segments.sequence = g.first;
+    segments.shared_first = -wave_max(first_seen) / kKvBlock;
+    segments.shared_count = max(min(g.blocks, (reach + kKvBlock - 1) / kKvBlock) - segments.shared_first, 0);
+    // a walker's blocks follow each other, so that it enters few segments
+    const int total = segments.shared_count + wave_add(lane < slots ? segments.own_count : 0);
+    const int share = (total + splits - 1) / splits, each = (share + WK - 1) / WK;
+    j0 = split * share + walker * each, j1 = min(min(total, (split + 1) * share), j0 + each);
   }
-  // the part of the blocks that is this split's, and this wave's share of that
-  const int share = splits == 1 ? max(hi - lo, 0) : (max(hi - lo, 0) + splits - 1) / splits;
-  const int j0 = lo + split * share + walker, j1 = min(hi, lo + (split + 1) * share);
+  constexpr int kNext = SHARED ? 1 : WK;   // from one of a walker's blocks to the next
 
   f32x16 o[E], s = {};
   float m = kNone, m_exp = 0.f, l = 0.f;
@@ -392,9 +496,24 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
 
   if (j0 < j1) {
     // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
-    Walk walk(j0, bpp);
-    int now = !SHARED && j0 == walker ? walk.on(d.cache, guess, head, bpp) : walk.at(d.cache, table, head, bpp), next = now;
-    if (j0 + WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+    Walk walk(SHARED ? 0 : j0, bpp);
+    SegmentWalk piece = {-1, 0, 0, 0, 0, bpp, false, nullptr};
+    int now, next, block_now = 0, slot_now = -1, block_next = 0, slot_next = -1;
+    if constexpr (SHARED) {
+      piece.enter(segments, j0, page_table, max_pages, sh.by_page);
+      now = next = piece.at(segments, d.cache, head);
+      block_now = block_next = piece.block;
+      slot_now = slot_next = piece.slot;
+      if (j0 + kNext < j1) {
+        piece.step(segments, page_table, max_pages, sh.by_page);
+        next = piece.at(segments, d.cache, head);
+        block_next = piece.block;
+        slot_next = piece.slot;
+      }
+    } else {
+      now = j0 == walker ? walk.on(d.cache, guess, head, bpp) : walk.at(d.cache, table, head, bpp), next = now;
+      if (j0 + WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+    }
     auto known = [](int b) { return max(b, 0); };
     auto scores = [&](const Raw<D>& k) {
       s = f32x16{};
@@ -408,10 +527,22 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     int ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)], most_vexp = kExpMin;
     scores(k);
     k = load_block<D, ONCE>(d.cache.k, known(next), lane);
-    for (int j = j0; j < j1; j += WK) {        // k: keys of the next step, v: values of this one
+    for (int j = j0; j < j1; j += kNext) {        // k: keys of the next step, v: values of this one
       const bool there = now >= 0;
+      const int block = SHARED ? block_now : j, slot = slot_now;
       now = next;
-      if (j + 2 * WK < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+      if constexpr (SHARED) {
+        block_now = block_next;
+        slot_now = slot_next;
+        if (j + 2 * kNext < j1) {
+          piece.step(segments, page_table, max_pages, sh.by_page);
+          next = piece.at(segments, d.cache, head);
+          block_next = piece.block;
+          slot_next = piece.slot;
+        }
+      } else {
+        if (j + 2 * kNext < j1) { walk.step(WK, bpp); next = walk.at(d.cache, table, head, bpp); }
+      }
       float factor = score_factor(a.to_log2, ke);
       const int vexp = uniform(min(max(ve - kExpBias, kExpMin), kExpMax));
       const float shift = (float)vexp;
@@ -419,8 +550,9 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
       most_vexp = max(most_vexp, vexp);
       const bool apart = most_vexp - vexp > kApart;
       ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)];
-      const int token = j * kKvBlock + 4 * half, to = there ? see_to - token : 0, from = see_from - token;      // of s[0]; s[i] is 8 (i / 4) + i % 4 further
-      const bool all = there && (j + 1) * kKvBlock <= see_all && j * kKvBlock >= see_all_from;
+      const bool here = there && (!SHARED || slot < 0 || slot == my_slot);        // another sequence's block is masked as a whole
+      const int token = block * kKvBlock + 4 * half, to = here ? see_to - token : 0, from = see_from - token;      // of s[0]; s[i] is 8 (i / 4) + i % 4 further
+      const bool all = there && (!SHARED || slot < 0 || slots == 1) && (block + 1) * kKvBlock <= see_all && block * kKvBlock >= see_all_from;
       if (!all) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -509,8 +641,8 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
       for (int e = 0; e < E; ++e) o[e] = product(halves(v.w[e].x, v.w[e].y), p[0], o[e]);
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = product(halves(v.w[e].z, v.w[e].w), p[1], o[e]);
-      if (WK == 1 || j + WK < j1) v = load_block<D, ONCE>(d.cache.v, known(now), lane);
-      if (WK > 1 && j + 2 * WK < j1) k = load_block<D, ONCE>(d.cache.k, known(next), lane);
+      if (WK == 1 || j + kNext < j1) v = load_block<D, ONCE>(d.cache.v, known(now), lane);
+      if (WK > 1 && j + 2 * kNext < j1) k = load_block<D, ONCE>(d.cache.k, known(next), lane);
     }
   }
 
@@ -584,10 +716,14 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     }
   }
   if constexpr (SHARED) {
-    if (valid) put_part<D, WK>(part, together ? sh.rows_cap : a.rows_cap, o, m, m_exp, l, walker, column, half);
-  } else {
-    if (valid) put_row<TYPE, D, WK>(a, o, m, m_exp, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
+    if (splits > 1) {
+      float* part = a.partial + (((int64_t)wave_tile * d.cache.kv_heads + head) * splits + split) * part_floats(32, D);
+      if (valid) put_part<D, WK>(part, 32, o, m, m_exp, l, walker, column, half);
+      else if (half == 0 && walker == 0) part[32 * D + 3 * column] = kAbsent;
+      return;
+    }
   }
+  if (valid) put_row<TYPE, D, WK>(a, o, m, m_exp, l, sequence, head, (int64_t)a.tiles * WR, wave_tile, split, walker, start + query, q_head, column, half);
 }
 
 template <int TYPE, int D, int WR, int WK, bool ONCE>
@@ -604,38 +740,36 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_shared_ke
 // Joins the parts of a row, four features of it at a time, by G neighbouring lanes: each takes every G-th part and they add each other up by row
 // permutations.  One lane, up to four parts on the way, for up to five parts and for full tiles, 16 lanes otherwise (1 sequence of 8000 in 32 parts 12.4 -> 10.5 us,
 // 32 rows of it in 8 parts 18.7 -> 19.2).  Workgroups go over sequences, key heads, wave tiles and a tile's pieces.
-//   SHARED: the parts of its group's shared blocks come before those of its own.
+//   SHARED: tiles are of groups; a row that is nobody's is marked in the first part.
 template <int TYPE, int D, int G, bool SHARED>
 __device__ __forceinline__ void attn_join(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs& a, const SharedArgs& sh) {
   const szo_attn_desc& d = a.d;
   const int wave_tile = blockIdx.x % wave_tiles, head = blockIdx.y, sequence = blockIdx.z;
-  const float* from = partial + (SHARED ? sh.own_at : 0) + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
-  const int start = max(q_start[sequence], 0), stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
-  const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
-  const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
-  const int column = i / (D / 4), f = i % (D / 4) * 4, row = wave_tile * 32 + column, query = row / a.group, q_head = head * a.group + row % a.group;
-  const float* shared_from = nullptr;
-  int shared_parts = 0, shared_column = 0;
+  const float* from = partial + (SHARED ? (int64_t)wave_tile * gridDim.y + head : ((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
+  int start, rows, first_row = wave_tile * 32;
   if constexpr (SHARED) {
-    const GroupOf g(sh, a, q_start, sequence, threadIdx.x % 64);
-    if (covered(sh, a, g, stop)) {
-      const int place = (start - g.start + query) * a.group + row % a.group;
-      shared_parts = sh.splits;
-      shared_column = place % 32;
-      shared_from = a.partial + (((int64_t)g.index * gridDim.y + head) * sh.wave_tiles + place / 32) * sh.splits * part_floats(sh.rows_cap, D);
-    }
+    const GroupTile t(sh, a, Batch(a, q_start, nullptr, threadIdx.x % 64), q_start, wave_tile, threadIdx.x % 64);
+    if (t.empty()) return;
+    start = t.start;
+    first_row = t.first_row;
+    rows = min(t.rows - first_row, 32);
+  } else {
+    start = max(q_start[sequence], 0);
+    const int stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
+    rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
   }
+  const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
+  const int column = i / (D / 4), f = i % (D / 4) * 4, row = first_row + column, query = SHARED ? sh.by_group.of(row) : row / a.group, q_head = head * a.group + row - query * a.group;
   if (column >= rows) return;                  // G lanes at once
+  if (SHARED && from[(int64_t)rows_cap * D + 3 * column] == kAbsent) return;
   float m = kNone, m_exp = 0.f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int kAhead = G == 1 ? 4 : 2;
 #pragma unroll kAhead
-  for (int s = g; s < splits + shared_parts; s += G) {
-    const bool of_group = SHARED && s < shared_parts;
-    const int cap = of_group ? sh.rows_cap : rows_cap, at = of_group ? shared_column : column;
-    const float* part = of_group ? shared_from + (int64_t)s * part_floats(cap, D) : from + (int64_t)(s - shared_parts) * part_floats(cap, D);
-    const float* stats = part + (int64_t)cap * D + 3 * at;
+  for (int s = g; s < splits; s += G) {
+    const float* part = from + (int64_t)s * part_floats(rows_cap, D);
+    const float* stats = part + (int64_t)rows_cap * D + 3 * column;
     const float ms = stats[0], es = stats[1], ls = stats[2];
-    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)at * D + f);
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
     const float over = (ms - m) + (es - m_exp), keep_half = half_of(fminf(-over, 0.f)), add_half = half_of(fminf(over, 0.f));
     const float keep = keep_half * keep_half, add = add_half * add_half;
     l = fmaf(l * keep_half, keep_half, ls * add_half * add_half);
@@ -788,92 +922,85 @@ int launch_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
 
 // ---- sequences that share a prefix -----------------------------------------------------------------------------------
 
-struct SharedPlan { int rows, wr, tiles, splits, rows_cap, own_tiles, own_splits, own_cap; };
+// How tiles and their blocks go to waves.  Four waves take tiles side by side (wr 4) where the tiles alone fill the chip; else four or eight share a tile's blocks and meet in LDS,
+// and with few tiles the blocks go to several workgroups, joined by a second kernel.  A wave's step takes 1.1 us, bound by the issue of its instructions, and as long beside a second
+// wave on its SIMD; a workgroup takes 4 us to find its rows and to begin, 2 to meet, a join 4 to 6.  So there are two waves a SIMD where the blocks allow: eight waves a
+// workgroup up to 256 tiles, but four where a tile has so few blocks that one of them a wave does not fill the chip.  us, 32 query and 8 key heads of 128 in bf16, parts 1, 2, 4, 8, 16 of four
+// waves / of eight: 64 sequences, one token each, behind 8192 shared ones and up to 500 own (64 tiles, 320 blocks each) 114, 69, 42, 35, 44 / 77, 50, 34, 42, 59; 16 of them
+// (16 tiles) 87, 55, 35, 24, 22 / 63, 42, 29, 22, 22; 256 behind 4 x 2048 (256 tiles, 104 blocks) 52, 43, 53 / 37, 51; 4 behind 1024 (8 tiles, 40 blocks) 14.6, 14.1, 13.7, 12.9,
+// 13.2 / 13.5, 15.8, 12.9, 13.2; answers of 3 to 61 tokens, 32 of them behind 4 x 2500 (976 tiles) 58, 87 / 73; 8 behind 2000 (344 tiles) 28, 40 / 36; 256 behind 8 x 2000 (7440 tiles)
+// 281 / 430, side by side 229.  szo_attn_cached takes 102, 31, 113, 9.9, 74, 27, 358 for these.
+struct SharedPlan { int wr, wk, tiles, splits; };
 
 SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   SharedPlan p;
-  const int64_t group = d->q_heads / d->cache.kv_heads, heads = d->cache.kv_heads;
-  auto blocks_of = [](int64_t tokens) { return (std::max<int64_t>(tokens, 1) + kKvBlock - 1) / kKvBlock; };
-  // rows of all of a group's sequences over the shared blocks
-  const int64_t rows = std::min<int64_t>(d->tokens, (int64_t)d->max_q * g->max_sequences) * group;
-  const int64_t held = std::min<int64_t>(d->tokens * group / 32 + g->groups, g->groups * ((rows + 31) / 32)) * heads;      // tiles that hold something, about
-  const int64_t blocks = blocks_of(d->window > 0 ? std::min<int64_t>(g->max_shared, (int64_t)d->window + d->max_q) : g->max_shared);
-  p.rows = (int)rows;
+  const int64_t group = d->q_heads / d->cache.kv_heads, heads = d->cache.kv_heads, rows = d->tokens * group;
+  const int64_t held = std::max<int64_t>(1, rows / 32) * heads;            // tiles that hold something, about
+  p.tiles = (int)(rows / 32 + g->groups + 2);
   p.wr = held >= 2048 ? 4 : 1;
-  p.tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
-  p.rows_cap = (int)std::min<int64_t>(32, rows);
-  const int64_t most = p.wr == 4 ? 1 : std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(held, 1), (blocks + 7) / 8));
-  p.splits = (int)std::min<int64_t>(most, 64);
-  // a sequence's rows over its own blocks
-  const int64_t own_rows = (int64_t)d->max_q * group, own_held = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((own_rows + 31) / 32)) * heads;
-  const int64_t own_blocks = blocks_of((int64_t)d->max_len - g->max_shared);
-  p.own_tiles = (int)((own_rows + 31) / 32);
-  p.own_cap = (int)std::min<int64_t>(32, own_rows);
-  p.own_splits = (int)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(own_held, 1), (own_blocks + 7) / 8)), 64);
+  // a tile's blocks: the shared ones, and half of the most of each sequence that is in it
+  const int64_t each = std::max<int64_t>(1, rows / d->cache.sequences), sequences = std::min<int64_t>(32, std::max<int64_t>(1, 32 / each));
+  const int64_t own = std::max<int64_t>(0, (int64_t)d->max_len - g->max_shared), blocks = g->max_shared / kKvBlock + sequences * (own / (2 * kKvBlock) + 1);
+  const bool wide = d->cache.head_dim > 128;                // a wave has its SIMD to itself
+  p.wk = p.wr == 4 ? 1 : !wide && held <= 256 && blocks / 8 >= 256 / held ? 8 : 4;
+  const int64_t chip = p.wk == 8 || wide ? 256 : 512;
+  p.splits = p.wr == 4 ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, std::min(chip / held, blocks / p.wk)), 64);
   return p;
 }
 
-// Whether anything is shared at all: else every sequence goes by itself.
-bool shares(const szo_attn_groups* g) { return g->groups > 0 && g->max_sequences > 0 && g->max_shared >= kKvBlock; }
+// Whether sequences go together: else each goes by itself, as szo_attn_cached has it.  They do where anything is shared and the chip's 2048 waves would have more than a block
+// each otherwise: below that nothing is waited for but the round trips that a wave begins with, of which groups have more (4 sequences behind 1024: 12.8 us together, 9.9 apart;
+// 16 behind 1024 12.9 and 14.0).
+bool together(const szo_attn_desc* d, const szo_attn_groups* g) {
+  if (g->groups == 0 || g->max_shared < kKvBlock) return false;
+  const int64_t group = d->q_heads / d->cache.kv_heads, rows = (int64_t)d->max_q * group;
+  const int64_t tiles = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((rows + 31) / 32)) * d->cache.kv_heads;
+  return tiles * ((int64_t)d->max_len / kKvBlock + 1) > 2048;
+}
 
 int check(const szo_attn_desc* d, const szo_attn_groups* g) {
   const int rc = check(d);
   if (rc != SZO_OK) return rc;
   if (!g || g->groups < 0 || g->max_sequences < 0 || g->max_shared < 0 || g->reserved) return SZO_EINVAL;
-  if (nothing(d) || !shares(g)) return SZO_OK;
+  if (nothing(d) || !together(d, g)) return SZO_OK;
   if (!g->group_start || !g->shared || !aligned_to(g->group_start, 4) || !aligned_to(g->shared, 4)) return SZO_EINVAL;
   const szo_kv_cache& c = d->cache;
-  if (std::min<int64_t>(d->tokens, (int64_t)d->max_q * g->max_sequences) * (d->q_heads / c.kv_heads) > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
+  if (d->tokens * (d->q_heads / c.kv_heads) > 0x3FFFFFFF || g->groups > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
   const SharedPlan p = plan_of(d, g);
-  const int64_t units = (int64_t)g->groups * p.tiles * p.splits, own = (int64_t)c.sequences * p.own_tiles * p.own_splits;
-  if ((units + own) * c.kv_heads > kMostGroups || (int64_t)p.own_tiles * 64 > 0x7FFFFFFF || c.sequences > 65535) return SZO_EUNSUPPORTED;
+  if ((int64_t)p.tiles * p.splits * c.kv_heads > kMostGroups) return SZO_EUNSUPPORTED;
   return SZO_OK;
 }
 
-size_t shared_floats(const szo_attn_desc* d, const szo_attn_groups* g, const SharedPlan& p) {
-  return (size_t)g->groups * d->cache.kv_heads * p.tiles * p.wr * p.splits * part_floats(p.rows_cap, d->cache.head_dim);
-}
-size_t own_floats(const szo_attn_desc* d, const SharedPlan& p) {
-  return (size_t)d->cache.sequences * d->cache.kv_heads * p.own_tiles * p.own_splits * part_floats(p.own_cap, d->cache.head_dim);
-}
-
 template <int TYPE, int D, int WR, int WK>
-int launch_shared(const AttnArgs& a, const SharedArgs& sh, int64_t units, hipStream_t s) {
+int launch_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
   constexpr size_t lds = WK == 1 ? 0 : (size_t)WK * 64 * (D / 2 + 3) * sizeof(float);
   static std::atomic<uint64_t> raised{0};
   if (lds > 64 * 1024) {
     const int rc = set_lds_limit_once(raised, (const void*)attn_shared_kernel<TYPE, D, WR, WK>, lds);
     if (rc != SZO_OK) return rc;
   }
+  const int64_t units = (int64_t)((sh.tiles + WR - 1) / WR) * sh.splits;
   attn_shared_kernel<TYPE, D, WR, WK><<<dim3((unsigned)(units * a.d.cache.kv_heads)), 64 * WR * WK, lds, s>>>(
-      a.d.q_start, a.d.cache.lengths, a.d.cache.page_table, a.d.cache.max_pages, a.blocks_per_page, a.splits, a.tiles, a, sh);
+      a.d.q_start, a.d.cache.lengths, a.d.cache.page_table, a.d.cache.max_pages, a.blocks_per_page, sh.splits, sh.tiles, a, sh);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }
 
 template <int TYPE, int D, int G>
 int join_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
-  const int pieces = (a.rows_cap * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
-  const dim3 grid((unsigned)(a.tiles * pieces), (unsigned)a.d.cache.kv_heads, (unsigned)a.d.cache.sequences);
-  attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, a.tiles, a.splits, a.rows_cap, a, sh);
+  constexpr int pieces = (32 * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
+  const dim3 grid((unsigned)(sh.tiles * pieces), (unsigned)a.d.cache.kv_heads);
+  attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, sh.tiles, sh.splits, 32, a, sh);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }
 
 template <int TYPE, int D>
-int launch_shared_all(const AttnArgs& a, SharedArgs sh, const SharedPlan& p, hipStream_t s) {
-  const int64_t own = (int64_t)a.d.cache.sequences * a.tiles * a.splits;
-  int rc;
-  if (p.wr == 4) {
-    rc = launch_shared<TYPE, D, 4, 1>(a, sh, sh.units, s);
-    if (rc != SZO_OK) return rc;
-    sh.first_unit = sh.units;
-    rc = launch_shared<TYPE, D, 1, 4>(a, sh, own, s);
-  } else {
-    rc = launch_shared<TYPE, D, 1, 4>(a, sh, sh.units + own, s);
-  }
-  if (rc != SZO_OK) return rc;
-  return sh.splits + a.splits < 6 || a.rows_cap > 16 ? join_shared<TYPE, D, 1>(a, sh, s) : join_shared<TYPE, D, 16>(a, sh, s);
+int launch_shared_all(const AttnArgs& a, const SharedArgs& sh, const SharedPlan& p, hipStream_t s) {
+  const int rc = p.wr == 4   ? launch_shared<TYPE, D, 4, 1>(a, sh, s)
+                 : p.wk == 8 ? launch_shared<TYPE, D <= 128 ? D : 128, 1, 8>(a, sh, s)
+                             : launch_shared<TYPE, D, 1, 4>(a, sh, s);
+  return rc != SZO_OK || sh.splits == 1 ? rc : join_shared<TYPE, D, 1>(a, sh, s);
 }
 
 template <int TYPE>
@@ -941,34 +1068,21 @@ int szo_attn_cached(const szo_attn_desc* d, void* workspace, void* stream) {
 
 size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* d, const szo_attn_groups* g) {
   if (check(d, g) != SZO_OK || nothing(d)) return 16;
-  if (!shares(g)) return szo_attn_workspace_bytes(d);
+  if (!together(d, g)) return szo_attn_workspace_bytes(d);
   const SharedPlan p = plan_of(d, g);
-  return (shared_floats(d, g, p) + own_floats(d, p)) * sizeof(float);
+  return p.splits == 1 ? 16 : (size_t)p.tiles * d->cache.kv_heads * p.splits * part_floats(32, d->cache.head_dim) * sizeof(float);
 }
 
 int szo_attn_shared(const szo_attn_desc* d, const szo_attn_groups* g, void* workspace, void* stream) {
   const int rc = check(d, g);
   if (rc != SZO_OK) return rc;
   if (nothing(d)) return SZO_OK;
-  if (!shares(g)) return szo_attn_cached(d, workspace, stream);
-  if (!workspace || !aligned_to(workspace, 16)) return SZO_EINVAL;
+  if (!together(d, g)) return szo_attn_cached(d, workspace, stream);
   const SharedPlan p = plan_of(d, g);
+  if (p.splits > 1 && (!workspace || !aligned_to(workspace, 16))) return SZO_EINVAL;
   AttnArgs a = args_of(d, workspace);
-  a.tiles = p.own_tiles;
-  a.splits = p.own_splits;
-  a.rows_cap = p.own_cap;
-  SharedArgs sh = {};
-  sh.group_start = g->group_start;
-  sh.shared = g->shared;
-  sh.groups = g->groups;
-  sh.most_blocks = g->max_shared / kKvBlock;
-  sh.tiles = p.tiles;
-  sh.wave_tiles = p.tiles * p.wr;
-  sh.splits = p.splits;
-  sh.rows_cap = p.rows_cap;
-  sh.rows = p.rows;
-  sh.units = g->groups * p.tiles * p.splits;
-  sh.own_at = (int64_t)shared_floats(d, g, p);
+  a.splits = 1;
+  const SharedArgs sh = {g->group_start, g->shared, g->groups, g->max_shared / kKvBlock, p.tiles, p.splits, divisor(a.group), divisor(a.blocks_per_page)};
   return d->type == SZO_BF16 ? launch_shared_dim<SZO_BF16>(a, sh, p, (hipStream_t)stream) : launch_shared_dim<SZO_F16>(a, sh, p, (hipStream_t)stream);
 }
 
