@@ -440,6 +440,9 @@ typedef struct szo_attn_groups {
  * szo_attn_cached, for more than 2^30 rows (tokens times query heads of a key head), and beyond 2^23 - 1 tiles times parts and key heads. */
 int szo_attn_shared(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */, void* workspace, void* stream);
 size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */);
+/* Inspection: plan[0]: 1 where sequences go together, 0 where each goes by itself as in szo_attn_cached (nothing shared, or so little to do that it is faster); then tiles side by
+ * side in a workgroup (4 or 1), waves that share a tile's blocks, parts of them. */
+int szo_attn_shared_plan(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */, int32_t* plan /* host, 4 */);
 
 /* Log probabilities of given tokens under softmax(scale * logits), row by row, in one pass over the logits:
  *   logp = scale x_target - log sum exp(scale x)      entropy = -sum p log p      alternatives: the `top` largest logits

@@ -1073,6 +1073,19 @@ size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* d, const szo_attn_gr
   return p.splits == 1 ? 16 : (size_t)p.tiles * d->cache.kv_heads * p.splits * part_floats(32, d->cache.head_dim) * sizeof(float);
 }
 
+int szo_attn_shared_plan(const szo_attn_desc* d, const szo_attn_groups* g, int32_t* plan) {
+  const int rc = check(d, g);
+  if (rc != SZO_OK) return rc;
+  if (!plan) return SZO_EINVAL;
+  const bool some = !nothing(d) && together(d, g);
+  const SharedPlan p = some ? plan_of(d, g) : SharedPlan{};
+  plan[0] = some;
+  plan[1] = p.wr;
+  plan[2] = p.wk;
+  plan[3] = p.splits;
+  return SZO_OK;
+}
+
 int szo_attn_shared(const szo_attn_desc* d, const szo_attn_groups* g, void* workspace, void* stream) {
   const int rc = check(d, g);
   if (rc != SZO_OK) return rc;

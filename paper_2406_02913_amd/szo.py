@@ -149,6 +149,7 @@ _SIGS = {
     "szo_attn_cached": (C.c_int, [_P(AttnDesc), C.c_void_p, C.c_void_p]),
     "szo_attn_plan": (C.c_int, [_P(AttnDesc), C.c_void_p]),
     "szo_attn_shared": (C.c_int, [_P(AttnDesc), _P(AttnGroups), C.c_void_p, C.c_void_p]),
+    "szo_attn_shared_plan": (C.c_int, [_P(AttnDesc), _P(AttnGroups), C.c_void_p]),
     "szo_attn_shared_workspace_bytes": (C.c_size_t, [_P(AttnDesc), _P(AttnGroups)]),
     "szo_attn_workspace_bytes": (C.c_size_t, [_P(AttnDesc)]),
     "szo_token_logprobs": (C.c_int, [_P(LogprobsDesc), C.c_void_p, C.c_void_p]),
@@ -561,6 +562,13 @@ def szo_attn_shared(desc, groups, workspace=None, stream=None):
 
 def szo_attn_shared_workspace_bytes(desc, groups):
     return int(lib.szo_attn_shared_workspace_bytes(C.byref(desc), C.byref(groups)))
+
+
+def szo_attn_shared_plan(desc, groups):
+    """(sequences go together, tiles of rows side by side, waves that share a tile's blocks, parts of the blocks)"""
+    plan = (C.c_int32 * 4)()
+    _check("szo_attn_shared_plan", lib.szo_attn_shared_plan(C.byref(desc), C.byref(groups), plan))
+    return tuple(plan)
 
 
 def make_logprobs_desc(logits, targets=None, logp=None, entropy=None, stats=None, top_logp=None, top_index=None, scale=1.0, loss_acc=None, loss_scale=1.0):

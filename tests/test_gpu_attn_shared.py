@@ -24,13 +24,19 @@ class Shared:
             for s in range(first, starts[g + 1]):
                 self.b.table[s, :pages] = self.b.table[first, :pages]
 
-    def check(self, monkeypatch, lengths, new, group, kind, max_sequences=None, max_shared=None, **kw):
+    def check(self, monkeypatch, lengths, new, group, kind, max_sequences=None, max_shared=None, max_len=1 << 17, plan=None, **kw):
+        """max_len: a hint; one as large as this makes small batches go together, in many parts."""
+        def call(d, room):
+            if plan is not None:
+                plan.append(szo.szo_attn_shared_plan(d, groups))
+            szo.szo_attn_shared(d, groups, room)
+
         groups = szo.make_attn_groups(ints(self.starts), ints(self.shared), max_sequences or max(b - a for a, b in zip(self.starts, self.starts[1:])),
                                       max(self.shared) if max_shared is None else max_shared)
         with monkeypatch.context() as m:
             m.setattr(szo, "szo_attn_workspace_bytes", lambda d: szo.szo_attn_shared_workspace_bytes(d, groups))
-            m.setattr(szo, "szo_attn_cached", lambda d, room: szo.szo_attn_shared(d, groups, room))
-            return one.check(self.b, lengths, new, group, kind, **kw)
+            m.setattr(szo, "szo_attn_cached", call)
+            return one.check(self.b, lengths, new, group, kind, max_len=max_len, **kw)
 
 
 # lengths, groups of sequences, shared tokens
@@ -101,11 +107,25 @@ def test_more_groups_and_sequences_than_a_wave_has_lanes(monkeypatch):
     Shared(lengths, [0, 150], [32], 1, 64, 32).check(monkeypatch, lengths, [1 if i % 3 else 0 for i in range(150)], 1, "bf16")
 
 
-def test_many_rows_take_their_blocks_side_by_side(monkeypatch):
-    """2100 tiles of rows of one prefix: the kernel with four tiles a workgroup, and sequences' own blocks in a second launch."""
-    lengths = [64 + 60 + i % 5 for i in range(70)]
-    new = [60 + i % 5 - 2 for i in range(70)]
-    Shared(lengths, [0, 70], [64], 8, 64, 32).check(monkeypatch, lengths, new, 2, "bf16")
+# head_dim, key heads, group, sequences, new tokens of each, hint of lengths -> what the plan says
+WAYS = [(64, 8, 2, 70, 60, 1 << 17, (1, 4, 1, 1)),                 # tiles side by side
+        (128, 8, 4, 70, 60, 1 << 17, (1, 4, 1, 1)), (256, 8, 2, 70, 61, 1 << 17, (1, 4, 1, 1)),
+        (128, 8, 4, 40, 10, 1 << 17, (1, 1, 4, 1)),                  # four waves a tile, whole
+        (128, 4, 4, 64, 1, 1 << 17, (1, 1, 8, 8)),                   # eight, in parts
+        (96, 32, 1, 256, 1, 2000, (1, 1, 8, 1)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),            # eight, whole
+        (64, 8, 1, 64, 1, 200, (1, 1, 4, 24)), (256, 2, 2, 64, 1, 600, (1, 1, 4, 32)), (96, 2, 3, 40, 1, 2400, (1, 1, 8, 42)),
+        (64, 1, 2, 5, 1, 200, (0, 0, 0, 0))]                          # each by itself
+
+
+@pytest.mark.parametrize("D,heads,group,sequences,new,hint,want", WAYS)
+def test_every_way_that_sizes_choose(monkeypatch, D, heads, group, sequences, new, hint, want):
+    """With groups that end inside tiles and lengths on both sides of a block's end."""
+    third = sequences // 3
+    lengths = [64 + new + i * 7 % 40 for i in range(third)] + [32 + new + i * 5 % 37 for i in range(third, sequences)]
+    many = [max(1, new - i % 4) for i in range(sequences)]
+    plan = []
+    Shared(lengths, [0, third, sequences], [64, 32], heads, D, 32).check(monkeypatch, lengths, many, group, "bf16", max_len=hint, plan=plan)
+    assert plan == [want]
 
 
 def test_pages_that_are_not_there_and_nan(monkeypatch):
@@ -134,7 +154,7 @@ def _plain(seed=5, B=6, D=128, heads=2, group=4, pre=256):
 
     def call():
         out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device=DEV)
-        d = szo.make_attn_desc(s.b.cache(), q, out, ints(list(range(B + 1))), 1, max(lengths), D ** -0.5, lse=lse)
+        d = szo.make_attn_desc(s.b.cache(), q, out, ints(list(range(B + 1))), 1, 1 << 17, D ** -0.5, lse=lse)
         room = torch.empty(szo.szo_attn_shared_workspace_bytes(d, groups), dtype=torch.uint8, device=DEV)
         return (out, lse), lambda: szo.szo_attn_shared(d, groups, room)
 
@@ -146,7 +166,7 @@ def test_queries_left_out_and_rows_behind_the_last_sequence_stay_as_they_are():
     q = torch.randn(20, 8, 128, device=DEV).bfloat16()
     out = torch.full_like(q, 3.0)
     start = [0, 3, 4, 9, 10, 11, 12]
-    d = szo.make_attn_desc(s.b.cache(), q, out, ints(start), 2, max(lengths), 128 ** -0.5)       # two queries of a sequence at most
+    d = szo.make_attn_desc(s.b.cache(), q, out, ints(start), 2, 1 << 17, 128 ** -0.5)            # two queries of a sequence at most
     szo.szo_attn_shared(d, groups, torch.empty(szo.szo_attn_shared_workspace_bytes(d, groups), dtype=torch.uint8, device=DEV))
     left = [2, 6, 7, 8] + list(range(12, 20))
     assert (out[left] == 3).all()
