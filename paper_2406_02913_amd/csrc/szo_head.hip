@@ -65,36 +65,40 @@ __device__ __forceinline__ uint2 rounded4(const f32x4& v, float by) {
   return __builtin_bit_cast(uint2, h);
 }
 
-// Logits of a tile: vocabulary entries of [v0, v0 + 256) by rows of [t0, t0 + BT).
-template <int TYPE, int BT, int WI, int WJ> using LogitTile = Tile<TYPE, false, false, kTileV, BT, WI, WJ>;
+// Logits of a tile: vocabulary entries of [v0, v0 + BV) by rows of [t0, t0 + BT).  Tiles of 256 x 256, or, for up to 448 rows, of 128 entries by all of them, so that the weight is
+// read once, and by half as many entries, so that more CUs do; with few rows LDS holds more steps, which is what hides the memory's latency then.
+constexpr int stages_of(int bv, int bt) { return bv == 256 ? 2 : (160 * 1024) / ((bv + bt) * 128) < 4 ? (160 * 1024) / ((bv + bt) * 128) : 4; }
+template <int TYPE, int BV, int BT> struct LogitTile : Tile<TYPE, false, false, BV, BT, 2, 4, stages_of(BV, BT)> {
+  static constexpr int kWaveV = BV / 2, kWaveT = BT / 4;
+};
 
-template <int TYPE, int BT, int WI, int WJ>
-__device__ __forceinline__ void logits_of(LogitTile<TYPE, BT, WI, WJ>& tile, const HeadArgs& a, int64_t v0, int64_t t0, lds_at lds, int wave, int lane) {
+template <int TYPE, int BV, int BT>
+__device__ __forceinline__ void logits_of(LogitTile<TYPE, BV, BT>& tile, const HeadArgs& a, int64_t v0, int64_t t0, lds_at lds, int wave, int lane) {
   const szo_head_desc& d = a.d;
-  const Operand w = {static_cast<const uint16_t*>(d.weight) + v0 * d.weight_stride, d.weight_stride, min((int64_t)kTileV, d.vocab - v0), d.width};
+  const Operand w = {static_cast<const uint16_t*>(d.weight) + v0 * d.weight_stride, d.weight_stride, min((int64_t)BV, d.vocab - v0), d.width};
   const Operand x = {static_cast<const uint16_t*>(d.x) + t0 * d.x_stride, d.x_stride, min((int64_t)BT, d.rows - t0), d.width};
   tile.run(w, x, d.width / kStep, lds, wave, lane);
 }
 
-template <int TYPE, int BT, int WI, int WJ>
+template <int TYPE, int BV, int BT>
 __global__ void __launch_bounds__(kThreads, 2) head_stats_kernel(const HeadArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  typedef LogitTile<TYPE, BT, WI, WJ> L;
+  typedef LogitTile<TYPE, BV, BT> L;
   const szo_head_desc& d = a.d;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
   int ti, tj;
   tile_of(blockIdx.x, a.tiles_v, a.tiles_t, ti, tj);
-  const int64_t v0 = (int64_t)ti * kTileV, t0 = (int64_t)tj * BT;
+  const int64_t v0 = (int64_t)ti * BV, t0 = (int64_t)tj * BT;
   L tile;
-  logits_of<TYPE, BT, WI, WJ>(tile, a, v0, t0, (lds_at)lds, wave, lane);
+  logits_of<TYPE, BV, BT>(tile, a, v0, t0, (lds_at)lds, wave, lane);
   __syncthreads();
-  float2* const meet = reinterpret_cast<float2*>(lds);                 // [WI][BT]
+  float2* const meet = reinterpret_cast<float2*>(lds);                 // [2][BT]
   const float by = d.scale * kLog2e;
-  const int mine = wi * (kTileV / WI) + 4 * (lane >> 4);              // this lane's first entry
-  const int there = (int)min((int64_t)kTileV, d.vocab - v0);
+  const int mine = wi * L::kWaveV + 4 * (lane >> 4);              // this lane's first entry
+  const int there = (int)min((int64_t)BV, d.vocab - v0);
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
-    const int column = wj * (BT / WJ) + 16 * j + (lane & 15);
+    const int column = wj * L::kWaveT + 16 * j + (lane & 15);
     const int64_t token = t0 + column;
     const int64_t target = token < d.rows && d.targets ? d.targets[token] : -1;
     float most = -__builtin_inff();
@@ -128,10 +132,10 @@ __global__ void __launch_bounds__(kThreads, 2) head_stats_kernel(const HeadArgs 
     if (t0 + column >= d.rows) break;
     float most = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WI; ++w) most = fmaxf(most, meet[w * BT + column].x);
+    for (int w = 0; w < 2; ++w) most = fmaxf(most, meet[w * BT + column].x);
     const float base = most == -__builtin_inff() ? 0.f : most;
 #pragma unroll
-    for (int w = 0; w < WI; ++w) sum += meet[w * BT + column].y * __builtin_amdgcn_exp2f((meet[w * BT + column].x - base) * by);
+    for (int w = 0; w < 2; ++w) sum += meet[w * BT + column].y * __builtin_amdgcn_exp2f((meet[w * BT + column].x - base) * by);
     a.parts[(t0 + column) * a.tiles_v + ti] = make_float2(most, sum);
   }
 }
@@ -205,23 +209,23 @@ __global__ void __launch_bounds__(256) head_zero_kernel(uint16_t* out, int64_t r
   if (row < rows) out[row * stride + i % width] = 0;
 }
 
-template <int TYPE, int BT, int WI, int WJ>
+template <int TYPE, int BV, int BT>
 __global__ void __launch_bounds__(kThreads, 2) head_grad_kernel(const HeadArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  typedef LogitTile<TYPE, BT, WI, WJ> L;
+  typedef LogitTile<TYPE, BV, BT> L;
   const szo_head_desc& d = a.d;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
   int ti, tj;
   tile_of(blockIdx.x, a.tiles_v, a.tiles_t, ti, tj);
-  const int64_t v0 = a.first_v + (int64_t)ti * kTileV, t0 = (int64_t)tj * BT;
+  const int64_t v0 = a.first_v + (int64_t)ti * BV, t0 = (int64_t)tj * BT;
   L tile;
-  logits_of<TYPE, BT, WI, WJ>(tile, a, v0, t0, (lds_at)lds, wave, lane);
+  logits_of<TYPE, BV, BT>(tile, a, v0, t0, (lds_at)lds, wave, lane);
   const float by = d.scale * kLog2e;
-  const int mine = wi * (kTileV / WI) + 4 * (lane >> 4);
-  const int there = (int)min((int64_t)kTileV, d.vocab - v0);
+  const int mine = wi * L::kWaveV + 4 * (lane >> 4);
+  const int there = (int)min((int64_t)BV, d.vocab - v0);
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
-    const int64_t token = t0 + wj * (BT / WJ) + 16 * j + (lane & 15);
+    const int64_t token = t0 + wj * L::kWaveT + 16 * j + (lane & 15);
     if (token >= a.rows64) continue;
     const bool in = token < d.rows;
     const float g = in ? a.row_grad[token] : 0.f, most = in ? d.stats[2 * token] : 0.f, sum = in ? d.stats[2 * token + 1] : 1.f;
@@ -351,6 +355,10 @@ constexpr int64_t kMostStride = 1 << 22;
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 int64_t tiles_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+// Tiles of logits: rows of one, vocabulary entries of one.
+int logit_rows(int64_t rows) { return rows <= 448 ? (int)tiles_of(rows, 64) * 64 : 256; }
+int logit_entries(int64_t rows) { return rows <= 448 ? 128 : 256; }
+// Rows of a tile of dx.
 int row_tile(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 int check(const szo_head_desc* d) {
@@ -361,7 +369,7 @@ int check(const szo_head_desc* d) {
   if (d->x_stride > kMostStride || d->weight_stride > kMostStride || d->x_stride % 8 || d->weight_stride % 8) return SZO_EUNSUPPORTED;
   if ((d->rows && !d->x) || (d->vocab && !d->weight) || !aligned_to(d->x, 16) || !aligned_to(d->weight, 16)) return SZO_EINVAL;
   if (!aligned_to(d->targets, 4) || !aligned_to(d->logp, 4) || !aligned_to(d->stats, 4) || !aligned_to(d->loss_acc, 8)) return SZO_EINVAL;
-  if (tiles_of(d->vocab, kTileV) * tiles_of(d->rows, row_tile(d->rows)) > kMostGroups) return SZO_EUNSUPPORTED;
+  if (d->rows && tiles_of(d->vocab, logit_entries(d->rows)) * tiles_of(d->rows, logit_rows(d->rows)) > kMostGroups) return SZO_EUNSUPPORTED;
   return SZO_OK;
 }
 
@@ -375,19 +383,28 @@ int launch(F* kernel, std::atomic<uint64_t>& raised, size_t bytes, int64_t group
   return SZO_OK;
 }
 
-template <int TYPE, int BT, int WI, int WJ>
+template <int TYPE, int BV, int BT>
 int logit_launch(const HeadArgs& a, bool backward, hipStream_t s) {
   static std::atomic<uint64_t> raised[2] = {{0}, {0}};
+  typedef LogitTile<TYPE, BV, BT> L;
   const int64_t groups = (int64_t)a.tiles_v * a.tiles_t;
-  return backward ? launch(head_grad_kernel<TYPE, BT, WI, WJ>, raised[1], LogitTile<TYPE, BT, WI, WJ>::kLds, groups, s, a)
-                  : launch(head_stats_kernel<TYPE, BT, WI, WJ>, raised[0], LogitTile<TYPE, BT, WI, WJ>::kLds, groups, s, a);
+  return backward ? launch(head_grad_kernel<TYPE, BV, BT>, raised[1], L::kLds, groups, s, a) : launch(head_stats_kernel<TYPE, BV, BT>, raised[0], L::kLds, groups, s, a);
 }
+// Logits of `vocab` entries.
 template <int TYPE>
-int logit_launch(const HeadArgs& a, bool backward, hipStream_t s) {
-  switch (row_tile(a.d.rows)) {
-    case 64: return logit_launch<TYPE, 64, 4, 2>(a, backward, s);
-    case 128: return logit_launch<TYPE, 128, 4, 2>(a, backward, s);
-    default: return logit_launch<TYPE, 256, 2, 4>(a, backward, s);
+int logit_launch(HeadArgs a, int64_t vocab, bool backward, hipStream_t s) {
+  const int bt = logit_rows(a.d.rows);
+  a.tiles_v = (int)tiles_of(vocab, logit_entries(a.d.rows));
+  a.tiles_t = (int)tiles_of(a.d.rows, bt);
+  if (logit_entries(a.d.rows) == 256) return logit_launch<TYPE, 256, 256>(a, backward, s);
+  switch (bt) {
+    case 64: return logit_launch<TYPE, 128, 64>(a, backward, s);
+    case 128: return logit_launch<TYPE, 128, 128>(a, backward, s);
+    case 192: return logit_launch<TYPE, 128, 192>(a, backward, s);
+    case 256: return logit_launch<TYPE, 128, 256>(a, backward, s);
+    case 320: return logit_launch<TYPE, 128, 320>(a, backward, s);
+    case 384: return logit_launch<TYPE, 128, 384>(a, backward, s);
+    default: return logit_launch<TYPE, 128, 448>(a, backward, s);
   }
 }
 
@@ -461,7 +478,7 @@ int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, in
     a.piece_v = std::min(p.pitch, d.vocab - a.first_v);
     a.tiles_v = (int)tiles_of(a.piece_v, kTileV);
     a.steps = (int)tiles_of(a.piece_v, kStep);
-    rc = logit_launch<TYPE>(a, true, s);
+    rc = logit_launch<TYPE>(a, a.piece_v, true, s);
     if (rc != SZO_OK) return rc;
     if (x_grad) {                            // before the weight's, which may overwrite the piece's rows of the weight
       a.out = x_grad;
@@ -491,7 +508,7 @@ int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, in
   return SZO_OK;
 }
 
-size_t parts_bytes(const szo_head_desc* d) { return up16((size_t)d->rows * tiles_of(d->vocab, kTileV) * sizeof(float2)); }
+size_t parts_bytes(const szo_head_desc* d) { return up16((size_t)d->rows * tiles_of(d->vocab, logit_entries(d->rows)) * sizeof(float2)); }
 
 }  // namespace
 }  // namespace szo
@@ -514,11 +531,10 @@ int szo_head_logprobs(const szo_head_desc* d, void* workspace, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   HeadArgs a = {};
   a.d = *d;
-  a.tiles_v = (int)tiles_of(d->vocab, kTileV);
-  a.tiles_t = (int)tiles_of(d->rows, row_tile(d->rows));
+  a.tiles_v = (int)tiles_of(d->vocab, logit_entries(d->rows));             // for the joining kernel
   a.parts = (float2*)workspace;
   a.hit = (float*)((char*)workspace + parts_bytes(d));
-  const int done = d->type == SZO_BF16 ? logit_launch<SZO_BF16>(a, false, s) : logit_launch<SZO_F16>(a, false, s);
+  const int done = d->type == SZO_BF16 ? logit_launch<SZO_BF16>(a, d->vocab, false, s) : logit_launch<SZO_F16>(a, d->vocab, false, s);
   if (done != SZO_OK) return done;
   head_join_kernel<<<dim3((unsigned)tiles_of(d->rows, 4)), 256, 0, s>>>(a);
   SZO_LAUNCH_CHECK();

@@ -1,7 +1,7 @@
 // Products of 16-bit matrices in tiles of BI x BJ for a workgroup of eight waves, C[i][j] = sum over r of A(i, r) B(j, r), sums in fp32 registers.
 //
 // Either operand lies in memory with r contiguous ("rows": a row of A is an i) or with i (j) contiguous ("columns": a row is an r).  A step takes 64 of r.  Its
-// operands go from memory to LDS without passing through registers, 16 bytes a lane and 1 KiB an instruction, two steps' worth held; lanes choose what they
+// operands go from memory to LDS without passing through registers, 16 bytes a lane and 1 KiB an instruction, two or more steps' worth held; lanes choose what they
 // read, since a load puts them side by side in LDS:
 //   rows     [row][64 of r]: the eight 16-byte pieces of a row are exchanged by (row / 2) mod 8, so that 16 lanes that read one piece of 16 rows touch every bank once
 //   columns  [r][256 of i], two r to an instruction: 16-wide groups are exchanged in pairs in odd r, pairs of r lie 64 bytes and eights of them 128 further than they are
@@ -83,34 +83,43 @@ struct Side {
     }
   }
 
+  static constexpr uint32_t kApart = COLUMNS ? kPairBytes : 2048;            // in LDS, of one load and the next
+  template <int N>
+  __device__ __forceinline__ void issue(uint32_t to, uint32_t from, rsrc_t rsrc) const {
+    uint32_t at;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    // m0 is no register that values are allocated to, which the compiler warns of; named all the same.  Wait states: a vector instruction may have written the
+    // descriptor just before.
+    if constexpr (N == 4) {
+      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
+                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(kApart) : "memory", "scc", "m0");
+    } else if constexpr (N == 2) {
+      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
+                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
+                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
+                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(kApart) : "memory", "scc", "m0");
+    } else {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(from), "s"(rsrc) : "memory", "scc", "m0");
+    }
+#pragma clang diagnostic pop
+  }
+
   // Loads of the next step, which is there; addresses out of bounds read as zero.  In assembly: behind the compiler's own form it waits for all of them at every LDS
   // read, and kept apart the loads' addresses would take registers that the main loop has not got.
   __device__ __forceinline__ void load(int stage) {
     const uint32_t bytes = COLUMNS ? (uint32_t)min(left - 1, kStep - 1) * pitch + row_bytes : (uint32_t)left;
     const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32), bytes, 0x00027000u};
     const uint32_t to = lds + (uint32_t)(stage * kStage);
-    uint32_t at;
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-    // m0 is no register that values are allocated to, which the compiler warns of; named all the same.  Wait states: a vector instruction may have written the
-    // descriptor just before.
-    if constexpr (kLoads == 4) {
-      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
-                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %0, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\tv_add_u32 %0, %2, %0\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
-                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(COLUMNS ? kPairBytes : 2048) : "memory", "scc", "m0");
-    } else if constexpr (kLoads == 2) {
-      asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\ts_nop 4\n\t"
-                   "buffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_add_u32 m0, m0, %5\n\ts_nop 0\n\t"
-                   "buffer_load_dwordx4 %0, %4, 0 offen lds"
-                   : "=&v"(at) : "s"(to), "s"(apart), "v"(from), "s"(rsrc), "i"(2048) : "memory", "scc", "m0");
-    } else {
-      static_assert(kLoads == 1, "64, 128 or 256");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(from), "s"(rsrc) : "memory", "scc", "m0");
-    }
-#pragma clang diagnostic pop
+    constexpr int kFours = kLoads / 4;
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) issue<4>(to + i * 4 * kApart, from + (uint32_t)i * 4 * apart, rsrc);
+    if constexpr (kLoads % 4 >= 2) issue<2>(to + kFours * 4 * kApart, from + (uint32_t)kFours * 4 * apart, rsrc);
+    if constexpr (kLoads % 2) issue<1>(to + (kLoads - 1) * kApart, from + (uint32_t)(kLoads - 1) * apart, rsrc);
     base += COLUMNS ? (uint64_t)pitch * kStep : (uint64_t)(kStep * 2);
     left -= COLUMNS ? kStep : kStep * 2;
   }
@@ -135,17 +144,17 @@ struct Side {
 };
 
 // The tile's sums: a lane has C[16 ti + 4 (lane / 16) + 0..3][16 tj + lane % 16] of its wave's part.  `steps` > 0 steps.
-template <int TYPE, bool A_COLUMNS, bool B_COLUMNS, int BI, int BJ, int WI, int WJ>
+template <int TYPE, bool A_COLUMNS, bool B_COLUMNS, int BI, int BJ, int WI, int WJ, int STAGES = 2>
 struct Tile {
   static constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
-  static constexpr int kLds = 2 * (stage_bytes<A_COLUMNS, BI>() + stage_bytes<B_COLUMNS, BJ>());
+  static constexpr int kLds = STAGES * (stage_bytes<A_COLUMNS, BI>() + stage_bytes<B_COLUMNS, BJ>());
   static_assert(WI * WJ == 8 && kLds <= 160 * 1024, "eight waves, one workgroup's LDS");
   typedef typename Product<TYPE>::vec vec;
   f32x4 sum[TI][TJ];
 
   __device__ __forceinline__ void run(const Operand& a_op, const Operand& b_op, int steps, lds_at lds, int wave, int lane) {
     Side<A_COLUMNS, BI, TI> a(a_op, lds, wave, wave / WJ * (BI / WI), lane);
-    Side<B_COLUMNS, BJ, TJ> b(b_op, lds + 2 * stage_bytes<A_COLUMNS, BI>(), wave, wave % WJ * (BJ / WJ), lane);
+    Side<B_COLUMNS, BJ, TJ> b(b_op, lds + STAGES * stage_bytes<A_COLUMNS, BI>(), wave, wave % WJ * (BJ / WJ), lane);
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
@@ -157,52 +166,59 @@ struct Tile {
     auto read_a = [&](int stage, int g) { x[g % (kAhead + 1)] = a.template fragment<TYPE>(stage, g / TI, g % TI); };
     auto read_b = [&](int stage, int half, int j) { y[half][j] = b.template fragment<TYPE>(stage, half, j); };
     static_assert(kGroups % (kAhead + 1) == 0, "a step begins with the ring's first place");
-    auto step = [&](int stage, int at) {
+    constexpr int kLoads = Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads;
+    auto step = [&](int stage, int next, int at) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         if (g == kGroups - kAhead) {
-          // every wave has read the stage, and the next one has arrived for all of them
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          if (at + 2 < steps) {
+          // every wave has read the stage, and the next one has arrived for all of them; those behind it may be on their way
+          if (STAGES == 2 || at + STAGES > steps) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "i"((STAGES - 2) * kLoads) : "memory");
+          if (at + STAGES < steps) {
             a.load(stage);
             b.load(stage);
           }
         }
         if (g < kGroups - kAhead) read_a(stage, g + kAhead);
-        else read_a(stage ^ 1, g + kAhead - kGroups);        // behind the last step: what lies there, for nothing
+        else read_a(next, g + kAhead - kGroups);             // behind the last step: what lies there, for nothing
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
           if (g == j * (TI / 2) / TJ) read_b(stage, 1, j);
-          if (g == kGroups - kAhead + j * 2 / TJ) read_b(stage ^ 1, 0, j);
+          if (g == kGroups - kAhead + j * 2 / TJ) read_b(next, 0, j);
         }
 #pragma unroll
         for (int j = 0; j < TJ; ++j) sum[g % TI][j] = Product<TYPE>::add(x[g % (kAhead + 1)], y[g / TI][j], sum[g % TI][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    a.load(0);
-    b.load(0);
-    if (steps > 1) {
-      a.load(1);
-      b.load(1);
-      constexpr int loads = Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads;
-      if constexpr (loads == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-      else if constexpr (loads == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-      else asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+      if (i < steps) {
+        a.load(i);
+        b.load(i);
+      }
+    if (steps >= STAGES) asm volatile("s_waitcnt vmcnt(%0)" :: "i"((STAGES - 1) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int j = 0; j < TJ; ++j) read_b(0, 0, j);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) read_a(0, g);
-    int at = 0;
-    for (; at + 1 < steps; at += 2) {
-      step(0, at);
-      step(1, at + 1);
+    if constexpr (STAGES == 2) {
+      int at = 0;
+      for (; at + 1 < steps; at += 2) {
+        step(0, 1, at);
+        step(1, 0, at + 1);
+      }
+      if (at < steps) step(0, 1, at);
+    } else {
+      int stage = 0;
+      for (int at = 0; at < steps; ++at) {
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+        step(stage, next, at);
+        stage = next;
+      }
     }
-    if (at < steps) step(0, at);
   }
 };
 
