@@ -65,10 +65,11 @@ __device__ __forceinline__ uint2 rounded4(const f32x4& v, float by) {
   return __builtin_bit_cast(uint2, h);
 }
 
-// Logits of a tile: vocabulary entries of [v0, v0 + BV) by rows of [t0, t0 + BT).  Tiles of 256 x 256, or, for up to 448 rows, of 128 entries by all of them, so that the weight is
-// read once, and by half as many entries, so that more CUs do; with few rows LDS holds more steps, which is what hides the memory's latency then.
-constexpr int stages_of(int bv, int bt) { return bv == 256 ? 2 : (160 * 1024) / ((bv + bt) * 128) < 4 ? (160 * 1024) / ((bv + bt) * 128) : 4; }
-template <int TYPE, int BV, int BT> struct LogitTile : Tile<TYPE, false, false, BV, BT, 2, 4, stages_of(BV, BT)> {
+// Logits of a tile: vocabulary entries of [v0, v0 + BV) by rows of [t0, t0 + BT).  Tiles of 256 x 256, or of 128 entries by up to 448 rows, so that up to so many rows read the weight
+// once, and more CUs do; with few rows LDS holds more steps, which is what hides the memory's latency then.
+constexpr int weight_stages(int bv, int bt) { return bv == 256 ? 2 : bt == 128 ? 4 : 3; }
+constexpr int row_stages(int bv, int bt) { return bv == 256 ? 2 : bt == 128 ? 4 : bt <= 256 ? 3 : 2; }          // 64 rows: two workgroups a CU
+template <int TYPE, int BV, int BT> struct LogitTile : Tile<TYPE, false, false, BV, BT, 2, 4, weight_stages(BV, BT), row_stages(BV, BT)> {
   static constexpr int kWaveV = BV / 2, kWaveT = BT / 4;
 };
 
@@ -355,9 +356,21 @@ constexpr int64_t kMostStride = 1 << 22;
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 int64_t tiles_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
-// Tiles of logits: rows of one, vocabulary entries of one.
-int logit_rows(int64_t rows) { return rows <= 448 ? (int)tiles_of(rows, 64) * 64 : 256; }
-int logit_entries(int64_t rows) { return rows <= 448 ? 128 : 256; }
+// Tiles of logits, chosen by the time of the rounds in which a CU each takes them, in units of a step of 64 of the width: a tile of 256 x 256 takes 1.33 us a step, one of 128
+// entries by n rows 0.27 + 0.0026 n.  That is what a few tiles take; the whole chip at work is up to a fifth slower, all kinds alike.  us for 32000 entries of width 4096, 256 x 256 / 128 by
+// 64, 128, 192, 256, 320, 384, 448: 64 rows 97 / 57, 58; 200 rows 103 / 127, 86, -, 74, 85; 300 rows 103 / -, 124, 106, -, 86, 95, 101; 600 rows 187 / -, -, 201, 187, 156, 171; 800 rows 202 / -, -, -,
+// 247, 228, -, 201; 8000 entries: 300 rows 88 / -, 40, 49, -, 69, 81, 90; 1000 rows 90 / -, -, -, 64, 74, 82, 91; 2000 rows 102.
+struct LogitPlan { int entries, rows; };
+LogitPlan logit_plan(int64_t rows, int64_t vocab) {
+  LogitPlan best = {256, 256};
+  auto rounds = [&](int entries, int n) { return (double)tiles_of(tiles_of(vocab, entries) * tiles_of(rows, n), 256); };
+  double least = 1.33 * rounds(256, 256);
+  for (int n = 448; n >= 64; n -= 64) {
+    const double us = (0.27 + 0.0026 * n) * rounds(128, n);
+    if (us <= least) { least = us; best = {128, n}; }
+  }
+  return best;
+}
 // Rows of a tile of dx.
 int row_tile(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
@@ -369,7 +382,10 @@ int check(const szo_head_desc* d) {
   if (d->x_stride > kMostStride || d->weight_stride > kMostStride || d->x_stride % 8 || d->weight_stride % 8) return SZO_EUNSUPPORTED;
   if ((d->rows && !d->x) || (d->vocab && !d->weight) || !aligned_to(d->x, 16) || !aligned_to(d->weight, 16)) return SZO_EINVAL;
   if (!aligned_to(d->targets, 4) || !aligned_to(d->logp, 4) || !aligned_to(d->stats, 4) || !aligned_to(d->loss_acc, 8)) return SZO_EINVAL;
-  if (d->rows && tiles_of(d->vocab, logit_entries(d->rows)) * tiles_of(d->rows, logit_rows(d->rows)) > kMostGroups) return SZO_EUNSUPPORTED;
+  if (d->rows) {
+    const LogitPlan p = logit_plan(d->rows, d->vocab);
+    if (tiles_of(d->vocab, p.entries) * tiles_of(d->rows, p.rows) > kMostGroups) return SZO_EUNSUPPORTED;
+  }
   return SZO_OK;
 }
 
@@ -393,11 +409,11 @@ int logit_launch(const HeadArgs& a, bool backward, hipStream_t s) {
 // Logits of `vocab` entries.
 template <int TYPE>
 int logit_launch(HeadArgs a, int64_t vocab, bool backward, hipStream_t s) {
-  const int bt = logit_rows(a.d.rows);
-  a.tiles_v = (int)tiles_of(vocab, logit_entries(a.d.rows));
-  a.tiles_t = (int)tiles_of(a.d.rows, bt);
-  if (logit_entries(a.d.rows) == 256) return logit_launch<TYPE, 256, 256>(a, backward, s);
-  switch (bt) {
+  const LogitPlan p = logit_plan(a.d.rows, vocab);
+  a.tiles_v = (int)tiles_of(vocab, p.entries);
+  a.tiles_t = (int)tiles_of(a.d.rows, p.rows);
+  if (p.entries == 256) return logit_launch<TYPE, 256, 256>(a, backward, s);
+  switch (p.rows) {
     case 64: return logit_launch<TYPE, 128, 64>(a, backward, s);
     case 128: return logit_launch<TYPE, 128, 128>(a, backward, s);
     case 192: return logit_launch<TYPE, 128, 192>(a, backward, s);
@@ -508,7 +524,7 @@ int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, in
   return SZO_OK;
 }
 
-size_t parts_bytes(const szo_head_desc* d) { return up16((size_t)d->rows * tiles_of(d->vocab, logit_entries(d->rows)) * sizeof(float2)); }
+size_t parts_bytes(const szo_head_desc* d) { return up16((size_t)d->rows * tiles_of(d->vocab, logit_plan(d->rows, d->vocab).entries) * sizeof(float2)); }
 
 }  // namespace
 }  // namespace szo
@@ -531,7 +547,7 @@ int szo_head_logprobs(const szo_head_desc* d, void* workspace, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   HeadArgs a = {};
   a.d = *d;
-  a.tiles_v = (int)tiles_of(d->vocab, logit_entries(d->rows));             // for the joining kernel
+  a.tiles_v = (int)tiles_of(d->vocab, logit_plan(d->rows, d->vocab).entries);             // for the joining kernel
   a.parts = (float2*)workspace;
   a.hit = (float*)((char*)workspace + parts_bytes(d));
   const int done = d->type == SZO_BF16 ? logit_launch<SZO_BF16>(a, d->vocab, false, s) : logit_launch<SZO_F16>(a, d->vocab, false, s);

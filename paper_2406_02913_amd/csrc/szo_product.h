@@ -143,18 +143,21 @@ struct Side {
   }
 };
 
+// SA and SB: steps of either operand that LDS holds.  Loads arrive in the order in which they are asked for, A's after B's of the same step, so with SA > SB a step waits for all but
+// A's newest: its loads have two steps to arrive, B's, which other CUs have asked for as well, one.
 // The tile's sums: a lane has C[16 ti + 4 (lane / 16) + 0..3][16 tj + lane % 16] of its wave's part.  `steps` > 0 steps.
-template <int TYPE, bool A_COLUMNS, bool B_COLUMNS, int BI, int BJ, int WI, int WJ, int STAGES = 2>
+template <int TYPE, bool A_COLUMNS, bool B_COLUMNS, int BI, int BJ, int WI, int WJ, int SA = 2, int SB = 2>
 struct Tile {
   static constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
-  static constexpr int kLds = STAGES * (stage_bytes<A_COLUMNS, BI>() + stage_bytes<B_COLUMNS, BJ>());
+  static constexpr int kLds = SA * stage_bytes<A_COLUMNS, BI>() + SB * stage_bytes<B_COLUMNS, BJ>();
+  static_assert(SA >= SB && SB >= 2, "A's loads come last");
   static_assert(WI * WJ == 8 && kLds <= 160 * 1024, "eight waves, one workgroup's LDS");
   typedef typename Product<TYPE>::vec vec;
   f32x4 sum[TI][TJ];
 
   __device__ __forceinline__ void run(const Operand& a_op, const Operand& b_op, int steps, lds_at lds, int wave, int lane) {
     Side<A_COLUMNS, BI, TI> a(a_op, lds, wave, wave / WJ * (BI / WI), lane);
-    Side<B_COLUMNS, BJ, TJ> b(b_op, lds + STAGES * stage_bytes<A_COLUMNS, BI>(), wave, wave % WJ * (BJ / WJ), lane);
+    Side<B_COLUMNS, BJ, TJ> b(b_op, lds + SA * stage_bytes<A_COLUMNS, BI>(), wave, wave % WJ * (BJ / WJ), lane);
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
@@ -166,25 +169,23 @@ struct Tile {
     auto read_a = [&](int stage, int g) { x[g % (kAhead + 1)] = a.template fragment<TYPE>(stage, g / TI, g % TI); };
     auto read_b = [&](int stage, int half, int j) { y[half][j] = b.template fragment<TYPE>(stage, half, j); };
     static_assert(kGroups % (kAhead + 1) == 0, "a step begins with the ring's first place");
-    constexpr int kLoads = Side<A_COLUMNS, BI, TI>::kLoads + Side<B_COLUMNS, BJ, TJ>::kLoads;
-    auto step = [&](int stage, int next, int at) {
+    constexpr int kLoadsA = Side<A_COLUMNS, BI, TI>::kLoads, kLoadsB = Side<B_COLUMNS, BJ, TJ>::kLoads;
+    auto step = [&](int in_a, int next_a, int in_b, int next_b, int at) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         if (g == kGroups - kAhead) {
           // every wave has read the stage, and the next one has arrived for all of them; those behind it may be on their way
-          if (STAGES == 2 || at + STAGES > steps) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "i"((STAGES - 2) * kLoads) : "memory");
-          if (at + STAGES < steps) {
-            a.load(stage);
-            b.load(stage);
-          }
+          if ((SA == 2 && SB == 2) || at + SA > steps) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "i"((SA > SB ? kLoadsA : 0) + (SB - 2) * (kLoadsA + kLoadsB)) : "memory");
+          if (at + SB < steps) b.load(in_b);
+          if (at + SA < steps) a.load(in_a);
         }
-        if (g < kGroups - kAhead) read_a(stage, g + kAhead);
-        else read_a(next, g + kAhead - kGroups);             // behind the last step: what lies there, for nothing
+        if (g < kGroups - kAhead) read_a(in_a, g + kAhead);
+        else read_a(next_a, g + kAhead - kGroups);             // behind the last step: what lies there, for nothing
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
-          if (g == j * (TI / 2) / TJ) read_b(stage, 1, j);
-          if (g == kGroups - kAhead + j * 2 / TJ) read_b(next, 0, j);
+          if (g == j * (TI / 2) / TJ) read_b(in_b, 1, j);
+          if (g == kGroups - kAhead + j * 2 / TJ) read_b(next_b, 0, j);
         }
 #pragma unroll
         for (int j = 0; j < TJ; ++j) sum[g % TI][j] = Product<TYPE>::add(x[g % (kAhead + 1)], y[g / TI][j], sum[g % TI][j]);
@@ -192,31 +193,32 @@ struct Tile {
       }
     };
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i)
+    for (int i = 0; i < SA; ++i)
       if (i < steps) {
+        if (i < SB) b.load(i);
         a.load(i);
-        b.load(i);
       }
-    if (steps >= STAGES) asm volatile("s_waitcnt vmcnt(%0)" :: "i"((STAGES - 1) * kLoads) : "memory");
+    if (steps >= SA) asm volatile("s_waitcnt vmcnt(%0)" :: "i"((SA - 1) * kLoadsA + (SB - 1) * kLoadsB) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int j = 0; j < TJ; ++j) read_b(0, 0, j);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) read_a(0, g);
-    if constexpr (STAGES == 2) {
+    if constexpr (SA == 2 && SB == 2) {
       int at = 0;
       for (; at + 1 < steps; at += 2) {
-        step(0, 1, at);
-        step(1, 0, at + 1);
+        step(0, 1, 0, 1, at);
+        step(1, 0, 1, 0, at + 1);
       }
-      if (at < steps) step(0, 1, at);
+      if (at < steps) step(0, 1, 0, 1, at);
     } else {
-      int stage = 0;
+      int in_a = 0, in_b = 0;
       for (int at = 0; at < steps; ++at) {
-        const int next = stage + 1 == STAGES ? 0 : stage + 1;
-        step(stage, next, at);
-        stage = next;
+        const int next_a = in_a + 1 == SA ? 0 : in_a + 1, next_b = in_b + 1 == SB ? 0 : in_b + 1;
+        step(in_a, next_a, in_b, next_b, at);
+        in_a = next_a;
+        in_b = next_b;
       }
     }
   }
