@@ -83,7 +83,7 @@ __device__ __forceinline__ void logits_of(LogitTile<TYPE, BV, BT>& tile, const H
 
 template <int TYPE, int BV, int BT>
 __global__ void __launch_bounds__(kThreads, 2) head_stats_kernel(const HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  extern __shared__ __attribute__((aligned(256))) uint8_t lds[];
   typedef LogitTile<TYPE, BV, BT> L;
   const szo_head_desc& d = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(256) head_zero_kernel(uint16_t* out, int64_t r
 
 template <int TYPE, int BV, int BT>
 __global__ void __launch_bounds__(kThreads, 2) head_grad_kernel(const HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  extern __shared__ __attribute__((aligned(256))) uint8_t lds[];
   typedef LogitTile<TYPE, BV, BT> L;
   const szo_head_desc& d = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
@@ -249,17 +249,17 @@ __global__ void __launch_bounds__(kThreads, 2) head_grad_kernel(const HeadArgs a
   }
 }
 
-// dx of a tile: features [k0, k0 + 256) by rows [t0, t0 + BT), over a part of the piece's vocabulary.
-template <int TYPE, int BT, int WI, int WJ>
+// dx of a tile: features [k0, k0 + BK) by rows [t0, t0 + BT), over a part of the piece's vocabulary.
+template <int TYPE, int BK, int BT>
 __global__ void __launch_bounds__(kThreads, 2) head_x_grad_kernel(const HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  typedef Tile<TYPE, true, false, 256, BT, WI, WJ> L;
+  extern __shared__ __attribute__((aligned(256))) uint8_t lds[];
+  typedef Tile<TYPE, true, false, BK, BT, 2, 4, weight_stages(BK, BT), row_stages(BK, BT)> L;
   const szo_head_desc& d = a.d;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
-  const int tiles_k = (d.width + 255) / 256, per = tiles_k * a.tiles_t, split = blockIdx.x / per;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
+  const int tiles_k = (d.width + BK - 1) / BK, per = tiles_k * a.tiles_t, split = blockIdx.x / per;
   int ti, tj;
   tile_of(blockIdx.x - split * per, tiles_k, a.tiles_t, ti, tj);
-  const int k0 = ti * 256, share = (a.steps + a.splits - 1) / a.splits, from = split * share, steps = min(share, a.steps - from);
+  const int k0 = ti * BK, share = (a.steps + a.splits - 1) / a.splits, from = split * share, steps = min(share, a.steps - from);
   const int64_t t0 = (int64_t)tj * BT, r0 = (int64_t)from * kStep;
   L tile;
   if (steps > 0) {
@@ -275,11 +275,11 @@ __global__ void __launch_bounds__(kThreads, 2) head_x_grad_kernel(const HeadArgs
   const float by = a.lift[1];
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
-    const int64_t token = t0 + wj * (BT / WJ) + 16 * j + (lane & 15);
+    const int64_t token = t0 + wj * (BT / 4) + 16 * j + (lane & 15);
     if (token >= d.rows) continue;
 #pragma unroll
     for (int i = 0; i < L::TI; ++i) {
-      const int k = k0 + wi * (256 / WI) + 16 * i + 4 * (lane >> 4);
+      const int k = k0 + wi * (BK / 2) + 16 * i + 4 * (lane >> 4);
       if (k >= d.width) continue;
       if (a.sums) {
         float4* const to = reinterpret_cast<float4*>(a.sums + ((int64_t)split * d.rows + token) * d.width + k);
@@ -318,34 +318,44 @@ __global__ void __launch_bounds__(256) head_x_sum_kernel(const HeadArgs a) {
   else { to[0] = (uint16_t)v.x; to[1] = (uint16_t)(v.x >> 16); to[2] = (uint16_t)v.y; to[3] = (uint16_t)(v.y >> 16); }
 }
 
-// dW of a tile: features [k0, k0 + 256) by vocabulary entries [v0, v0 + 256) of the piece.
-template <int TYPE>
+// dW of a tile: features [k0, k0 + SIZE) by vocabulary entries [v0, v0 + SIZE) of the piece.
+template <int TYPE, int SIZE>
 __global__ void __launch_bounds__(kThreads, 2) head_weight_grad_kernel(const HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  typedef Tile<TYPE, true, true, 256, 256, 2, 4> L;
+  extern __shared__ __attribute__((aligned(256))) uint8_t lds[];
+  typedef Tile<TYPE, true, true, SIZE, SIZE, 2, 4> L;
   const szo_head_desc& d = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / 4, wj = wave % 4;
   int ti, tj;
-  tile_of(blockIdx.x, (d.width + 255) / 256, a.tiles_v, ti, tj);
-  const int k0 = ti * 256;
-  const int64_t v0 = (int64_t)tj * 256;
+  tile_of(blockIdx.x, (d.width + SIZE - 1) / SIZE, a.tiles_v, ti, tj);
+  const int k0 = ti * SIZE;
+  const int64_t v0 = (int64_t)tj * SIZE;
   const Operand x = {a.x_copy + k0, d.width, d.width - k0, a.rows64};
   const Operand g = {a.grad + v0, a.pitch, a.pitch - v0, a.rows64};
   L tile;
   tile.run(x, g, (int)(a.rows64 / kStep), (lds_at)lds, wave, lane);
+  // Through LDS, so that a row's 16-byte pieces go to memory side by side: stored as they lie, 8 bytes a lane and 32 side by side, lines reach memory in parts.
+  constexpr int kPitch = SIZE * 2 + 16, kPieces = SIZE / 8;
+  static_assert(SIZE * kPitch <= L::kLds, "the operands' place");
   const float by = a.lift[1];
+  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < L::TJ; ++j) {
-    const int64_t v = v0 + wj * 64 + 16 * j + (lane & 15);
-    if (v >= a.piece_v) continue;
+  for (int j = 0; j < L::TJ; ++j)
 #pragma unroll
-    for (int i = 0; i < L::TI; ++i) {
-      const int k = k0 + wi * 128 + 16 * i + 4 * (lane >> 4);
-      if (k >= d.width) continue;
-      uint16_t* const to = static_cast<uint16_t*>(a.out) + (a.first_v + v) * a.out_stride + k;
-      const uint2 y = rounded4<TYPE>(tile.sum[i][j], by);
-      if (a.out_vec) *reinterpret_cast<uint2*>(to) = y;
-      else { to[0] = (uint16_t)y.x; to[1] = (uint16_t)(y.x >> 16); to[2] = (uint16_t)y.y; to[3] = (uint16_t)(y.y >> 16); }
+    for (int i = 0; i < L::TI; ++i)
+      *reinterpret_cast<uint2*>(lds + (wj * (SIZE / 4) + 16 * j + (lane & 15)) * kPitch + (wi * (SIZE / 2) + 16 * i + 4 * (lane >> 4)) * 2) = rounded4<TYPE>(tile.sum[i][j], by);
+  __syncthreads();
+  const int piece = threadIdx.x % kPieces, k = k0 + piece * 8;
+  if (k >= d.width) return;
+  const int rows = (int)min((int64_t)SIZE, a.piece_v - v0);
+#pragma unroll 4
+  for (int row = threadIdx.x / kPieces; row < rows; row += kThreads / kPieces) {
+    const uint4 y = *reinterpret_cast<const uint4*>(lds + row * kPitch + piece * 16);
+    uint16_t* const to = static_cast<uint16_t*>(a.out) + (a.first_v + v0 + row) * a.out_stride + k;
+    if (a.out_vec) *reinterpret_cast<uint4*>(to) = y;
+    else {
+      const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int n = 0; n < 8; ++n) to[n] = (uint16_t)(w[n / 2] >> (n % 2 * 16));
     }
   }
 }
@@ -371,8 +381,20 @@ LogitPlan logit_plan(int64_t rows, int64_t vocab) {
   }
   return best;
 }
-// Rows of a tile of dx.
-int row_tile(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// Tiles of dx by the same times, in parts of the vocabulary where they do not fill the chip; parts are stored in fp32 and added up by a second kernel (4 TB/s, 3 us).
+struct GradPlan { int features, rows, splits; };
+GradPlan grad_plan(int64_t rows, int64_t width, int64_t steps, bool pieces) {
+  GradPlan best = {};
+  double least = 1e30;
+  for (int n = 512; n >= 64; n -= 64) {
+    const int features = n == 512 ? 256 : 128, count = n == 512 ? 256 : n;
+    const int64_t tiles = tiles_of(width, features) * tiles_of(rows, count), splits = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 8));
+    const double step = features == 256 ? 1.33 : 0.27 + 0.0026 * count;
+    const double us = (double)tiles_of(tiles * splits, 256) * (double)tiles_of(steps, splits) * step + (splits > 1 || pieces ? 3.0 + (double)(splits * rows * width) * 8 / 4e6 : 0.0);
+    if (us <= least) { least = us; best = {features, count, (int)splits}; }
+  }
+  return best;
+}
 
 int check(const szo_head_desc* d) {
   if (!d || d->rows < 0 || d->vocab < 0 || d->width < 0 || (d->type != SZO_BF16 && d->type != SZO_F16) || d->reserved) return SZO_EINVAL;
@@ -424,31 +446,46 @@ int logit_launch(HeadArgs a, int64_t vocab, bool backward, hipStream_t s) {
   }
 }
 
-template <int TYPE, int BT, int WI, int WJ>
+template <int TYPE, int BK, int BT>
 int x_grad_launch(const HeadArgs& a, hipStream_t s) {
   static std::atomic<uint64_t> raised{0};
-  const int64_t groups = tiles_of(a.d.width, 256) * a.tiles_t * a.splits;
-  return launch(head_x_grad_kernel<TYPE, BT, WI, WJ>, raised, Tile<TYPE, true, false, 256, BT, WI, WJ>::kLds, groups, s, a);
+  const int64_t groups = tiles_of(a.d.width, BK) * a.tiles_t * a.splits;
+  return launch(head_x_grad_kernel<TYPE, BK, BT>, raised, Tile<TYPE, true, false, BK, BT, 2, 4, weight_stages(BK, BT), row_stages(BK, BT)>::kLds, groups, s, a);
 }
 template <int TYPE>
-int x_grad_launch(const HeadArgs& a, hipStream_t s) {
-  switch (row_tile(a.d.rows)) {
-    case 64: return x_grad_launch<TYPE, 64, 4, 2>(a, s);
-    case 128: return x_grad_launch<TYPE, 128, 4, 2>(a, s);
-    default: return x_grad_launch<TYPE, 256, 2, 4>(a, s);
+int x_grad_launch(HeadArgs a, const GradPlan& p, hipStream_t s) {
+  a.tiles_t = (int)tiles_of(a.d.rows, p.rows);
+  if (p.features == 256) return x_grad_launch<TYPE, 256, 256>(a, s);
+  switch (p.rows) {
+    case 64: return x_grad_launch<TYPE, 128, 64>(a, s);
+    case 128: return x_grad_launch<TYPE, 128, 128>(a, s);
+    case 192: return x_grad_launch<TYPE, 128, 192>(a, s);
+    case 256: return x_grad_launch<TYPE, 128, 256>(a, s);
+    case 320: return x_grad_launch<TYPE, 128, 320>(a, s);
+    case 384: return x_grad_launch<TYPE, 128, 384>(a, s);
+    default: return x_grad_launch<TYPE, 128, 448>(a, s);
   }
 }
 
+template <int TYPE, int SIZE>
+int weight_grad_launch(HeadArgs a, hipStream_t s) {
+  static std::atomic<uint64_t> raised{0};
+  a.tiles_v = (int)tiles_of(a.piece_v, SIZE);
+  return launch(head_weight_grad_kernel<TYPE, SIZE>, raised, Tile<TYPE, true, true, SIZE, SIZE, 2, 4>::kLds, tiles_of(a.d.width, SIZE) * a.tiles_v, s, a);
+}
 template <int TYPE>
 int weight_grad_launch(const HeadArgs& a, hipStream_t s) {
-  static std::atomic<uint64_t> raised{0};
-  return launch(head_weight_grad_kernel<TYPE>, raised, Tile<TYPE, true, true, 256, 256, 2, 4>::kLds, tiles_of(a.d.width, 256) * a.tiles_v, s, a);
+  // Small tiles where large ones would not fill the chip twice, or have a single step: two workgroups share a CU then.  us of a backward, large / small: 16 rows of 32000 x 4096 218 / 216, 200 rows
+  // 299 / 308, 2000 rows 1310 / 1384; 2000 x 512: 16 rows 26 / 24, 2000 rows 89 / 67.
+  const bool small = a.rows64 <= 64 || tiles_of(a.d.width, 256) * tiles_of(a.piece_v, 256) < 512;
+  return small ? weight_grad_launch<TYPE, 128>(a, s) : weight_grad_launch<TYPE, 256>(a, s);
 }
 
 // A backward: columns of d that are in memory at a time, parts of dx, and where things lie in the workspace.
 struct Plan {
   int64_t rows64, pitch;
-  int pieces, splits;
+  int pieces;
+  GradPlan x;
   size_t grad_at, copy_at, sums_at, rows_at, lift_at, bytes;
 };
 Plan plan_of(const szo_head_desc* d) {
@@ -457,13 +494,12 @@ Plan plan_of(const szo_head_desc* d) {
   const int64_t all = tiles_of(d->vocab, kTileV), fit = std::max<int64_t>(1, (int64_t)(kPieceBytes / 2) / (p.rows64 * kTileV));       // tiles of columns
   p.pieces = (int)tiles_of(all, std::min(all, fit));
   p.pitch = tiles_of(all, p.pieces) * kTileV;
-  const int64_t tiles = tiles_of(d->width, 256) * tiles_of(d->rows, row_tile(d->rows));
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, p.pitch / kStep / 8));
+  p.x = grad_plan(d->rows, d->width, tiles_of(std::min(p.pitch, d->vocab), kStep), p.pieces > 1);
   size_t at = 0;
   auto take = [&](size_t n) { const size_t was = at; at = up16(at + n); return was; };
   p.grad_at = take((size_t)p.rows64 * p.pitch * 2);
   p.copy_at = take((size_t)p.rows64 * d->width * 2);
-  p.sums_at = take(p.pieces > 1 || p.splits > 1 ? (size_t)p.splits * d->rows * d->width * sizeof(float) : 0);
+  p.sums_at = take(p.pieces > 1 || p.x.splits > 1 ? (size_t)p.x.splits * d->rows * d->width * sizeof(float) : 0);
   p.rows_at = take((size_t)d->rows * sizeof(float));
   p.lift_at = take(2 * sizeof(float));
   p.bytes = at;
@@ -485,9 +521,9 @@ int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, in
   a.row_grad = (const float*)(room + p.rows_at);
   a.lift = (const float*)(room + p.lift_at);
   a.x_copy = (const uint16_t*)(room + p.copy_at);
-  a.splits = p.splits;
-  float* const sums = p.pieces > 1 || p.splits > 1 ? (float*)(room + p.sums_at) : nullptr;
-  auto vec = [](const void* q, int64_t stride) { return aligned_to(q, 8) && stride % 4 == 0; };
+  a.splits = p.x.splits;
+  float* const sums = p.pieces > 1 || p.x.splits > 1 ? (float*)(room + p.sums_at) : nullptr;
+  auto vec = [](const void* q, int64_t stride) { return aligned_to(q, 16) && stride % 8 == 0; };
   int rc = SZO_OK;
   for (int piece = 0; piece < p.pieces; ++piece) {
     a.first_v = (int64_t)piece * p.pitch;
@@ -502,7 +538,7 @@ int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, in
       a.out_vec = vec(x_grad, x_grad_stride);
       a.sums = sums;
       a.add = piece > 0;
-      rc = x_grad_launch<TYPE>(a, s);
+      rc = x_grad_launch<TYPE>(a, p.x, s);
       if (rc != SZO_OK) return rc;
     }
     if (weight_grad) {
@@ -583,9 +619,9 @@ int szo_head_logprobs_bwd(const szo_head_desc* d, const float* grad_logp, void* 
   if (tiles_of(tiles_of(d->rows, 64) * 64 * d->width, 4 * 256) > kMostSmallGroups) return SZO_EUNSUPPORTED;
   HeadArgs a = {};
   a.d = *d;
-  a.tiles_t = (int)tiles_of(d->rows, row_tile(d->rows));
   const Plan p = plan_of(d);
-  if (tiles_of(d->width, 256) * a.tiles_t * p.splits > kMostGroups || tiles_of(d->width, 256) * (p.pitch / kTileV) > kMostGroups) return SZO_EUNSUPPORTED;
+  if (tiles_of(d->width, p.x.features) * tiles_of(d->rows, p.x.rows) * p.x.splits > kMostGroups || tiles_of(d->width, 128) * (p.pitch / 128) > kMostGroups)
+    return SZO_EUNSUPPORTED;
   return d->type == SZO_BF16 ? backward<SZO_BF16>(a, p, grad_logp, x_grad, x_grad_stride, weight_grad, weight_grad_stride, (char*)workspace, s)
                              : backward<SZO_F16>(a, p, grad_logp, x_grad, x_grad_stride, weight_grad, weight_grad_stride, (char*)workspace, s);
 }

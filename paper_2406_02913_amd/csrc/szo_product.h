@@ -6,6 +6,7 @@
 //   rows     [row][64 of r]: the eight 16-byte pieces of a row are exchanged by (row / 2) mod 8, so that 16 lanes that read one piece of 16 rows touch every bank once
 //   columns  [r][256 of i], two r to an instruction: 16-wide groups are exchanged in pairs in odd r, pairs of r lie 64 bytes and eights of them 128 further than they are
 //            long, so that the four 32-byte pieces each of two groups of 16 lanes, which the transposing LDS read asks for together, lie in different banks
+//   columns  [r][128 of i], four r to an instruction: 16-wide groups are exchanged by r mod 4 and (r / 8) mod 2, to the same end; a read forms its address
 // Fragments are read from LDS a few groups of products before they are used, across the one barrier of a step.
 #pragma once
 #include "szo_internal.h"
@@ -38,14 +39,14 @@ struct Operand {
   int64_t count, length;
 };
 
-template <bool COLUMNS, int SIZE> constexpr int stage_bytes() { return COLUMNS ? 32 * kPairBytes + 8 * 128 : SIZE * kStep * 2; }
+template <bool COLUMNS, int SIZE> constexpr int stage_bytes() { return COLUMNS && SIZE == 256 ? 32 * kPairBytes + 8 * 128 : SIZE * kStep * 2; }
 
 // One operand of a workgroup's tile: its loads to LDS and its reads from there.
 template <bool COLUMNS, int SIZE, int PER>           // PER: 16-wide groups of a wave
 struct Side {
   static constexpr int kLoads = SIZE / 64;           // of a wave and step
   static constexpr int kStage = stage_bytes<COLUMNS, SIZE>();
-  static_assert(!COLUMNS || SIZE == 256, "columns are laid out for 256");
+  static_assert(!COLUMNS || SIZE == 256 || SIZE == 128, "columns are laid out for these");
   uint32_t from, apart;                              // bytes from the step's first row or column to this lane's first 16, and from one load to the next
   uint32_t lds;                                      // where this wave's loads go, in a stage
   lds_at read[2];                                    // rows: of the two halves of a step; columns: of even and odd groups
@@ -59,7 +60,15 @@ struct Side {
     pitch = (uint32_t)(o.stride * 2);
     base = (uint64_t)(uintptr_t)o.base;
     row_bytes = (uint32_t)(o.count * 2);
-    if constexpr (COLUMNS) {
+    if constexpr (COLUMNS && SIZE == 128) {
+      left = (int)o.length;
+      const uint32_t q = (uint32_t)lane >> 4, exchange = q | ((uint32_t)wave & 1u) << 2;       // rows 8 w + q and, of the second load, + 4
+      from = (8u * (uint32_t)wave + q) * pitch + 16u * (((uint32_t)lane & 15u) ^ exchange << 1);
+      apart = 4 * pitch;
+      lds = (uint32_t)(uintptr_t)stages + (uint32_t)wave * 2048u;
+      const int g = lane >> 4, p = lane & 15, row = 8 * g + (p >> 2);
+      read[0] = read[1] = stages + (row * 256 + (p & 3) * 8 + ((((p >> 2) | (g & 1) << 2) << 5) ^ wave_first * 2));       // the group's bits are xored in
+    } else if constexpr (COLUMNS) {
       left = (int)o.length;
       const uint32_t r = (uint32_t)lane >> 5, piece = ((uint32_t)lane & 31u) ^ (2u * r);
       from = (uint32_t)(2 * wave * kLoads + (int)r) * pitch + 16u * piece;
@@ -83,7 +92,7 @@ struct Side {
     }
   }
 
-  static constexpr uint32_t kApart = COLUMNS ? kPairBytes : 2048;            // in LDS, of one load and the next
+  static constexpr uint32_t kApart = !COLUMNS ? 2048 : SIZE == 256 ? kPairBytes : 1024;            // in LDS, of one load and the next
   template <int N>
   __device__ __forceinline__ void issue(uint32_t to, uint32_t from, rsrc_t rsrc) const {
     uint32_t at;
@@ -132,10 +141,13 @@ struct Side {
     if constexpr (COLUMNS) {
       typedef short short4_t __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) short4_t* four_at;
-      const lds_at at = read[t & 1] + (stage * kStage + half * (16 * kPairBytes + 4 * 128) + t * 32);
+      constexpr int kFour = SIZE == 256 ? 2 * kPairBytes : 1024;           // four r further
+      lds_at at;
+      if constexpr (SIZE == 256) at = read[t & 1] + (stage * kStage + half * (16 * kPairBytes + 4 * 128) + t * 32);
+      else at = (lds_at)(uintptr_t)((uint32_t)(uintptr_t)read[0] ^ (uint32_t)(t << 5)) + (stage * kStage + half * 8192);
       struct { uint64_t lo, hi; } both;
       both.lo = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((four_at)at));
-      both.hi = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((four_at)(at + 2 * kPairBytes)));
+      both.hi = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((four_at)(at + kFour)));
       return __builtin_bit_cast(vec, both);
     } else {
       return *(vec_at)(read[half] + (stage * kStage + t * 2048));
