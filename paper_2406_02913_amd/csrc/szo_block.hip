@@ -48,9 +48,14 @@ __device__ __forceinline__ Raw fetch(const void* base, int type, int64_t row, co
   Raw r = {};
   if constexpr (VEC) {
     if (base && p.first < p.width) {
-      const char* at = static_cast<const char*>(base) + (row + p.first) * (type == SZO_F32 ? 4 : 2);
-      r.a = *reinterpret_cast<const words4*>(at);
-      if (type == SZO_F32) r.b = *reinterpret_cast<const words4*>(at + 16);
+      if (type == SZO_F32) {
+        const char* at = static_cast<const char*>(base) + row * 4;         // the same for the wave: a lane's part of the address stays 32 bits
+        r.a = *reinterpret_cast<const words4*>(at + (uint32_t)p.first * 4u);
+        r.b = *reinterpret_cast<const words4*>(at + (uint32_t)p.first * 4u + 16u);
+      } else {
+        const char* at = static_cast<const char*>(base) + row * 2;
+        r.a = *reinterpret_cast<const words4*>(at + (uint32_t)p.first * 2u);
+      }
     }
   } else {
     float v[8];
@@ -87,7 +92,8 @@ __device__ __forceinline__ void widen(const Raw& r, int type, float (&v)[8]) {
 template <bool VEC, int TYPE>
 __device__ __forceinline__ void put_as(void* base, int64_t row, const Place<VEC>& p, const float (&v)[8]) {
   if constexpr (VEC) {
-    if (p.first < p.width) store_f32<TYPE, 8, true>(base, row + p.first, v);
+    typedef typename TypeOf<TYPE>::type T;
+    if (p.first < p.width) store_f32<TYPE, 8, true>(static_cast<T*>(base) + row, (int64_t)(uint32_t)p.first, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -119,22 +125,49 @@ __device__ __forceinline__ void factor(const float* base, int64_t row, const Pla
 struct Meeting {
   float (*slots)[kMostWaves][2];     // [exchange][wave]
   int waves, wave, first;            // waves of a row, this one, first one of the row
+  float count;                       // features of the wave that this lane adds up for, lane modulo 16; 0: none
 };
 
-// Sums of two values over a row.
+// Sum over 32 lanes, in every lane of them.
+__device__ __forceinline__ float half_sum(float v) {
+  v = lanes_sum<16>(v);
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+#endif
+  return v;
+}
+__device__ __forceinline__ float from_lane(float v, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
+
+// Sums of two values over a row, each in half of the lanes; sixteen lanes take a wave's each where waves meet.
 __device__ __forceinline__ void row_sums(const Meeting& m, int slot, float& a, float& b) {
+  float v = 0.f;
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  v = half_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+#endif
+  if (m.waves > 1) {
+    const int lane = threadIdx.x % 64, other = lane % 16, half = lane / 32;
+    if (lane % 32 == 0) m.slots[slot][m.first + m.wave][half] = v;
+    __syncthreads();
+    v = lanes_sum<16>(other < m.waves ? m.slots[slot][m.first + other][half] : 0.f);
+  }
+  a = from_lane(v, 0);
+  b = from_lane(v, 32);
+}
+// Sum of one value.
+__device__ __forceinline__ void row_sum(const Meeting& m, int slot, float& a) {
   a = lanes_sum<64>(a);
-  b = lanes_sum<64>(b);
   if (m.waves == 1) return;
-  if (threadIdx.x % 64 == 0) { m.slots[slot][m.first + m.wave][0] = a; m.slots[slot][m.first + m.wave][1] = b; }
+  const int lane = threadIdx.x % 64, other = lane % 16;
+  if (lane == 0) m.slots[slot][m.first + m.wave][0] = a;
   __syncthreads();
-  a = b = 0.f;
-  for (int w = 0; w < m.waves; ++w) { a += m.slots[slot][m.first + w][0]; b += m.slots[slot][m.first + w][1]; }
+  a = lanes_sum<16>(other < m.waves ? m.slots[slot][m.first + other][0] : 0.f);
 }
 
-// Mean (0 for RMS norms) and 1 / sqrt(var + eps) of a row.  `count`: features of this wave.
+// Mean (0 for RMS norms) and 1 / sqrt(var + eps) of a row whose places behind the end hold 0.  `own`: features of this wave.
 template <int CH, bool VEC>
-__device__ __forceinline__ void row_stats(const Meeting& m, int slot, const float (&v)[CH][8], const Place<VEC> (&at)[CH], bool layer, int width, float eps,
+__device__ __forceinline__ void row_stats(const Meeting& m, int slot, const float (&v)[CH][8], const Place<VEC> (&at)[CH], bool layer, float own, float inverse_width, float eps,
                                           float& mean, float& r) {
   float square = 0.f;
   if (!layer) {
@@ -143,65 +176,60 @@ __device__ __forceinline__ void row_stats(const Meeting& m, int slot, const floa
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) square = fmaf(v[c][i], v[c][i], square);
-    float unused = 0.f;
-    row_sums(m, slot, square, unused);
+    row_sum(m, slot, square);
   } else {
-    float count = 0.f, sum = 0.f;
+    float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { count += at[c].on(i) ? 1.f : 0.f; sum += v[c][i]; }
-    count = lanes_sum<64>(count);
-    mean = lanes_sum<64>(sum) / fmaxf(count, 1.f);
+      for (int i = 0; i < 8; ++i) sum += v[c][i];
+    mean = lanes_sum<64>(sum) / fmaxf(own, 1.f);
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+      const float about = at[c].on(0) ? mean : 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = at[c].on(i) ? v[c][i] - mean : 0.f;
+        const float x = v[c][i] - (VEC ? about : at[c].on(i) ? mean : 0.f);
         square = fmaf(x, x, square);
       }
+    }
     square = lanes_sum<64>(square);
     if (m.waves > 1) {
-      // a wave's count follows from the width: only the two others are exchanged, the counts are added up again from the places
-      if (threadIdx.x % 64 == 0) { m.slots[slot][m.first + m.wave][0] = mean; m.slots[slot][m.first + m.wave][1] = square; }
+      const int lane = threadIdx.x % 64, other = lane % 16;
+      if (lane == 0) { m.slots[slot][m.first + m.wave][0] = mean; m.slots[slot][m.first + m.wave][1] = square; }
       __syncthreads();
-      float all = 0.f;
-      for (int w = 0; w < m.waves; ++w) {
-        float n = 0.f;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          // features of wave w in chunk c: neighbours with VEC, else eight runs of 64
-          if (VEC) n += (float)min(max(width - (c * m.waves + w) * 512, 0), 512);
-          else
-            for (int i = 0; i < 8; ++i) n += (float)min(max(width - ((c * 8 + i) * m.waves + w) * 64, 0), 64);
-        }
-        all = fmaf(n, m.slots[slot][m.first + w][0], all);
-      }
-      mean = all / (float)width;
-      square = 0.f;
-      for (int w = 0; w < m.waves; ++w) {
-        float n = 0.f;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          if (VEC) n += (float)min(max(width - (c * m.waves + w) * 512, 0), 512);
-          else
-            for (int i = 0; i < 8; ++i) n += (float)min(max(width - ((c * 8 + i) * m.waves + w) * 64, 0), 64);
-        }
-        const float off = m.slots[slot][m.first + w][0] - mean;
-        square += fmaf(n * off, off, m.slots[slot][m.first + w][1]);
-      }
+      const bool there = other < m.waves;
+      const float its = there ? m.slots[slot][m.first + other][0] : 0.f, squares = there ? m.slots[slot][m.first + other][1] : 0.f;
+      mean = lanes_sum<16>(m.count * its) * inverse_width;
+      const float off = its - mean;
+      square = lanes_sum<16>(there ? fmaf(m.count * off, off, squares) : 0.f);
     }
   }
-  r = 1.f / sqrtf(square / (float)width + eps);
+  r = 1.f / sqrtf(square * inverse_width + eps);
 }
 
 // unit = (v - mean) r, and 0 behind the row's end
 template <int CH, bool VEC>
 __device__ __forceinline__ void to_unit(float (&v)[CH][8], const Place<VEC> (&at)[CH], float mean, float r) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
+    const float about = at[c].on(0) ? mean : 0.f, by = at[c].on(0) ? r : 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = at[c].on(i) ? (v[c][i] - mean) * r : 0.f;
+    for (int i = 0; i < 8; ++i) v[c][i] = VEC ? (v[c][i] - about) * by : at[c].on(i) ? (v[c][i] - mean) * r : 0.f;
+  }
+}
+
+// Features of a wave of a row: neighbours with VEC, else runs of 64.
+template <int CH, bool VEC>
+__device__ __forceinline__ float features_of(int wave, int waves, int width) {
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if (VEC) n += min(max(width - (c * waves + wave) * 512, 0), 512);
+    else
+      for (int i = 0; i < 8; ++i) n += min(max(width - ((c * 8 + i) * waves + wave) * 64, 0), 64);
+  }
+  return (float)n;
 }
 
 template <int CH, bool VEC>
@@ -210,13 +238,14 @@ __device__ __forceinline__ void find_places(Place<VEC> (&p)[CH], int thread, int
   for (int c = 0; c < CH; ++c) p[c] = Place<VEC>(c, thread, threads, width);
 }
 
-template <int CH, bool VEC, int THREADS>
+template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
 __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs args) {
   __shared__ float slots[2][kMostWaves][2];
   const szo_block_desc& d = args.d;
   const int waves = args.waves, threads = waves * 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int row = wave / waves, thread = threadIdx.x - row * threads;
-  const Meeting m = {slots, waves, wave - row * waves, row * waves};
+  const float inverse = 1.f / (float)d.width, own = features_of<CH, VEC>(wave - row * waves, waves, d.width);
+  const Meeting m = {slots, waves, wave - row * waves, row * waves, (int)(threadIdx.x % 16) < waves ? features_of<CH, VEC>(threadIdx.x % 16, waves, d.width) : 0.f};
   const int64_t token = (int64_t)blockIdx.x * (blockDim.x / threads) + row;
   const bool there = token < d.tokens;                      // rows that are not still take part in the barriers
   Place<VEC> p[CH];
@@ -230,9 +259,9 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs arg
   float y[CH][8], h[CH][8], w[8], b[8];
 #pragma unroll
   for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
-  if (d.y && d.post) {
+  if (POST) {                                               // then there is a block's output
     float mean, r;
-    row_stats<CH, VEC>(m, 0, y, p, d.norm == SZO_NORM_LAYER, d.width, d.eps, mean, r);
+    row_stats<CH, VEC>(m, 0, y, p, LAYER, own, inverse, d.eps, mean, r);
     to_unit<CH, VEC>(y, p, mean, r);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -252,7 +281,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs arg
   }
   if (!d.x_out) return;
   float mean, r;
-  row_stats<CH, VEC>(m, 1, h, p, d.norm == SZO_NORM_LAYER, d.width, d.eps, mean, r);
+  row_stats<CH, VEC>(m, 1, h, p, LAYER, own, inverse, d.eps, mean, r);
   to_unit<CH, VEC>(h, p, mean, r);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -265,16 +294,15 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs arg
 }
 
 // A workgroup walks rows and keeps what it adds up over them in registers, eight features of up to five sums a thread; no atomics, so the order is fixed.
-template <int CH, bool VEC, int THREADS>
+template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
 __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 : 1) block_norm_bwd_kernel(const BlockArgs args) {
   __shared__ float slots[4][kMostWaves][2];
   const szo_block_desc& d = args.d;
   const szo_block_grads& g = args.g;
   const int waves = args.waves, threads = waves * 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rows = blockDim.x / threads, row = wave / waves, thread = threadIdx.x - row * threads;
-  const Meeting m = {slots, waves, wave - row * waves, row * waves};
-  const bool layer = d.norm == SZO_NORM_LAYER, post = d.y && d.post;
-  const float inverse = 1.f / (float)d.width;
+  const float inverse = 1.f / (float)d.width, own = features_of<CH, VEC>(wave - row * waves, waves, d.width);
+  const Meeting m = {slots, waves, wave - row * waves, row * waves, (int)(threadIdx.x % 16) < waves ? features_of<CH, VEC>(threadIdx.x % 16, waves, d.width) : 0.f};
   float sums[kSets][CH][8];
 #pragma unroll
   for (int s = 0; s < kSets; ++s)
@@ -295,13 +323,27 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
       gx_raw[c] = fetch<VEC>(g.x_out_grad, d.x_type, token * g.x_out_stride, p[c]);
       gh_raw[c] = fetch<VEC>(g.h_out_grad, d.h_type, token * g.h_out_stride, p[c]);
     }
-    float y[CH][8], gh[CH][8], w[8], b[8], y_r = 0.f;
+    float y[CH][8], gh[CH][8], a[CH][8], gate[CH][8], w[CH][8], y_r = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
-    if (post) {
+    if (POST) {
       float mean;
-      row_stats<CH, VEC>(m, 0, y, p, layer, d.width, d.eps, mean, y_r);
+      row_stats<CH, VEC>(m, 0, y, p, LAYER, own, inverse, d.eps, mean, y_r);
       to_unit<CH, VEC>(y, p, mean, y_r);
+    }
+    if (d.y) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        float b[8];
+        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate[c]);
+        factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w[c]);
+        factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          a[c][i] = fmaf(y[c][i], w[c][i], b[i]);
+          gate[c][i] *= d.y_scale;
+        }
+      }
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) widen<VEC>(gh_raw[c], d.h_type, gh[c]);
@@ -310,81 +352,72 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         widen<VEC>(h_raw[c], d.h_type, h[c]);
-        float a[8], gate[8];
-        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
-        factor<VEC>(post ? d.post_weight : nullptr, 0, p[c], 1.f, w);
-        factor<VEC>(post ? d.post_bias : nullptr, 0, p[c], 0.f, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          a[i] = fmaf(y[c][i], w[i], b[i]);
-          h[c][i] = d.y ? fmaf(d.y_scale * gate[i], a[i], d.h_scale * h[c][i]) : d.h_scale * h[c][i];
-        }
+        for (int i = 0; i < 8; ++i) h[c][i] = d.y ? fmaf(gate[c][i], a[c][i], d.h_scale * h[c][i]) : d.h_scale * h[c][i];
       }
-      row_stats<CH, VEC>(m, 1, h, p, layer, d.width, d.eps, mean, r);
+      row_stats<CH, VEC>(m, 1, h, p, LAYER, own, inverse, d.eps, mean, r);
       to_unit<CH, VEC>(h, p, mean, r);
       if (!there) r = 0.f;                                  // with eps 0 it is infinite, and nothing times it would be NaN in the sums
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        float pre[8];
         widen<VEC>(gx_raw[c], d.x_type, u[c]);
-        factor<VEC>(d.pre_weight, 0, p[c], 1.f, w);
+        factor<VEC>(d.pre_weight, 0, p[c], 1.f, pre);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPreWeight][c][i] = fmaf(u[c][i], h[c][i], sums[kPreWeight][c][i]);
           sums[kPreBias][c][i] += u[c][i];
-          u[c][i] *= w[i];
+          u[c][i] *= pre[i];
           sum += u[c][i];
           dot = fmaf(u[c][i], h[c][i], dot);
         }
       }
       row_sums(m, 2, sum, dot);
-      sum = layer ? sum * inverse : 0.f;
+      sum = LAYER ? sum * inverse : 0.f;
       dot *= inverse;
 #pragma unroll
       for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) gh[c][i] = fmaf(r, u[c][i] - sum - h[c][i] * dot, gh[c][i]);
+        for (int i = 0; i < 8; ++i) gh[c][i] = fmaf(r, fmaf(-h[c][i], dot, u[c][i] - sum), gh[c][i]);
     }
     if (g.h_grad) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        float to[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = d.h_scale * gh[c][i];
-        put<VEC>(g.h_grad, d.h_type, token * g.h_stride, p[c], w);
+        for (int i = 0; i < 8; ++i) to[i] = d.h_scale * gh[c][i];
+        put<VEC>(g.h_grad, d.h_type, token * g.h_stride, p[c], to);
       }
     }
     if (!d.y) continue;
-    // from here on gh is the gradient by what the residual stream was given, then by the norm's output, then by its input
+    // from here on gh is the gradient by the norm's output, then by its input; the gate holds y_scale
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float gate[8], into[8];
-      factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
-      factor<VEC>(post ? d.post_weight : nullptr, 0, p[c], 1.f, w);
-      factor<VEC>(post ? d.post_bias : nullptr, 0, p[c], 0.f, b);
+      float into[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float t = d.y_scale * gh[c][i];
-        into[i] = t * fmaf(y[c][i], w[i], b[i]);
+        into[i] = d.y_scale * gh[c][i] * a[c][i];
         sums[kGate][c][i] += into[i];
-        gh[c][i] = t * gate[i];
+        gh[c][i] *= gate[c][i];
         sums[kPostWeight][c][i] = fmaf(gh[c][i], y[c][i], sums[kPostWeight][c][i]);
         sums[kPostBias][c][i] += gh[c][i];
-        if (post) {
-          gh[c][i] *= w[i];
+        if (POST) {
+          gh[c][i] *= w[c][i];
           sum += gh[c][i];
           dot = fmaf(gh[c][i], y[c][i], dot);
         }
       }
       if (g.gate_grad && d.gate_stride) put<VEC>(g.gate_grad, SZO_F32, token * g.gate_stride, p[c], into);
     }
-    if (post) {
+    if (POST) {
       row_sums(m, 3, sum, dot);
-      sum = layer ? sum * inverse : 0.f;
+      sum = LAYER ? sum * inverse : 0.f;
       dot *= inverse;
 #pragma unroll
       for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) gh[c][i] = y_r * (gh[c][i] - sum - y[c][i] * dot);
+        for (int i = 0; i < 8; ++i) gh[c][i] = y_r * fmaf(-y[c][i], dot, gh[c][i] - sum);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) put<VEC>(g.y_grad, d.y_type, token * g.y_stride, p[c], gh[c]);
@@ -463,17 +496,23 @@ bool inputs_vec(const szo_block_desc* d) {
          aligned_to(d->post_weight, 16) && aligned_to(d->post_bias, 16) && aligned_to(d->pre_weight, 16) && aligned_to(d->pre_bias, 16);
 }
 
-template <int CH, bool VEC, int THREADS>
+template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
 void launch(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
   const int threads = 64 * a.waves * rows_of(a.waves);
-  if (backward) block_norm_bwd_kernel<CH, VEC, THREADS><<<dim3((unsigned)groups), threads, 0, s>>>(a);
-  else block_norm_kernel<CH, VEC, THREADS><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+  if (backward) block_norm_bwd_kernel<CH, VEC, THREADS, LAYER, POST><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+  else block_norm_kernel<CH, VEC, THREADS, LAYER, POST><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+}
+template <int CH, bool VEC, int THREADS>
+void launch_norm(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+  const bool layer = a.d.norm == SZO_NORM_LAYER, post = a.d.y && a.d.post;
+  if (layer) post ? launch<CH, VEC, THREADS, true, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, true, false>(a, groups, backward, s);
+  else post ? launch<CH, VEC, THREADS, false, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, false, false>(a, groups, backward, s);
 }
 template <bool VEC>
 void launch_all(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
-  if (a.d.width <= 4096) launch<1, VEC, 512>(a, groups, backward, s);
-  else if (a.d.width <= 8192) launch<2, VEC, 512>(a, groups, backward, s);
-  else launch<2, VEC, 1024>(a, groups, backward, s);
+  if (a.d.width <= 4096) launch_norm<1, VEC, 512>(a, groups, backward, s);
+  else if (a.d.width <= 8192) launch_norm<2, VEC, 512>(a, groups, backward, s);
+  else launch_norm<2, VEC, 1024>(a, groups, backward, s);
 }
 
 }  // namespace

@@ -170,38 +170,40 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
 
-// scale * gradient of each row, lifted for fp16 by the power of two that takes the largest to 2^13 .. 2^14: with |1 - p| <= 1 nothing overflows, and what is
-// 2^-27 of the largest still has all its bits.
-__global__ void __launch_bounds__(1024) head_rows_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* lift) {
-  __shared__ float part[16];
+// The first workgroup: scale * gradient of each row, lifted for fp16 by the power of two that takes the largest to 2^13 .. 2^14: with |1 - p| <= 1 nothing overflows, and what is
+// 2^-27 of the largest still has all its bits.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
+__global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* lift, int64_t rows64, uint16_t* x_copy) {
+  if (blockIdx.x > 0) {
+    const int per = d.width / 8;
+    const int64_t i = (int64_t)(blockIdx.x - 1) * 256 + threadIdx.x, row = i / per, at = i % per * 8;
+    if (row >= rows64) return;
+    const int64_t target = row < d.rows && d.targets ? d.targets[row] : -1;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (target >= 0 && target < d.vocab) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + row * d.x_stride + at);
+    *reinterpret_cast<uint4*>(x_copy + row * d.width + at) = v;
+    return;
+  }
+  __shared__ float part[4];
   float most = 0.f;
   auto of = [&](int64_t i) {
     const int64_t t = d.targets ? d.targets[i] : -1;
     return t >= 0 && t < d.vocab ? grad[i] * d.scale : 0.f;
   };
-  for (int64_t i = threadIdx.x; i < d.rows; i += 1024) {
-    const float g = fabsf(of(i));
-    if (g < __builtin_inff()) most = fmaxf(most, g);
-  }
+  if (d.type == SZO_F16)
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
+      const float g = fabsf(of(i));
+      if (g < __builtin_inff()) most = fmaxf(most, g);
+    }
   most = lanes_max<64>(most);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
   __syncthreads();
-  for (int w = 0; w < 16; ++w) most = fmaxf(most, part[w]);
-  const int up = d.type == SZO_F16 && most > 0.f ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
+  for (int w = 0; w < 4; ++w) most = fmaxf(most, part[w]);
+  const int up = most > 0.f ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
   const float by = __builtin_amdgcn_ldexpf(1.f, up);
-  for (int64_t i = threadIdx.x; i < d.rows; i += 1024) row_grad[i] = of(i) * by;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < d.rows; i += 256) row_grad[i] = of(i) * by;
   if (threadIdx.x == 0) { lift[0] = by; lift[1] = __builtin_amdgcn_ldexpf(1.f, -up); }
-}
-
-// x with rows that have no target as 0: they may hold anything, and 0 times infinity would reach the weight's gradient.
-__global__ void __launch_bounds__(256) head_copy_kernel(const szo_head_desc d, int64_t rows64, uint16_t* out) {
-  const int per = d.width / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per, at = i % per * 8;
-  if (row >= rows64) return;
-  const int64_t target = row < d.rows && d.targets ? d.targets[row] : -1;
-  uint4 v = make_uint4(0, 0, 0, 0);
-  if (target >= 0 && target < d.vocab) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + row * d.x_stride + at);
-  *reinterpret_cast<uint4*>(out + row * d.width + at) = v;
 }
 
 // Rows of nothing.
@@ -509,12 +511,9 @@ Plan plan_of(const szo_head_desc* d) {
 template <int TYPE>
 int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad, int64_t weight_grad_stride, char* room, hipStream_t s) {
   const szo_head_desc& d = a.d;
-  head_rows_kernel<<<1, 1024, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.lift_at));
+  const int64_t copies = weight_grad ? tiles_of(p.rows64 * (d.width / 8), 256) : 0;
+  head_prepare_kernel<<<dim3((unsigned)(1 + copies)), 256, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.lift_at), p.rows64, (uint16_t*)(room + p.copy_at));
   SZO_LAUNCH_CHECK();
-  if (weight_grad) {
-    head_copy_kernel<<<dim3((unsigned)tiles_of(p.rows64 * (d.width / 8), 256)), 256, 0, s>>>(d, p.rows64, (uint16_t*)(room + p.copy_at));
-    SZO_LAUNCH_CHECK();
-  }
   a.rows64 = p.rows64;
   a.pitch = p.pitch;
   a.grad = (uint16_t*)(room + p.grad_at);
@@ -616,7 +615,7 @@ int szo_head_logprobs_bwd(const szo_head_desc* d, const float* grad_logp, void* 
   }
   if (!d->stats || !grad_logp || !workspace || !aligned_to(workspace, 16)) return SZO_EINVAL;
   if (!x_grad && !weight_grad) return SZO_OK;
-  if (tiles_of(tiles_of(d->rows, 64) * 64 * d->width, 4 * 256) > kMostSmallGroups) return SZO_EUNSUPPORTED;
+  if (tiles_of(tiles_of(d->rows, 64) * 64 * d->width, 4 * 256) >= kMostSmallGroups) return SZO_EUNSUPPORTED;
   HeadArgs a = {};
   a.d = *d;
   const Plan p = plan_of(d);
