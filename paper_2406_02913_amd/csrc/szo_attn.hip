@@ -25,7 +25,6 @@ namespace {
 constexpr int kThreads = 256;              // of the joining kernel
 constexpr int64_t kMostGroups = 0xFFFFFFFFll / 512;      // a launch counts its threads in 32 bits
 constexpr float kNone = -3.402823466e38f;  // running maximum of a row that has seen nothing: the lowest finite value, so that differences stay defined
-constexpr float kAbsent = __builtin_inff();      // in place of a maximum: a tile's row that is nobody's
 constexpr float kSlack = 4.f;              // the maximum may fall behind by this many binary places before sums are scaled
 constexpr float kLift = 11.f;              // weights are held times 2^11: up to 2^15 with the slack, and all 11 bits of fp16 down to 2^-25 of the largest
 // The denominator is held times 2^40 beside that.  Its largest term is the one of the block with exponent e that sets the maximum, 2^(51 - e), from 2^-73 (with the slack)
@@ -67,6 +66,16 @@ struct SharedArgs {
 // A part's sums: rows_cap rows of head_dim numerators, then maximum (two floats) and denominator of each.  A multiple of 16 bytes, which rows are stored
 // and read in.
 __host__ __device__ constexpr int part_floats(int rows_cap, int head_dim) { return (rows_cap * (head_dim + 3) + 3) / 4 * 4; }
+
+// With sequences that share prefixes: [wave tile][key head][split] of 32 rows, and behind them, in a tile's first part, each row's token (-1: nobody's) and query head, which the
+// join would have to search for (5 -> 3 us).
+__host__ __device__ constexpr int shared_part_floats(int head_dim) { return part_floats(32, head_dim) + 64; }
+__device__ __forceinline__ float* shared_part(const AttnArgs& a, int wave_tile, int head, int splits, int head_dim) {
+  return a.partial + ((int64_t)wave_tile * a.d.cache.kv_heads + head) * splits * shared_part_floats(head_dim);
+}
+__device__ __forceinline__ int2* whose_rows(const AttnArgs& a, int wave_tile, int head, int splits, int head_dim) {
+  return reinterpret_cast<int2*>(shared_part(a, wave_tile, head, splits, head_dim) + part_floats(32, head_dim));
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -416,7 +425,11 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     wave_tile = tile * WR + wave % WR;
     const Batch batch(a, q_start, lengths, lane);
     const GroupTile g(sh, a, batch, q_start, wave_tile, lane);
-    if (g.empty()) return;                                 // all waves that meet have the same tile
+    if (g.empty()) {                                       // all waves that meet have the same tile
+      if (splits > 1 && split == 0 && walker == 0 && half == 0)
+        whose_rows(a, wave_tile, head, splits, D)[column] = make_int2(-1, 0);
+      return;
+    }
     const int row = g.first_row + column, of_start = sh.by_group.of(row), token = g.start + of_start;
     const int token_first = g.start + sh.by_group.of(g.first_row), token_last = g.start + sh.by_group.of(min(g.first_row + 32, g.rows) - 1);
     q_head = head * a.group + row - of_start * a.group;
@@ -717,9 +730,8 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
   }
   if constexpr (SHARED) {
     if (splits > 1) {
-      float* part = a.partial + (((int64_t)wave_tile * d.cache.kv_heads + head) * splits + split) * part_floats(32, D);
-      if (valid) put_part<D, WK>(part, 32, o, m, m_exp, l, walker, column, half);
-      else if (half == 0 && walker == 0) part[32 * D + 3 * column] = kAbsent;
+      if (valid) put_part<D, WK>(shared_part(a, wave_tile, head, splits, D) + (int64_t)split * shared_part_floats(D), 32, o, m, m_exp, l, walker, column, half);
+      if (split == 0 && walker == 0 && half == 0) whose_rows(a, wave_tile, head, splits, D)[column] = make_int2(valid ? start + query : -1, q_head);
       return;
     }
   }
@@ -740,33 +752,34 @@ __global__ void __launch_bounds__(64 * WR * WK, D <= 128 ? 2 : 1) attn_shared_ke
 // Joins the parts of a row, four features of it at a time, by G neighbouring lanes: each takes every G-th part and they add each other up by row
 // permutations.  One lane, up to four parts on the way, for up to five parts and for full tiles, 16 lanes otherwise (1 sequence of 8000 in 32 parts 12.4 -> 10.5 us,
 // 32 rows of it in 8 parts 18.7 -> 19.2).  Workgroups go over sequences, key heads, wave tiles and a tile's pieces.
-//   SHARED: tiles are of groups; a row that is nobody's is marked in the first part.
+//   SHARED: a tile's first part says whose its rows are.
 template <int TYPE, int D, int G, bool SHARED>
-__device__ __forceinline__ void attn_join(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs& a, const SharedArgs& sh) {
+__device__ __forceinline__ void attn_join(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs& a) {
   const szo_attn_desc& d = a.d;
   const int wave_tile = blockIdx.x % wave_tiles, head = blockIdx.y, sequence = blockIdx.z;
-  const float* from = partial + (SHARED ? (int64_t)wave_tile * gridDim.y + head : ((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_floats(rows_cap, D);
-  int start, rows, first_row = wave_tile * 32;
-  if constexpr (SHARED) {
-    const GroupTile t(sh, a, Batch(a, q_start, nullptr, threadIdx.x % 64), q_start, wave_tile, threadIdx.x % 64);
-    if (t.empty()) return;
-    start = t.start;
-    first_row = t.first_row;
-    rows = min(t.rows - first_row, 32);
-  } else {
-    start = max(q_start[sequence], 0);
-    const int stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
-    rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
-  }
+  const int part_size = SHARED ? shared_part_floats(D) : part_floats(rows_cap, D);
+  const float* from = SHARED ? shared_part(a, wave_tile, head, splits, D) : partial + (((int64_t)sequence * gridDim.y + head) * wave_tiles + wave_tile) * splits * part_size;
   const int i = (blockIdx.x / wave_tiles * kThreads + threadIdx.x) / G, g = threadIdx.x % G;
-  const int column = i / (D / 4), f = i % (D / 4) * 4, row = first_row + column, query = SHARED ? sh.by_group.of(row) : row / a.group, q_head = head * a.group + row - query * a.group;
-  if (column >= rows) return;                  // G lanes at once
-  if (SHARED && from[(int64_t)rows_cap * D + 3 * column] == kAbsent) return;
+  const int column = i / (D / 4), f = i % (D / 4) * 4;
+  int token, q_head;
+  if constexpr (SHARED) {
+    const int2 whose = whose_rows(a, wave_tile, head, splits, D)[column];
+    token = whose.x;
+    q_head = whose.y;
+    if (token < 0) return;
+  } else {
+    const int start = max(q_start[sequence], 0), stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
+    const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
+    const int row = wave_tile * 32 + column, query = row / a.group;
+    q_head = head * a.group + row % a.group;
+    token = start + query;
+    if (column >= rows) return;                // G lanes at once
+  }
   float m = kNone, m_exp = 0.f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int kAhead = G == 1 ? 4 : 2;
 #pragma unroll kAhead
   for (int s = g; s < splits; s += G) {
-    const float* part = from + (int64_t)s * part_floats(rows_cap, D);
+    const float* part = from + (int64_t)s * part_size;
     const float* stats = part + (int64_t)rows_cap * D + 3 * column;
     const float ms = stats[0], es = stats[1], ls = stats[2];
     const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)column * D + f);
@@ -791,21 +804,19 @@ __device__ __forceinline__ void attn_join(const int32_t* q_start, const float* p
   }
   const float by = inverse_sum(l);
   const float y[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
-  const int64_t at = (int64_t)(start + query) * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
+  const int64_t at = (int64_t)token * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
   if (a.vec_out) store_f32<TYPE, 4, true>(d.out, at, y);
   else store_f32<TYPE, 4, false>(d.out, at, y);
-  if (d.lse && f == 0)
-    d.lse[(int64_t)(start + query) * d.q_heads + q_head] = log_sum(m, m_exp, l);
+  if (d.lse && f == 0) d.lse[(int64_t)token * d.q_heads + q_head] = log_sum(m, m_exp, l);
 }
 
 template <int TYPE, int D, int G>
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a) {
-  attn_join<TYPE, D, G, false>(q_start, partial, wave_tiles, splits, rows_cap, a, SharedArgs{});
+  attn_join<TYPE, D, G, false>(q_start, partial, wave_tiles, splits, rows_cap, a);
 }
 template <int TYPE, int D, int G>
-__global__ void __launch_bounds__(kThreads) attn_shared_join_kernel(const int32_t* q_start, const float* partial, int wave_tiles, int splits, int rows_cap, const AttnArgs a,
-                                                                    const SharedArgs sh) {
-  attn_join<TYPE, D, G, true>(q_start, partial, wave_tiles, splits, rows_cap, a, sh);
+__global__ void __launch_bounds__(kThreads) attn_shared_join_kernel(int wave_tiles, int splits, const AttnArgs a) {
+  attn_join<TYPE, D, G, true>(nullptr, nullptr, wave_tiles, splits, 32, a);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -990,7 +1001,7 @@ template <int TYPE, int D, int G>
 int join_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
   constexpr int pieces = (32 * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
   const dim3 grid((unsigned)(sh.tiles * pieces), (unsigned)a.d.cache.kv_heads);
-  attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(a.d.q_start, a.partial, sh.tiles, sh.splits, 32, a, sh);
+  attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(sh.tiles, sh.splits, a);
   SZO_LAUNCH_CHECK();
   return SZO_OK;
 }
@@ -1070,7 +1081,7 @@ size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* d, const szo_attn_gr
   if (check(d, g) != SZO_OK || nothing(d)) return 16;
   if (!together(d, g)) return szo_attn_workspace_bytes(d);
   const SharedPlan p = plan_of(d, g);
-  return p.splits == 1 ? 16 : (size_t)p.tiles * d->cache.kv_heads * p.splits * part_floats(32, d->cache.head_dim) * sizeof(float);
+  return p.splits == 1 ? 16 : (size_t)p.tiles * d->cache.kv_heads * p.splits * shared_part_floats(d->cache.head_dim) * sizeof(float);
 }
 
 int szo_attn_shared_plan(const szo_attn_desc* d, const szo_attn_groups* g, int32_t* plan) {

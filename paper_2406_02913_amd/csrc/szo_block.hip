@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
       gx_raw[c] = fetch<VEC>(g.x_out_grad, d.x_type, token * g.x_out_stride, p[c]);
       gh_raw[c] = fetch<VEC>(g.h_out_grad, d.h_type, token * g.h_out_stride, p[c]);
     }
-    float y[CH][8], gh[CH][8], a[CH][8], gate[CH][8], w[CH][8], y_r = 0.f;
+    float y[CH][8], h[CH][8], gh[CH][8], a[CH][8], gate[8], w[8], y_r = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
     if (POST) {
@@ -331,30 +331,26 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
       row_stats<CH, VEC>(m, 0, y, p, LAYER, own, inverse, d.eps, mean, y_r);
       to_unit<CH, VEC>(y, p, mean, y_r);
     }
-    if (d.y) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
+    for (int c = 0; c < CH; ++c) {
+      widen<VEC>(h_raw[c], d.h_type, h[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[c][i] *= d.h_scale;
+      if (d.y) {
         float b[8];
-        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate[c]);
-        factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w[c]);
+        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
+        factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
         factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          a[c][i] = fmaf(y[c][i], w[c][i], b[i]);
-          gate[c][i] *= d.y_scale;
+          a[c][i] = fmaf(y[c][i], w[i], b[i]);
+          h[c][i] = fmaf(d.y_scale * gate[i], a[c][i], h[c][i]);
         }
       }
+      widen<VEC>(gh_raw[c], d.h_type, gh[c]);
     }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) widen<VEC>(gh_raw[c], d.h_type, gh[c]);
     if (g.x_out_grad) {
-      float h[CH][8], u[CH][8], mean, r, sum = 0.f, dot = 0.f;
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        widen<VEC>(h_raw[c], d.h_type, h[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[c][i] = d.y ? fmaf(gate[c][i], a[c][i], d.h_scale * h[c][i]) : d.h_scale * h[c][i];
-      }
+      float u[CH][8], mean, r, sum = 0.f, dot = 0.f;
       row_stats<CH, VEC>(m, 1, h, p, LAYER, own, inverse, d.eps, mean, r);
       to_unit<CH, VEC>(h, p, mean, r);
       if (!there) r = 0.f;                                  // with eps 0 it is infinite, and nothing times it would be NaN in the sums
@@ -390,20 +386,23 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
       }
     }
     if (!d.y) continue;
-    // from here on gh is the gradient by the norm's output, then by its input; the gate holds y_scale
+    // from here on gh is the gradient by the norm's output, then by its input.  Gate and weight are read again: kept, they would take registers that are not there (80 -> 76 us).
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float into[8];
+      factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
+      factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        into[i] = d.y_scale * gh[c][i] * a[c][i];
+        const float t = d.y_scale * gh[c][i];
+        into[i] = t * a[c][i];
         sums[kGate][c][i] += into[i];
-        gh[c][i] *= gate[c][i];
+        gh[c][i] = t * gate[i];
         sums[kPostWeight][c][i] = fmaf(gh[c][i], y[c][i], sums[kPostWeight][c][i]);
         sums[kPostBias][c][i] += gh[c][i];
         if (POST) {
-          gh[c][i] *= w[c][i];
+          gh[c][i] *= w[i];
           sum += gh[c][i];
           dot = fmaf(gh[c][i], y[c][i], dot);
         }

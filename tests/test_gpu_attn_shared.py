@@ -112,7 +112,7 @@ WAYS = [(64, 8, 2, 70, 60, 1 << 17, (1, 4, 1, 1)),                 # tiles side 
         (128, 8, 4, 70, 60, 1 << 17, (1, 4, 1, 1)), (256, 8, 2, 70, 61, 1 << 17, (1, 4, 1, 1)),
         (128, 8, 4, 40, 10, 1 << 17, (1, 1, 4, 1)),                  # four waves a tile, whole
         (128, 4, 4, 64, 1, 1 << 17, (1, 1, 8, 8)),                   # eight, in parts
-        (96, 32, 1, 256, 1, 2000, (1, 1, 8, 1)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),            # eight, whole
+        (96, 16, 2, 256, 1, 2000, (1, 1, 8, 1)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),            # eight, whole
         (64, 8, 1, 64, 1, 200, (1, 1, 4, 24)), (256, 2, 2, 64, 1, 600, (1, 1, 4, 32)), (96, 2, 3, 40, 1, 2400, (1, 1, 8, 42)),
         (64, 1, 2, 5, 1, 200, (0, 0, 0, 0))]                          # each by itself
 
