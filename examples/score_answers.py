@@ -1,9 +1,10 @@
 """Scores candidate answers, decodes and fine-tunes with a small decoder of sparse int4 linears.
 
-A decoder block's linears are the library's sensitive-sparse int4 layers; between them stand its norms of queries and keys with the rotation,
-its 8-bit key/value cache and the attention over it, and behind the head its log probabilities.  Prompts go into the cache once; every candidate
-answer is scored behind its prompt by the log probabilities of its tokens, as classification by a language model does; then a few tokens are
-decoded greedily, and a zeroth-order step moves the head's sensitive weights by the answers' likelihood.
+A decoder block's linears are the library's sensitive-sparse int4 layers; between them stand its norms around a block with the residual stream, its
+norms of queries and keys with the rotation, its 8-bit key/value cache and the attention over it, and behind the head its log probabilities.  Prompts
+go into the cache once, and the candidates of a prompt share the pages that it fills; every candidate answer is scored behind its prompt by the log
+probabilities of its tokens, as classification by a language model does; then a few tokens are decoded greedily, and a zeroth-order step moves the
+head's sensitive weights by the answers' likelihood.
 
     python examples/score_answers.py [--layers 2] [--prompts 3]
 """
@@ -18,10 +19,6 @@ from paper_2406_02913_amd import szo                                    # noqa: 
 from paper_2406_02913_amd.stack import build_linear                     # noqa: E402
 
 DEV = "cuda"
-
-
-def rms(x):
-    return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6)
 
 
 class Linear:
@@ -43,7 +40,7 @@ class Linear:
 
 
 class Decoder:
-    def __init__(self, layers=2, hidden=512, q_heads=8, kv_heads=2, head_dim=64, vocab=2000, sequences=6, most=256, page=64):
+    def __init__(self, layers=2, hidden=512, q_heads=8, kv_heads=2, head_dim=64, vocab=2000, sequences=6, most=256, page=32):
         self.q_heads, self.kv_heads, self.head_dim, self.vocab = q_heads, kv_heads, head_dim, vocab
         gen = torch.Generator(device=DEV)
         gen.manual_seed(1)
@@ -61,9 +58,20 @@ class Decoder:
         self.head = Linear(999, vocab, hidden, base)
         angle = torch.arange(most, device=DEV)[:, None] * 10000.0 ** (-torch.arange(0, head_dim, 2, device=DEV) / head_dim)
         self.cos, self.sin = angle.cos().contiguous(), angle.sin().contiguous()
-        # every sequence has its own pages here; a server would hand them out as sequences grow
+        # every sequence has its own pages here until share() is called; a server would hand them out as sequences grow
         self.table = torch.arange(sequences * most // page, dtype=torch.int32, device=DEV).view(sequences, -1)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=DEV)
+        self.page, self.groups = page, None
+
+    def share(self, prompts, each):
+        """Groups of `each` sequences that have the same prompt; the pages that it fills are the first one's.  What is left of each prompt goes to pages of its own."""
+        whole = [p // self.page for p in prompts]
+        for i, pages in enumerate(whole):
+            self.table[i * each + 1:(i + 1) * each, :pages] = self.table[i * each, :pages]
+        start = torch.arange(0, each * len(prompts) + 1, each, dtype=torch.int32, device=DEV)
+        shared = torch.tensor([w * self.page for w in whole], dtype=torch.int32, device=DEV)
+        self.groups = szo.make_attn_groups(start, shared, each, max(whole) * self.page)
+        return [w * self.page for w in whole]
 
     def hidden_states(self, tokens, new, had):
         """Appends tokens (i64 [sum(new)], sequence after sequence) behind `had` cached ones of each sequence; their final states."""
@@ -72,8 +80,9 @@ class Decoder:
         positions = torch.cat([torch.arange(h, h + n, dtype=torch.int32) for h, n in zip(had, new)]).to(DEV)
         T, D, longest = len(tokens), self.head_dim, max(h + n for h, n in zip(had, new))
         x = self.embedding[tokens]
+        h, y = torch.empty_like(x, dtype=torch.bfloat16), None
         for block in self.blocks:
-            h = rms(x)
+            szo.szo_block_norm(szo.make_block_desc(y, x, x, h))              # the last block's output joins the stream; its norm is what the linears take
             q, k, v = (block[n](h).view(T, -1, D) for n in "qkv")
             q_out, k_out = torch.empty_like(q, dtype=torch.bfloat16), torch.empty_like(k, dtype=torch.bfloat16)
             szo.szo_qk_norm_rope(szo.make_qk_desc(q, k, positions, self.cos, self.sin, q_out, k_out, q_weight=block["q_norm"], k_weight=block["k_norm"]))
@@ -81,9 +90,13 @@ class Decoder:
             szo.szo_kv_cache_write(cache, szo.make_kv_tokens(k_out, v.to(torch.bfloat16), start, max(new)))
             out = torch.empty_like(q_out)
             attn = szo.make_attn_desc(cache, q_out, out, start, max(new), longest, D ** -0.5)
-            szo.szo_attn_cached(attn, torch.empty(szo.szo_attn_workspace_bytes(attn), dtype=torch.uint8, device=DEV))
-            x = x + block["o"](out.view(T, -1))
-        return rms(x)
+            if self.groups is None:
+                szo.szo_attn_cached(attn, torch.empty(szo.szo_attn_workspace_bytes(attn), dtype=torch.uint8, device=DEV))
+            else:
+                szo.szo_attn_shared(attn, self.groups, torch.empty(szo.szo_attn_shared_workspace_bytes(attn, self.groups), dtype=torch.uint8, device=DEV))
+            y = block["o"](out.view(T, -1))
+        szo.szo_block_norm(szo.make_block_desc(y, x, None, h))
+        return h
 
     def log_probs(self, states, targets, top=0, **perturbed):
         """Log probabilities of targets, their entropy, and the best `top` tokens."""
@@ -110,9 +123,13 @@ def main(argv=None):
         prompts[2 * i + 1] = prompts[2 * i]
     answers = [torch.randint(model.vocab, (int(torch.randint(1, 9, (1,), generator=gen)),), generator=gen) for _ in range(2 * n)]
 
-    # the prompts without their last token go into the cache; that token and the answer are what is scored
+    # the prompts without their last token go into the cache, whole pages of them once; that token and the answer are what is scored
     had = [len(p) - 1 for p in prompts]
-    model.hidden_states(torch.cat([p[:-1] for p in prompts]).to(DEV), had, [0] * len(had))
+    model.hidden_states(torch.cat([p[:-1] for p in prompts[::2]]).to(DEV), [h if i % 2 == 0 else 0 for i, h in enumerate(had)], [0] * len(had))
+    shared = model.share(had[::2], 2)
+    rest = [h - shared[i // 2] if i % 2 else 0 for i, h in enumerate(had)]
+    if any(rest):
+        model.hidden_states(torch.cat([p[h - r:h] for p, h, r in zip(prompts, had, rest)]).to(DEV), rest, [h - r for h, r in zip(had, rest)])
     new = [len(a) for a in answers]
     fed = torch.cat([torch.cat([p[-1:], a[:-1]]) for p, a in zip(prompts, answers)]).to(DEV)
     targets = torch.cat(answers).to(torch.int32).to(DEV)
