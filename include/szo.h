@@ -276,7 +276,8 @@ int szo_workspace_init(void* workspace, void* stream);
  * y is what a block's last linear gives, h the residual stream, x what the next block's linears (or the head) take.  y NULL: no block in
  * front (h' = h_scale h); h NULL: no stream yet (0); outputs that are NULL are not computed; weights that are NULL are 1, biases 0, a gate 1.  The gate is
  * one row for every token, or one for all with gate_stride 0.  Sums and products in fp32, each output rounded once to its type, x from the unrounded h'.
- * Squares are fp32: values above 1e19 give infinities.  An output may be an input's own buffer, with its type and stride. */
+ * Squares are fp32: values above 1e19 give infinities.  An output may be the buffer of y, h or a gate of its own for each token, with its type and stride.
+ * SZO_EUNSUPPORTED: wider rows, and batches that take 2^22 workgroups (a token each above 1024 features, two above 512, four up to there). */
 #define SZO_NORM_RMS   0
 #define SZO_NORM_LAYER 1
 typedef struct szo_block_desc {
@@ -431,8 +432,8 @@ int szo_attn_plan(const szo_attn_desc* desc /* host */, int32_t* plan /* host, 4
  * shared[g] whole blocks of 32 tokens count, max_shared tokens at most; tokens behind a sequence's length and masked ones have no influence here either.  Sequences
  * of no group share nothing. */
 typedef struct szo_attn_groups {
-  int32_t groups, max_sequences;/* most sequences of a group: a hint                                     */
-  int32_t max_shared, reserved; /* most shared tokens                                                    */
+  int32_t groups, max_sequences;/* most sequences of a group: a hint, for the split of the work          */
+  int32_t max_shared, reserved; /* most shared tokens that count                                         */
   const int32_t* group_start;   /* device [groups + 1], ascending from 0 to sequences                    */
   const int32_t* shared;        /* device [groups]                                                       */
 } szo_attn_groups;
@@ -496,15 +497,15 @@ typedef struct szo_head_desc {
   double loss_scale;
 } szo_head_desc;
 /* workspace: device, szo_head_workspace_bytes(desc) for this very descriptor, 16-byte aligned, for this call alone while it runs.  SZO_EUNSUPPORTED: widths and strides
- * other than those named, a vocabulary above 2^30, 2^23 tiles of 256 vocabulary entries and 64 to 256 rows. */
+ * other than those named, a vocabulary above 2^30, rows from 2^26 on, more than 2^23 - 1 tiles of 128 or 256 vocabulary entries by 64 to 448 rows. */
 int szo_head_logprobs(const szo_head_desc* desc /* host */, void* workspace, void* stream);
 size_t szo_head_workspace_bytes(const szo_head_desc* desc /* host */);
 /* Gradients by x and by the weight of a scalar whose gradient by logp is grad_logp (device fp32 [rows]), from the forward's stats:
  *   d = scale grad_logp (1[v = target] - p),   x_grad = d weight,   weight_grad = d^T x
  * The logits are computed again, piece by piece of the vocabulary; d is rounded to the type (fp16: times a power of two that the largest gradient sets).  x_grad and weight_grad (device,
- * of the type, rows x_grad_stride and weight_grad_stride apart, 2-byte aligned; either may be NULL) are overwritten and may be the buffers of x and weight.  Rows whose target
- * is ignored have gradient 0 and no part in weight_grad, whatever they hold.  workspace: szo_head_bwd_workspace_bytes(desc), up to 256 MiB for a piece of d and
- * what sums of x_grad take. */
+ * of the type, rows x_grad_stride and weight_grad_stride apart, 2-byte aligned; either may be NULL) are overwritten and may be the buffers of x and weight, with their strides.  Rows whose target
+ * is ignored have gradient 0 and no part in weight_grad, whatever they hold.  workspace: szo_head_bwd_workspace_bytes(desc): up to 256 MiB (or 256 entries) for a piece of d, as
+ * much as x, and what sums of x_grad take.  SZO_EUNSUPPORTED also for rows times width from 2^34 on. */
 int szo_head_logprobs_bwd(const szo_head_desc* desc /* host */, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad,
                           int64_t weight_grad_stride, void* workspace, void* stream);
 size_t szo_head_bwd_workspace_bytes(const szo_head_desc* desc /* host */);

@@ -950,7 +950,7 @@ SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   p.tiles = (int)(rows / 32 + g->groups + 2);
   p.wr = held >= 2048 ? 4 : 1;
   // a tile's blocks: the shared ones, and half of the most of each sequence that is in it
-  const int64_t each = std::max<int64_t>(1, rows / d->cache.sequences), sequences = std::min<int64_t>(32, std::max<int64_t>(1, 32 / each));
+  const int64_t each = std::max<int64_t>(1, rows / d->cache.sequences), sequences = std::max<int64_t>(1, std::min<int64_t>(32 / each, g->max_sequences));
   const int64_t own = std::max<int64_t>(0, (int64_t)d->max_len - g->max_shared), blocks = g->max_shared / kKvBlock + sequences * (own / (2 * kKvBlock) + 1);
   const bool wide = d->cache.head_dim > 128;                // a wave has its SIMD to itself
   p.wk = p.wr == 4 ? 1 : !wide && held <= 256 && blocks / 8 >= 256 / held ? 8 : 4;

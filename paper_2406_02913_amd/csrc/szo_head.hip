@@ -406,6 +406,7 @@ int check(const szo_head_desc* d) {
   if (d->x_stride > kMostStride || d->weight_stride > kMostStride || d->x_stride % 8 || d->weight_stride % 8) return SZO_EUNSUPPORTED;
   if ((d->rows && !d->x) || (d->vocab && !d->weight) || !aligned_to(d->x, 16) || !aligned_to(d->weight, 16)) return SZO_EINVAL;
   if (!aligned_to(d->targets, 4) || !aligned_to(d->logp, 4) || !aligned_to(d->stats, 4) || !aligned_to(d->loss_acc, 8)) return SZO_EINVAL;
+  if (tiles_of(d->rows, 4) > kMostSmallGroups) return SZO_EUNSUPPORTED;
   if (d->rows) {
     const LogitPlan p = logit_plan(d->rows, d->vocab);
     if (tiles_of(d->vocab, p.entries) * tiles_of(d->rows, p.rows) > kMostGroups) return SZO_EUNSUPPORTED;

@@ -132,7 +132,7 @@ def test_head_refuses(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(width=0), dict(width=96), dict(width=65600, x_stride=65600, weight_stride=65600), dict(vocab=(1 << 30) + 1), dict(rows=1 << 31), dict(x_stride=130),
-                                dict(weight_stride=(1 << 22) + 8), dict(rows=1 << 30, vocab=1 << 30)])
+                                dict(weight_stride=(1 << 22) + 8), dict(rows=1 << 30, vocab=1 << 30), dict(rows=(1 << 26) + 1, vocab=1)])
 def test_head_does_not_take(kw):
     assert szo.lib.szo_head_logprobs(C.byref(head(**kw)), P, None) == szo.EUNSUPPORTED
 
