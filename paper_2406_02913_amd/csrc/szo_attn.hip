@@ -40,7 +40,7 @@ struct AttnArgs {
   float to_log2;                           // |scale| * log2(e)
   bool negate;                             // scale < 0: queries change sign
   float* partial;                          // [sequence][key head][wave tile][split] of part_floats()
-  bool vec_q, vec_out;
+  bool vec_out;
 };
 
 // floor(v / d) for 0 <= v < 2^31: with 2^(l - 1) < d <= 2^l and m = ceil(2^(31 + l) / d) it is v m / 2^(31 + l), exactly.
@@ -122,27 +122,27 @@ template <> struct Score<SZO_F16> {
   static __device__ __forceinline__ f32x16 add(vec k, vec q, f32x16 s) { return product(k, q, s); }
 };
 
-// A lane's row of queries, in the order of the features that a block of keys has: 32 s + 16 half + 8 u .. + 7.
+// A lane's row of queries, in the order of the features that a block of keys has: 32 s + 16 half + 8 u .. + 7.  Loading them waits for nothing: addresses are of any
+// alignment, a lane without a row reads another one's, and what arrives is made 0 there and changes its sign where that is asked for afterwards.
 template <int TYPE, int D> struct Query {
   typename Score<TYPE>::vec part[D / 32][2];
-  __device__ __forceinline__ void load(const void* base, int64_t at, bool valid, bool aligned, bool negate, int half) {
-    typedef typename Score<TYPE>::vec vec;
+  __device__ __forceinline__ void load(const void* base, int64_t at, int half) {
+    typedef typename Score<TYPE>::vec loose __attribute__((aligned(2)));
     const auto* p = static_cast<const typename TypeOf<TYPE>::type*>(base) + at + 16 * half;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        vec x = {};
-        if (valid) {
-          if (aligned) x = *reinterpret_cast<const vec*>(p + 32 * s + 8 * u);
-          else
+      for (int u = 0; u < 2; ++u) part[s][u] = *reinterpret_cast<const loose*>(p + 32 * s + 8 * u);
+  }
+  __device__ __forceinline__ void arrived(bool valid, bool negate) {
+    const uint32_t keep = valid ? 0xFFFFFFFFu : 0u, flip = negate ? 0x80008000u : 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[32 * s + 8 * u + i];
-        }
-        uint4 w = __builtin_bit_cast(uint4, x);
-        const uint32_t flip = negate ? 0x80008000u : 0u;
-        w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-        part[s][u] = __builtin_bit_cast(vec, w);
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        uint4 w = __builtin_bit_cast(uint4, part[s][u]);
+        w.x = w.x & keep ^ flip; w.y = w.y & keep ^ flip; w.z = w.z & keep ^ flip; w.w = w.w & keep ^ flip;
+        part[s][u] = __builtin_bit_cast(typename Score<TYPE>::vec, w);
       }
   }
 };
@@ -250,14 +250,17 @@ __device__ __forceinline__ void put_row(const AttnArgs& a, const f32x16 (&o)[D /
 struct Batch {
   int first, stop, length;                 // first token; lane i: token behind sequence i, its length
   bool fits;
-  __device__ __forceinline__ Batch(const AttnArgs& a, const int32_t* q_start, const int32_t* lengths, int lane) : first(0), stop(0), length(0) {
-    const int sequences = a.d.cache.sequences;
+  __device__ __forceinline__ Batch(const AttnArgs& a, const int32_t* q_start, const int32_t* lengths, int lane) {
+    const int sequences = a.d.cache.sequences, i = min(lane, sequences - 1);
     fits = sequences <= 64;
-    if (fits) {
-      first = clamped(a, q_start[0]);
-      stop = clamped(a, q_start[min(lane, sequences - 1) + 1]);
-      if (lengths) length = lengths[min(lane, sequences - 1)];
-    }
+    first = q_start[0];
+    stop = q_start[i + 1];
+    length = lengths[i];
+  }
+  // The loads wait for nothing until here.
+  __device__ __forceinline__ void arrived(const AttnArgs& a) {
+    first = clamped(a, first);
+    stop = clamped(a, stop);
   }
   static __device__ __forceinline__ int clamped(const AttnArgs& a, int at) { return max((int)min((int64_t)at, a.d.tokens), 0); }
   __device__ __forceinline__ int start_of(const AttnArgs& a, const int32_t* q_start, int sequence) const {
@@ -274,14 +277,19 @@ struct GroupTile {
   int first, last;                         // the group's sequences; first == last: no rows
   int start, rows, first_row;              // its first token, its rows, the tile's first row among them
   int blocks;                              // that its sequences share
-  __device__ __forceinline__ GroupTile(const SharedArgs& sh, const AttnArgs& a, const Batch& batch, const int32_t* q_start, int tile, int lane)
+  __device__ __forceinline__ GroupTile(const SharedArgs& sh, const AttnArgs& a, Batch& batch, const int32_t* q_start, int tile, int lane)
       : first(0), last(0), start(0), rows(0), first_row(0), blocks(0) {
     int e = -1, tokens = 0, stop = 0;
+    auto start_at = [&](int i) { return sh.group_start[min(max(i - 1, 0), sh.groups)]; };            // there is one group at least
+    auto shared_at = [&](int i) { return sh.shared[min(max(i - 1, 0), sh.groups - 1)]; };
+    int begins = start_at(lane), common = shared_at(lane);
+    batch.arrived(a);
     for (int k = 0;; k += 64) {
       const int i = k + lane;
-      const int sequence = i == 0 ? 0 : i <= sh.groups + 1 ? min(max(sh.group_start[i - 1], 0), a.d.cache.sequences) : a.d.cache.sequences;
+      if (k > 0) { begins = start_at(i); common = shared_at(i); }
+      const int sequence = i == 0 ? 0 : i <= sh.groups + 1 ? min(max(begins, 0), a.d.cache.sequences) : a.d.cache.sequences;
       const int at = batch.start_of(a, q_start, sequence);
-      const int common = i >= 1 && i <= sh.groups ? sh.shared[i - 1] : 0;
+      if (i < 1 || i > sh.groups) common = 0;
       const int c = __popcll(__ballot(i <= sh.groups + 1 && at * a.group / 32 + i <= tile));            // they ascend: the first c
       if (c > 0) {
         e = k + c - 1;
@@ -311,8 +319,15 @@ struct Segments {
 };
 struct SegmentWalk {
   int slot, left, block, page_at, sub, per_page;     // blocks of the segment from this one on, the block's number in its sequence and where it lies
+  int own_from;                                      // of all slots' blocks, the first one of this walk
   bool entered;                                      // at a slot's first block
   const int32_t* table;
+  // Shared blocks from `at` to `to`, then slots' ones.
+  __device__ __forceinline__ void begin(const Segments& g, int at, int to, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    slot = at < to ? -1 : 0;
+    enter(g, at < to ? at : own_from, page_table, max_pages, by_page);
+    if (at < to) left = to - at;
+  }
   __device__ __forceinline__ void enter(const Segments& g, int at, const int32_t* page_table, int max_pages, const Divisor& by_page) {
     int n = g.count(slot);
     while (at >= n) { at -= n; n = g.count(++slot); }          // blocks asked for are there
@@ -330,7 +345,7 @@ struct SegmentWalk {
       if (++sub == per_page) { sub = 0; ++page_at; }
     } else {
       ++slot;
-      enter(g, 0, page_table, max_pages, by_page);
+      enter(g, slot == 0 ? own_from : 0, page_table, max_pages, by_page);
     }
   }
   __device__ __forceinline__ int at(const Segments& g, const szo_kv_cache& c, int head) const {
@@ -375,6 +390,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
   const int lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), column = lane % 32, half = lane / 32;
   // What a wave's rows are and which blocks they go over.
   int head, sequence = 0, split, wave_tile, start, query, q_head, see_to, see_from, see_all, see_all_from, j0, j1, guess = -1;
+  int shared_from = 0, shared_to = 0, own_from = 0;         // SHARED: of the blocks that sequences share, of all slots' own ones
   bool valid;
   const int32_t* table = nullptr;
   Query<TYPE, D> q;
@@ -407,7 +423,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     valid = row < rows;
     see_to = !valid ? 0 : d.causal ? min(length, behind + query + 1) : length;
     see_from = window_from(behind + query);
-    q.load(d.q, (int64_t)(start + query) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, valid, a.vec_q, a.negate, half);
+    q.load(d.q, (int64_t)(start + (valid ? query : 0)) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, half);
 
     // blocks that some row of the wave sees, the part of them that is this split's, and this wave's share of that
     const int pos_first = behind + first_row / a.group, pos_last = behind + (min(first_row + 32, rows) - 1) / a.group;
@@ -423,7 +439,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     const int tile = unit / splits;
     split = unit - tile * splits;
     wave_tile = tile * WR + wave % WR;
-    const Batch batch(a, q_start, lengths, lane);
+    Batch batch(a, q_start, lengths, lane);
     const GroupTile g(sh, a, batch, q_start, wave_tile, lane);
     if (g.empty()) {                                       // all waves that meet have the same tile
       if (splits > 1 && split == 0 && walker == 0 && half == 0)
@@ -433,7 +449,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     const int row = g.first_row + column, of_start = sh.by_group.of(row), token = g.start + of_start;
     const int token_first = g.start + sh.by_group.of(g.first_row), token_last = g.start + sh.by_group.of(min(g.first_row + 32, g.rows) - 1);
     q_head = head * a.group + row - of_start * a.group;
-    q.load(d.q, (int64_t)token * d.q_token_stride + (int64_t)q_head * d.q_head_stride, row < g.rows, a.vec_q, a.negate, half);
+    q.load(d.q, (int64_t)(row < g.rows ? token : g.start) * d.q_token_stride + (int64_t)q_head * d.q_head_stride, half);
     // The sequences that have rows in the tile, 64 side by side; those that have go to slots, one lane each (at most 32, since each has a token).
     int slot_start = 0, slot_last = 0, slot_behind = 0, slot_length = 0;       // this lane's slot: first token, last query that counts, position of the first one, length
     int reach = 0, first_seen = -0x7FFFFFFF, all_to = -0x7FFFFFFF, all_from = 0;      // of all slots: largest, and smallest with the sign changed
@@ -493,10 +509,13 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     segments.sequence = g.first;
     segments.shared_first = -wave_max(first_seen) / kKvBlock;
     segments.shared_count = max(min(g.blocks, (reach + kKvBlock - 1) / kKvBlock) - segments.shared_first, 0);
-    // a walker's blocks follow each other, so that it enters few segments
-    const int total = segments.shared_count + wave_add(lane < slots ? segments.own_count : 0);
-    const int share = (total + splits - 1) / splits, each = (share + WK - 1) / WK;
-    j0 = split * share + walker * each, j1 = min(min(total, (split + 1) * share), j0 + each);
+    // Every walker takes a run of the shared blocks and a run of the own ones, which are slower (masked, and from memory that no other tile reads: 4500 cycles beside 2600); the
+    // first walkers have a shared block more than the last, the last an own one.  Runs, so that a walker enters few segments.
+    const int own = wave_add(lane < slots ? segments.own_count : 0), walkers = splits * WK, mine = split * WK + walker, mirrored = walkers - 1 - mine;
+    const int shared_share = (segments.shared_count + walkers - 1) / walkers, own_share = (own + walkers - 1) / walkers;
+    shared_from = min(mine * shared_share, segments.shared_count), shared_to = min(shared_from + shared_share, segments.shared_count);
+    own_from = min(mirrored * own_share, own);
+    j0 = 0, j1 = shared_to - shared_from + min(own_share, own - own_from);
   }
   constexpr int kNext = SHARED ? 1 : WK;   // from one of a walker's blocks to the next
 
@@ -510,10 +529,10 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
   if (j0 < j1) {
     // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
     Walk walk(SHARED ? 0 : j0, bpp);
-    SegmentWalk piece = {-1, 0, 0, 0, 0, bpp, false, nullptr};
+    SegmentWalk piece = {-1, 0, 0, 0, 0, bpp, own_from, false, nullptr};
     int now, next, block_now = 0, slot_now = -1, block_next = 0, slot_next = -1;
     if constexpr (SHARED) {
-      piece.enter(segments, j0, page_table, max_pages, sh.by_page);
+      piece.begin(segments, shared_from, shared_to, page_table, max_pages, sh.by_page);
       now = next = piece.at(segments, d.cache, head);
       block_now = block_next = piece.block;
       slot_now = slot_next = piece.slot;
@@ -538,6 +557,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     };
     Raw<D> k = load_block<D, ONCE>(d.cache.k, known(now), lane), v = load_block<D, ONCE>(d.cache.v, known(now), lane);
     int ke = d.cache.k_exp[known(now)], ve = d.cache.v_exp[known(now)], most_vexp = kExpMin;
+    q.arrived(valid, a.negate);
     scores(k);
     k = load_block<D, ONCE>(d.cache.k, known(next), lane);
     for (int j = j0; j < j1; j += kNext) {        // k: keys of the next step, v: values of this one
@@ -764,9 +784,8 @@ __device__ __forceinline__ void attn_join(const int32_t* q_start, const float* p
   int token, q_head;
   if constexpr (SHARED) {
     const int2 whose = whose_rows(a, wave_tile, head, splits, D)[column];
-    token = whose.x;
+    token = whose.x;                           // looked at behind the parts, which are asked for beside it; those of a row that is nobody's are read for nothing
     q_head = whose.y;
-    if (token < 0) return;
   } else {
     const int start = max(q_start[sequence], 0), stop = max((int)min((int64_t)q_start[sequence + 1], d.tokens), 0);
     const int rows = min(max(0, min(stop - start, d.max_q)) * a.group - wave_tile * 32, 32);
@@ -802,6 +821,7 @@ __device__ __forceinline__ void attn_join(const int32_t* q_start, const float* p
     for (int k = 0; k < 4; ++k) o[k] = lanes_sum<G>(o[k] * keep);
     if (g) return;
   }
+  if (SHARED && token < 0) return;
   const float by = inverse_sum(l);
   const float y[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
   const int64_t at = (int64_t)token * d.out_token_stride + (int64_t)q_head * d.out_head_stride + f;
@@ -933,14 +953,15 @@ int launch_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
 
 // ---- sequences that share a prefix -----------------------------------------------------------------------------------
 
-// How tiles and their blocks go to waves.  Four waves take tiles side by side (wr 4) where the tiles alone fill the chip; else four or eight share a tile's blocks and meet in LDS,
-// and with few tiles the blocks go to several workgroups, joined by a second kernel.  A wave's step takes 1.1 us, bound by the issue of its instructions, and as long beside a second
-// wave on its SIMD; a workgroup takes 4 us to find its rows and to begin, 2 to meet, a join 4 to 6.  So there are two waves a SIMD where the blocks allow: eight waves a
-// workgroup up to 256 tiles, but four where a tile has so few blocks that one of them a wave does not fill the chip.  us, 32 query and 8 key heads of 128 in bf16, parts 1, 2, 4, 8, 16 of four
-// waves / of eight: 64 sequences, one token each, behind 8192 shared ones and up to 500 own (64 tiles, 320 blocks each) 114, 69, 42, 35, 44 / 77, 50, 34, 42, 59; 16 of them
-// (16 tiles) 87, 55, 35, 24, 22 / 63, 42, 29, 22, 22; 256 behind 4 x 2048 (256 tiles, 104 blocks) 52, 43, 53 / 37, 51; 4 behind 1024 (8 tiles, 40 blocks) 14.6, 14.1, 13.7, 12.9,
-// 13.2 / 13.5, 15.8, 12.9, 13.2; answers of 3 to 61 tokens, 32 of them behind 4 x 2500 (976 tiles) 58, 87 / 73; 8 behind 2000 (344 tiles) 28, 40 / 36; 256 behind 8 x 2000 (7440 tiles)
-// 281 / 430, side by side 229.  szo_attn_cached takes 102, 31, 113, 9.9, 74, 27, 358 for these.
+// How tiles and their blocks go to waves.  Four waves take tiles side by side (wr 4), or four or eight share a tile's blocks and meet in LDS, and with few tiles the blocks go to several
+// workgroups, joined by a second kernel.  A wave's step takes 1.1 us, bound by the issue of its instructions, and as long beside a second
+// wave on its SIMD; a workgroup takes 4 us to find its rows and to begin, 2 to meet, a join 4.  So there are two waves a SIMD where the blocks allow: eight waves a
+// workgroup up to 256 tiles, but four where a tile has so few blocks that one of them a wave does not fill the chip; and side by side from 2048 tiles on, unless rounds of 2048 that are
+// partly filled cost more than meetings, 7 us for each 512 tiles, do.  us, 32 query and 8 key heads of 128 in bf16, parts 1, 2, 4, 8, 16 of four
+// waves / of eight: 64 sequences, one token each, behind 8192 shared ones and up to 500 own (64 tiles, 320 blocks each) 104, 61, 37, 32 / 68, 44, 30, 40; 16 of them
+// (16 tiles) 81, 48, 31, 23 / 57, 37, 25, 21, 21; 256 behind 4 x 2048 (256 tiles, 104 blocks) 50, 42, 52 / 36, 49; 4 behind 1024 (8 tiles, 40 blocks) 14.6, 14.1, 13.7, 12.9,
+// 13.2 / 13.5, 15.8, 12.9, 13.2; answers of 3 to 61 tokens, 32 of them behind 4 x 2500 (976 tiles) 60, 87 / 72, side by side 77; 8 behind 2000 (344 tiles) 28, 40 / 35; 64 behind 2 x 2000 (2100
+// tiles) 101 / 136, side by side 114; 256 behind 8 x 2000 (7440 tiles) 295 / 443, side by side 241.  szo_attn_cached takes 102, 31, 113, 9.9, 74, 27, -, 358 for these.
 struct SharedPlan { int wr, wk, tiles, splits; };
 
 SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
@@ -948,10 +969,10 @@ SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   const int64_t group = d->q_heads / d->cache.kv_heads, heads = d->cache.kv_heads, rows = d->tokens * group;
   const int64_t held = std::max<int64_t>(1, rows / 32) * heads;            // tiles that hold something, about
   p.tiles = (int)(rows / 32 + g->groups + 2);
-  p.wr = held >= 2048 ? 4 : 1;
   // a tile's blocks: the shared ones, and half of the most of each sequence that is in it
   const int64_t each = std::max<int64_t>(1, rows / d->cache.sequences), sequences = std::max<int64_t>(1, std::min<int64_t>(32 / each, g->max_sequences));
   const int64_t own = std::max<int64_t>(0, (int64_t)d->max_len - g->max_shared), blocks = g->max_shared / kKvBlock + sequences * (own / (2 * kKvBlock) + 1);
+  p.wr = held >= 2048 && 1.13 * (double)(blocks * ((held + 2047) / 2048)) < (0.283 * (double)blocks + 7.0) * (double)held / 512 ? 4 : 1;
   const bool wide = d->cache.head_dim > 128;                // a wave has its SIMD to itself
   p.wk = p.wr == 4 ? 1 : !wide && held <= 256 && blocks / 8 >= 256 / held ? 8 : 4;
   const int64_t chip = p.wk == 8 || wide ? 256 : 512;
@@ -1033,7 +1054,6 @@ AttnArgs args_of(const szo_attn_desc* d, void* workspace) {
   a.to_log2 = (d->scale < 0.f ? -d->scale : d->scale) * 1.44269504088896341f;
   a.negate = d->scale < 0.f;
   a.partial = (float*)workspace;
-  a.vec_q = aligned_to(d->q, 16) && d->q_token_stride % 8 == 0 && d->q_head_stride % 8 == 0;
   a.vec_out = aligned_to(d->out, 8) && d->out_token_stride % 4 == 0 && d->out_head_stride % 4 == 0;
   return a;
 }

@@ -108,8 +108,8 @@ def test_more_groups_and_sequences_than_a_wave_has_lanes(monkeypatch):
 
 
 # head_dim, key heads, group, sequences, new tokens of each, hint of lengths -> what the plan says
-WAYS = [(64, 8, 2, 70, 60, 1 << 17, (1, 4, 1, 1)),                 # tiles side by side
-        (128, 8, 4, 70, 60, 1 << 17, (1, 4, 1, 1)), (256, 8, 2, 70, 61, 1 << 17, (1, 4, 1, 1)),
+WAYS = [(64, 8, 2, 70, 60, 200, (1, 4, 1, 1)), (64, 8, 2, 80, 60, 1 << 17, (1, 1, 4, 1)),                 # tiles side by side
+        (128, 8, 4, 70, 60, 200, (1, 4, 1, 1)), (256, 8, 2, 70, 61, 200, (1, 4, 1, 1)),
         (128, 8, 4, 40, 10, 1 << 17, (1, 1, 4, 1)),                  # four waves a tile, whole
         (128, 4, 4, 64, 1, 1 << 17, (1, 1, 8, 8)),                   # eight, in parts
         (96, 16, 2, 256, 1, 2000, (1, 1, 8, 1)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),            # eight, whole
