@@ -16,8 +16,10 @@ namespace szo {
 namespace {
 
 constexpr int kMostWidth = 16384, kMostWaves = 16;
-constexpr int kSets = 5;             // sums over tokens: pre weight, pre bias, post weight, post bias, gate
-enum Set { kPreWeight, kPreBias, kPostWeight, kPostBias, kGate };
+// Sums over tokens.  Those behind the post norm are of t unit and t with t = y_scale gh' (times the gate where each token has its own): a gate that all tokens share is a factor of
+// the gradients by weight and bias, and its own one is weight and bias times the two sums.
+constexpr int kSets = 4;
+enum Set { kPreWeight, kPreBias, kPostWeight, kPostBias };
 
 struct BlockArgs {
   szo_block_desc d;
@@ -293,7 +295,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs arg
   }
 }
 
-// A workgroup walks rows and keeps what it adds up over them in registers, eight features of up to five sums a thread; no atomics, so the order is fixed.
+// A workgroup walks rows and keeps what it adds up over them in registers, eight features of up to four sums a thread; no atomics, so the order is fixed.
 template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
 __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 : 1) block_norm_bwd_kernel(const BlockArgs args) {
   __shared__ float slots[4][kMostWaves][2];
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
       gx_raw[c] = fetch<VEC>(g.x_out_grad, d.x_type, token * g.x_out_stride, p[c]);
       gh_raw[c] = fetch<VEC>(g.h_out_grad, d.h_type, token * g.h_out_stride, p[c]);
     }
-    float y[CH][8], h[CH][8], gh[CH][8], a[CH][8], gate[8], w[8], y_r = 0.f;
+    float y[CH][8], h[CH][8], gh[CH][8], gate[8], w[8], y_r = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
     if (POST) {
@@ -342,10 +344,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
         factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
         factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          a[c][i] = fmaf(y[c][i], w[i], b[i]);
-          h[c][i] = fmaf(d.y_scale * gate[i], a[c][i], h[c][i]);
-        }
+        for (int i = 0; i < 8; ++i) h[c][i] = fmaf(d.y_scale * gate[i], fmaf(y[c][i], w[i], b[i]), h[c][i]);
       }
       widen<VEC>(gh_raw[c], d.h_type, gh[c]);
     }
@@ -390,24 +389,28 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float into[8];
       factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
       factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
+      if (g.gate_grad && d.gate_stride) {
+        float into[8];
+        factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, into);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) into[i] = d.y_scale * gh[c][i] * fmaf(y[c][i], w[i], into[i]);
+        put<VEC>(g.gate_grad, SZO_F32, token * g.gate_stride, p[c], into);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float t = d.y_scale * gh[c][i];
-        into[i] = t * a[c][i];
-        sums[kGate][c][i] += into[i];
         gh[c][i] = t * gate[i];
-        sums[kPostWeight][c][i] = fmaf(gh[c][i], y[c][i], sums[kPostWeight][c][i]);
-        sums[kPostBias][c][i] += gh[c][i];
+        const float s = d.gate_stride ? gh[c][i] : t;
+        sums[kPostWeight][c][i] = fmaf(s, y[c][i], sums[kPostWeight][c][i]);
+        sums[kPostBias][c][i] += s;
         if (POST) {
           gh[c][i] *= w[i];
           sum += gh[c][i];
           dot = fmaf(gh[c][i], y[c][i], dot);
         }
       }
-      if (g.gate_grad && d.gate_stride) put<VEC>(g.gate_grad, SZO_F32, token * g.gate_stride, p[c], into);
     }
     if (POST) {
       row_sums(m, 3, sum, dot);
@@ -435,23 +438,41 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
 // 64 neighbouring sums per workgroup: 16 rows of threads walk the partials, then add each other up in order.
 __global__ void __launch_bounds__(1024) block_sums_kernel(const float* __restrict__ partials, int64_t width, int sets, int count, const BlockArgs args) {
   __shared__ double rows[16][65];
-  const int column = threadIdx.x % 64, row = threadIdx.x / 64, set = blockIdx.y;
+  const int column = threadIdx.x % 64, row = threadIdx.x / 64;
   const int64_t i = (int64_t)blockIdx.x * 64 + column;
-  double s = 0.0;
-  if (i < width)
+  auto total = [&](int set) {
+    double s = 0.0;
+    if (i < width)
 #pragma unroll 4
-    for (int p = row; p < count; p += 16) s += (double)partials[((int64_t)p * sets + set) * width + i];
-  rows[row][column] = s;
-  __syncthreads();
-  for (int half = 8; half; half /= 2) {
-    if (row < half) rows[row][column] += rows[row + half][column];
+      for (int p = row; p < count; p += 16) s += (double)partials[((int64_t)p * sets + set) * width + i];
+    rows[row][column] = s;
     __syncthreads();
+    for (int half = 8; half; half /= 2) {
+      if (row < half) rows[row][column] += rows[row + half][column];
+      __syncthreads();
+    }
+    return rows[0][column];
+  };
+  const szo_block_desc& d = args.d;
+  const szo_block_grads& g = args.g;
+  const int set = blockIdx.y;
+  const bool gate_too = set == args.set_at[kPostWeight] && g.gate_grad && d.gate_stride == 0, biased = gate_too && d.post && d.post_bias;
+  const double sum = total(set);
+  double by_bias = 0.0;
+  if (biased) {
+    __syncthreads();
+    by_bias = total(args.set_at[kPostBias]);
   }
   if (row || i >= width) return;
-  float* const to[kSets] = {args.g.pre_weight_grad, args.g.pre_bias_grad, args.g.post_weight_grad, args.g.post_bias_grad, args.g.gate_grad};
-#pragma unroll
-  for (int k = 0; k < kSets; ++k)
-    if (args.set_at[k] == set) to[k][i] = (float)rows[0][column];
+  const double gate = d.gate && d.gate_stride == 0 ? (double)d.gate[i] : 1.0;
+  if (set == args.set_at[kPreWeight]) g.pre_weight_grad[i] = (float)sum;
+  else if (set == args.set_at[kPreBias]) g.pre_bias_grad[i] = (float)sum;
+  else if (set == args.set_at[kPostBias]) {
+    if (g.post_bias_grad) g.post_bias_grad[i] = (float)(gate * sum);
+  } else {
+    if (g.post_weight_grad) g.post_weight_grad[i] = (float)(gate * sum);
+    if (gate_too) g.gate_grad[i] = (float)(sum * (d.post && d.post_weight ? (double)d.post_weight[i] : 1.0) + (biased ? by_bias * (double)d.post_bias[i] : 0.0));
+  }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -559,13 +580,14 @@ int szo_block_norm_bwd(const szo_block_desc* d, const szo_block_grads* g, void* 
   a.d = *d;
   a.g = *g;
   a.waves = waves_of(d->width);
-  float* const wanted[kSets] = {g->pre_weight_grad, g->pre_bias_grad, g->post_weight_grad, g->post_bias_grad, d->gate_stride ? nullptr : g->gate_grad};
+  float* const by_gate = d->gate_stride ? nullptr : g->gate_grad;         // a sum over tokens too
+  const bool wanted[kSets] = {g->pre_weight_grad != nullptr, g->pre_bias_grad != nullptr, g->post_weight_grad || by_gate, g->post_bias_grad || (by_gate && d->post && d->post_bias)};
   for (int k = 0; k < kSets; ++k) a.set_at[k] = wanted[k] ? a.sets++ : -1;
   if (a.sets && (!workspace || !aligned_to(workspace, 16))) return SZO_EINVAL;
   hipStream_t s = (hipStream_t)stream;
   if (d->tokens == 0) {
-    for (int k = 0; k < kSets; ++k)
-      if (wanted[k] && zero_words(wanted[k], d->width, s)) return SZO_ELAUNCH;
+    for (float* sums : {g->pre_weight_grad, g->pre_bias_grad, g->post_weight_grad, g->post_bias_grad, by_gate})
+      if (sums && zero_words(sums, d->width, s)) return SZO_ELAUNCH;
     return SZO_OK;
   }
   a.partials = a.sets ? (float*)workspace : nullptr;
