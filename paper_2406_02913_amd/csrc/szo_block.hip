@@ -76,6 +76,20 @@ __device__ __forceinline__ Raw fetch(const void* base, int type, int64_t row, co
   return r;
 }
 
+// The first and the second 16 bytes of eight features by themselves (the second ones are there in fp32 alone).
+template <bool VEC>
+__device__ __forceinline__ words4 fetch_first(const void* base, int type, int64_t row, const Place<VEC>& p) {
+  words4 v = {};
+  if (base && p.first < p.width) v = *reinterpret_cast<const words4*>(static_cast<const char*>(base) + row * (type == SZO_F32 ? 4 : 2) + (uint32_t)p.first * (type == SZO_F32 ? 4u : 2u));
+  return v;
+}
+template <bool VEC>
+__device__ __forceinline__ words4 fetch_second(const void* base, int type, int64_t row, const Place<VEC>& p) {
+  words4 v = {};
+  if (base && p.first < p.width && type == SZO_F32) v = *reinterpret_cast<const words4*>(static_cast<const char*>(base) + row * 4 + (uint32_t)p.first * 4u + 16u);
+  return v;
+}
+
 template <bool VEC>
 __device__ __forceinline__ void widen(const Raw& r, int type, float (&v)[8]) {
   if (!VEC || type == SZO_F32) {
@@ -295,16 +309,48 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockArgs arg
   }
 }
 
+// Four sets of factors, 128 bytes a thread; wider rows have too many for two workgroups' LDS.
+constexpr int kFactors = 4;
+__host__ __device__ constexpr bool holds_factors(int ch, bool vec) { return vec && ch == 1; }
+
 // A workgroup walks rows and keeps what it adds up over them in registers, eight features of up to four sums a thread; no atomics, so the order is fixed.
-template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
+//   Bound by the memory's latency and by instructions: a row has four exchanges between its waves, and two workgroups a CU are all that the sums leave room for.  So the next row's
+// first 16 bytes a thread are asked for half a row ahead, what all tokens share lies in LDS (through L2 it was 64 KiB and more a row), and the usual case of one 16-bit type has kernels
+// without questions about types (SAME; -1: any types).  4096 tokens of 4096 in bf16, layer norms with biases and a shared gate: 72 us without all that, 67 with types and half of
+// the loads ahead, 62 with LDS and without loads ahead, 60 with both: 201 MB and 34 MB of partial sums, written and read.
+//   SAME: the type of y, h and x.
+template <int CH, bool VEC, int THREADS, bool LAYER, bool POST, int SAME>
 __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 : 1) block_norm_bwd_kernel(const BlockArgs args) {
   __shared__ float slots[4][kMostWaves][2];
   const szo_block_desc& d = args.d;
   const szo_block_grads& g = args.g;
+  const int y_type = SAME < 0 ? d.y_type : SAME, h_type = SAME < 0 ? d.h_type : SAME, x_type = SAME < 0 ? d.x_type : SAME;
   const int waves = args.waves, threads = waves * 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rows = blockDim.x / threads, row = wave / waves, thread = threadIdx.x - row * threads;
   const float inverse = 1.f / (float)d.width, own = features_of<CH, VEC>(wave - row * waves, waves, d.width);
   const Meeting m = {slots, waves, wave - row * waves, row * waves, (int)(threadIdx.x % 16) < waves ? features_of<CH, VEC>(threadIdx.x % 16, waves, d.width) : 0.f};
+  constexpr bool kHeld = holds_factors(CH, VEC);
+  extern __shared__ __attribute__((aligned(16))) float4 held[];        // [factor][2][thread], each thread's own features
+  if constexpr (kHeld) {
+    const Place<VEC> at(0, thread, threads, d.width);
+    const float* const from[kFactors] = {d.pre_weight, d.post_weight, d.post_bias, d.gate_stride ? nullptr : d.gate};
+#pragma unroll
+    for (int k = 0; k < kFactors; ++k) {
+      if (!from[k]) continue;
+      const Raw w = fetch<VEC>(from[k], SZO_F32, 0, at);
+      held[2 * k * blockDim.x + threadIdx.x] = __builtin_bit_cast(float4, w.a);
+      held[(2 * k + 1) * blockDim.x + threadIdx.x] = __builtin_bit_cast(float4, w.b);
+    }
+  }
+  auto shared_factor = [&](int k, const float* base, const Place<VEC>& at, float none, float (&v)[8]) {
+    if (!kHeld || !base) return factor<VEC>(base, 0, at, none, v);
+    const float4 lo = held[2 * k * blockDim.x + threadIdx.x], hi = held[(2 * k + 1) * blockDim.x + threadIdx.x];
+    v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+  };
+  auto gate_factor = [&](int64_t token, const Place<VEC>& at, float (&v)[8]) {
+    if (d.gate_stride) factor<VEC>(d.gate, token * d.gate_stride, at, 1.f, v);
+    else shared_factor(3, d.gate, at, 1.f, v);
+  };
   float sums[kSets][CH][8];
 #pragma unroll
   for (int s = 0; s < kSets; ++s)
@@ -312,6 +358,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sums[s][c][i] = 0.f;
+  constexpr bool kEarly = VEC && CH == 1;               // rows of more have registers for no more
+  words4 y_next = {}, h_next = {}, gx_next = {}, gh_next = {};
+  auto early = [&](int64_t token) {
+    if constexpr (kEarly) {
+      const Place<VEC> q(0, thread, threads, token < d.tokens ? d.width : 0);
+      y_next = fetch_first<VEC>(d.y, y_type, token * d.y_stride, q);
+      h_next = fetch_first<VEC>(g.x_out_grad ? d.h : nullptr, h_type, token * d.h_stride, q);
+      gx_next = fetch_first<VEC>(g.x_out_grad, x_type, token * g.x_out_stride, q);
+      gh_next = fetch_first<VEC>(g.h_out_grad, h_type, token * g.h_out_stride, q);
+    }
+  };
+  early((int64_t)blockIdx.x * rows + row);
   for (int64_t first = (int64_t)blockIdx.x * rows; first < d.tokens; first += (int64_t)gridDim.x * rows) {
     const int64_t token = first + row;
     const bool there = token < d.tokens;
@@ -320,14 +378,24 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
     Raw y_raw[CH], h_raw[CH], gx_raw[CH], gh_raw[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      y_raw[c] = fetch<VEC>(d.y, d.y_type, token * d.y_stride, p[c]);
-      h_raw[c] = fetch<VEC>(g.x_out_grad ? d.h : nullptr, d.h_type, token * d.h_stride, p[c]);
-      gx_raw[c] = fetch<VEC>(g.x_out_grad, d.x_type, token * g.x_out_stride, p[c]);
-      gh_raw[c] = fetch<VEC>(g.h_out_grad, d.h_type, token * g.h_out_stride, p[c]);
+      if constexpr (kEarly) {
+        y_raw[c] = Raw{y_next, fetch_second<VEC>(d.y, y_type, token * d.y_stride, p[c])};
+        h_raw[c] = Raw{h_next, fetch_second<VEC>(g.x_out_grad ? d.h : nullptr, h_type, token * d.h_stride, p[c])};
+      } else {
+        y_raw[c] = fetch<VEC>(d.y, y_type, token * d.y_stride, p[c]);
+        h_raw[c] = fetch<VEC>(g.x_out_grad ? d.h : nullptr, h_type, token * d.h_stride, p[c]);
+      }
+      if constexpr (kEarly) {
+        gx_raw[c] = Raw{gx_next, fetch_second<VEC>(g.x_out_grad, x_type, token * g.x_out_stride, p[c])};
+        gh_raw[c] = Raw{gh_next, fetch_second<VEC>(g.h_out_grad, h_type, token * g.h_out_stride, p[c])};
+      } else {
+        gx_raw[c] = fetch<VEC>(g.x_out_grad, x_type, token * g.x_out_stride, p[c]);
+        gh_raw[c] = fetch<VEC>(g.h_out_grad, h_type, token * g.h_out_stride, p[c]);
+      }
     }
     float y[CH][8], h[CH][8], gh[CH][8], gate[8], w[8], y_r = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], d.y_type, y[c]);
+    for (int c = 0; c < CH; ++c) widen<VEC>(y_raw[c], y_type, y[c]);
     if (POST) {
       float mean;
       row_stats<CH, VEC>(m, 0, y, p, LAYER, own, inverse, d.eps, mean, y_r);
@@ -335,19 +403,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      widen<VEC>(h_raw[c], d.h_type, h[c]);
+      widen<VEC>(h_raw[c], h_type, h[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[c][i] *= d.h_scale;
       if (d.y) {
         float b[8];
-        factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
-        factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
-        factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, b);
+        gate_factor(token, p[c], gate);
+        shared_factor(1, POST ? d.post_weight : nullptr, p[c], 1.f, w);
+        shared_factor(2, POST ? d.post_bias : nullptr, p[c], 0.f, b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[c][i] = fmaf(d.y_scale * gate[i], fmaf(y[c][i], w[i], b[i]), h[c][i]);
       }
-      widen<VEC>(gh_raw[c], d.h_type, gh[c]);
+      widen<VEC>(gh_raw[c], h_type, gh[c]);
     }
+    early(token + (int64_t)gridDim.x * rows);
     if (g.x_out_grad) {
       float u[CH][8], mean, r, sum = 0.f, dot = 0.f;
       row_stats<CH, VEC>(m, 1, h, p, LAYER, own, inverse, d.eps, mean, r);
@@ -356,8 +425,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         float pre[8];
-        widen<VEC>(gx_raw[c], d.x_type, u[c]);
-        factor<VEC>(d.pre_weight, 0, p[c], 1.f, pre);
+        widen<VEC>(gx_raw[c], x_type, u[c]);
+        shared_factor(0, d.pre_weight, p[c], 1.f, pre);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPreWeight][c][i] = fmaf(u[c][i], h[c][i], sums[kPreWeight][c][i]);
@@ -381,7 +450,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
         float to[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) to[i] = d.h_scale * gh[c][i];
-        put<VEC>(g.h_grad, d.h_type, token * g.h_stride, p[c], to);
+        put<VEC>(g.h_grad, h_type, token * g.h_stride, p[c], to);
       }
     }
     if (!d.y) continue;
@@ -389,11 +458,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      factor<VEC>(d.gate, token * d.gate_stride, p[c], 1.f, gate);
-      factor<VEC>(POST ? d.post_weight : nullptr, 0, p[c], 1.f, w);
+      gate_factor(token, p[c], gate);
+      shared_factor(1, POST ? d.post_weight : nullptr, p[c], 1.f, w);
       if (g.gate_grad && d.gate_stride) {
         float into[8];
-        factor<VEC>(POST ? d.post_bias : nullptr, 0, p[c], 0.f, into);
+        shared_factor(2, POST ? d.post_bias : nullptr, p[c], 0.f, into);
 #pragma unroll
         for (int i = 0; i < 8; ++i) into[i] = d.y_scale * gh[c][i] * fmaf(y[c][i], w[i], into[i]);
         put<VEC>(g.gate_grad, SZO_F32, token * g.gate_stride, p[c], into);
@@ -422,7 +491,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 && CH == 1 && VEC ? 4 
         for (int i = 0; i < 8; ++i) gh[c][i] = y_r * fmaf(-y[c][i], dot, gh[c][i] - sum);
     }
 #pragma unroll
-    for (int c = 0; c < CH; ++c) put<VEC>(g.y_grad, d.y_type, token * g.y_stride, p[c], gh[c]);
+    for (int c = 0; c < CH; ++c) put<VEC>(g.y_grad, y_type, token * g.y_stride, p[c], gh[c]);
   }
   if (!args.partials) return;
   float* to = args.partials + ((int64_t)blockIdx.x * rows + row) * args.sets * d.width;
@@ -516,23 +585,44 @@ bool inputs_vec(const szo_block_desc* d) {
          aligned_to(d->post_weight, 16) && aligned_to(d->post_bias, 16) && aligned_to(d->pre_weight, 16) && aligned_to(d->pre_bias, 16);
 }
 
+template <int CH, bool VEC, int THREADS, bool LAYER, bool POST, int SAME>
+int launch_backward(const BlockArgs& a, int64_t groups, int threads, hipStream_t s) {
+  static std::atomic<uint64_t> raised{0};
+  const size_t lds = holds_factors(CH, VEC) ? (size_t)threads * kFactors * 2 * sizeof(float4) : 0;
+  if (lds > 48 * 1024) {
+    const int rc = set_lds_limit_once(raised, (const void*)block_norm_bwd_kernel<CH, VEC, THREADS, LAYER, POST, SAME>, lds);
+    if (rc != SZO_OK) return rc;
+  }
+  block_norm_bwd_kernel<CH, VEC, THREADS, LAYER, POST, SAME><<<dim3((unsigned)groups), threads, lds, s>>>(a);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
+}
 template <int CH, bool VEC, int THREADS, bool LAYER, bool POST>
-void launch(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+int launch(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
   const int threads = 64 * a.waves * rows_of(a.waves);
-  if (backward) block_norm_bwd_kernel<CH, VEC, THREADS, LAYER, POST><<<dim3((unsigned)groups), threads, 0, s>>>(a);
-  else block_norm_kernel<CH, VEC, THREADS, LAYER, POST><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+  if (backward) {
+    if constexpr (VEC) {
+      const bool same = a.d.y_type == a.d.h_type && a.d.h_type == a.d.x_type;
+      if (same && a.d.h_type == SZO_BF16) return launch_backward<CH, VEC, THREADS, LAYER, POST, SZO_BF16>(a, groups, threads, s);
+      if (same && a.d.h_type == SZO_F16) return launch_backward<CH, VEC, THREADS, LAYER, POST, SZO_F16>(a, groups, threads, s);
+    }
+    return launch_backward<CH, VEC, THREADS, LAYER, POST, -1>(a, groups, threads, s);
+  }
+  block_norm_kernel<CH, VEC, THREADS, LAYER, POST><<<dim3((unsigned)groups), threads, 0, s>>>(a);
+  SZO_LAUNCH_CHECK();
+  return SZO_OK;
 }
 template <int CH, bool VEC, int THREADS>
-void launch_norm(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+int launch_norm(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
   const bool layer = a.d.norm == SZO_NORM_LAYER, post = a.d.y && a.d.post;
-  if (layer) post ? launch<CH, VEC, THREADS, true, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, true, false>(a, groups, backward, s);
-  else post ? launch<CH, VEC, THREADS, false, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, false, false>(a, groups, backward, s);
+  if (layer) return post ? launch<CH, VEC, THREADS, true, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, true, false>(a, groups, backward, s);
+  return post ? launch<CH, VEC, THREADS, false, true>(a, groups, backward, s) : launch<CH, VEC, THREADS, false, false>(a, groups, backward, s);
 }
 template <bool VEC>
-void launch_all(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
-  if (a.d.width <= 4096) launch_norm<1, VEC, 512>(a, groups, backward, s);
-  else if (a.d.width <= 8192) launch_norm<2, VEC, 512>(a, groups, backward, s);
-  else launch_norm<2, VEC, 1024>(a, groups, backward, s);
+int launch_all(const BlockArgs& a, int64_t groups, bool backward, hipStream_t s) {
+  if (a.d.width <= 4096) return launch_norm<1, VEC, 512>(a, groups, backward, s);
+  if (a.d.width <= 8192) return launch_norm<2, VEC, 512>(a, groups, backward, s);
+  return launch_norm<2, VEC, 1024>(a, groups, backward, s);
 }
 
 }  // namespace
@@ -554,9 +644,7 @@ int szo_block_norm(const szo_block_desc* d, void* stream) {
   const int64_t groups = (d->tokens - 1) / rows + 1;
   if (groups > kMostGroups) return SZO_EUNSUPPORTED;
   const bool vec = inputs_vec(d) && vec_ok(d->h_out, d->h_out_stride, d->h_type) && vec_ok(d->x_out, d->x_out_stride, d->x_type);
-  vec ? launch_all<true>(a, groups, false, (hipStream_t)stream) : launch_all<false>(a, groups, false, (hipStream_t)stream);
-  SZO_LAUNCH_CHECK();
-  return SZO_OK;
+  return vec ? launch_all<true>(a, groups, false, (hipStream_t)stream) : launch_all<false>(a, groups, false, (hipStream_t)stream);
 }
 
 size_t szo_block_workspace_bytes(const szo_block_desc* d) {
@@ -595,8 +683,8 @@ int szo_block_norm_bwd(const szo_block_desc* d, const szo_block_grads* g, void* 
                    vec_ok(g->y_grad, g->y_stride, d->y_type) && vec_ok(g->h_grad, g->h_stride, d->h_type) &&
                    (!d->gate_stride || vec_ok(g->gate_grad, g->gate_stride, SZO_F32));
   const int64_t groups = bwd_groups(d);
-  vec ? launch_all<true>(a, groups, true, s) : launch_all<false>(a, groups, true, s);
-  SZO_LAUNCH_CHECK();
+  const int done = vec ? launch_all<true>(a, groups, true, s) : launch_all<false>(a, groups, true, s);
+  if (done != SZO_OK) return done;
   if (a.sets) {
     block_sums_kernel<<<dim3((unsigned)((d->width + 63) / 64), (unsigned)a.sets), 1024, 0, s>>>(a.partials, d->width, a.sets, (int)groups * rows_of(a.waves), a);
     SZO_LAUNCH_CHECK();
