@@ -20,7 +20,9 @@ CASES = [(1, 1, False, True, None, "f32", "f32", "f32", "plain"), (3, 5, True, T
          (4, 4096, False, True, "row", "f32", "f32", "bf16", "plain"), (3, 4104, True, True, "row", "f32", "bf16", "f32", "plain"),
          (2, 5001, True, True, "token", "f32", "f32", "f32", "odd"), (700, 4096, True, True, "row", "bf16", "bf16", "bf16", "plain"),
          (2, 8200, True, True, "row", "bf16", "f32", "f32", "plain"), (3, 16384, False, True, "token", "f32", "bf16", "bf16", "plain"),
-         (2, 12345, True, True, "row", "f16", "f32", "bf16", "plain")]
+         (2, 12345, True, True, "row", "f16", "f32", "bf16", "plain"), (5000, 512, True, True, "row", "f16", "f16", "f16", "plain"),
+         (2100, 1024, False, False, "token", "bf16", "bf16", "bf16", "plain"), (530, 2048, False, True, "row", "f16", "f16", "f16", "strided"),
+         (520, 1600, True, True, "token", "f32", "f32", "f32", "plain"), (300, 8192, True, True, "row", "bf16", "bf16", "bf16", "plain")]
 
 
 def _np(t):
