@@ -7,6 +7,8 @@
 // logit, where it has it), and a small kernel joins the tiles of a row.  The backward computes them again, turns them into d, rounded to 16 bits, and multiplies that
 // twice.  d is in memory for a piece of the vocabulary at a time.  Three products of the same size, bound by the matrix cores for many rows and by one pass
 // over the weight for few.
+//   A head of 32000 entries of width 4096 in bf16, forward: 16 rows 46 to 62 us (262 MB of weight, read at 5.7 to 4.2 TB/s), 300 rows 90, 4096 rows 800 to 830 (1.30 to 1.34 PFLOP/s).  Backward
+// of 4096 rows 2520: d 859 with 262 MB written, dx 759 (1.41 PFLOP/s), dW 845, the copy of x 21.  200 rows of width 2048 in fp16 157: 44, 48 and 6 for its parts, 56, 3.5.
 #include <algorithm>
 #include "szo_product.h"
 
