@@ -86,7 +86,7 @@ def test_sums_of_a_block_norm_fit_their_workspace():
             waves = -(-width // (512 if width <= 4096 else 1024))
             rows = max(1, 4 // waves)
             groups = min(-(-tokens // rows), 256 * max(1, (16 if width <= 4096 else 8) // (waves * rows)))
-            assert size == 5 * 4 * width * groups * rows
+            assert size == 4 * 4 * width * groups * rows            # four sums in fp32: a gate that tokens share has none of its own
 
 
 # ---- attention behind shared prefixes ------------------------------------------------------------
