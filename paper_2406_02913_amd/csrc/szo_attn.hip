@@ -308,7 +308,7 @@ struct GroupTile {
     first_row = (tile - (start * a.group / 32 + e)) * 32;
     blocks = a.d.cache.pages == 0 ? 0 : (int)min((int64_t)min(max(tokens, 0) / kKvBlock, sh.most_blocks), (int64_t)a.d.cache.max_pages * a.blocks_per_page);
   }
-  __device__ __forceinline__ bool empty() const { return first >= last || first_row >= rows; }
+  __device__ __forceinline__ bool empty() const { return first >= last || (uint32_t)first_row >= (uint32_t)rows; }           // starts that do not ascend: below 0
 };
 
 // What a tile goes over: the shared blocks (slot -1), then the own ones of each sequence that has rows in it; lane k has those of slot k.
@@ -506,7 +506,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     see_all = -wave_max(all_to);
     see_all_from = wave_max(all_from);
     segments.own_page = lane < slots && segments.own_count > 0 ? page_table[(int64_t)segments.own_sequence * max_pages + sh.by_page.of(segments.own_first)] : -1;
-    segments.sequence = g.first;
+    segments.sequence = __builtin_amdgcn_readlane(segments.own_sequence, 0);            // one that has new tokens: of others no pages need be there any more
     segments.shared_first = -wave_max(first_seen) / kKvBlock;
     segments.shared_count = max(min(g.blocks, (reach + kKvBlock - 1) / kKvBlock) - segments.shared_first, 0);
     // Every walker takes a run of the shared blocks and a run of the own ones, which are slower (masked, and from memory that no other tile reads: 4500 cycles beside 2600); the

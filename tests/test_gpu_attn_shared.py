@@ -161,6 +161,14 @@ def _plain(seed=5, B=6, D=128, heads=2, group=4, pre=256):
     return s, q, groups, lengths, call
 
 
+def test_a_group_whose_first_sequence_is_done(monkeypatch):
+    """It has no new tokens, and its pages are somebody else's or nobody's by now."""
+    lengths = [300, 290, 310, 275, 260, 333]
+    s = Shared(lengths, [0, 3, 6], [256, 224], 2, 128, 32)
+    s.b.table[0], s.b.table[3] = -1, np.roll(s.b.table[4], 3)
+    s.check(monkeypatch, [0] + lengths[1:3] + [64] + lengths[4:], [0, 1, 2, 0, 3, 1], 4, "bf16")
+
+
 def test_queries_left_out_and_rows_behind_the_last_sequence_stay_as_they_are():
     s, q, groups, lengths, _ = _plain()
     q = torch.randn(20, 8, 128, device=DEV).bfloat16()
