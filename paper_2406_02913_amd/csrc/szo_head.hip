@@ -99,11 +99,16 @@ __global__ void __launch_bounds__(kThreads, 2) head_stats_kernel(const HeadArgs 
   const float by = d.scale * kLog2e;
   const int mine = wi * L::kWaveV + 4 * (lane >> 4);              // this lane's first entry
   const int there = (int)min((int64_t)BV, d.vocab - v0);
+  int32_t targets[L::TJ];                                // all of them before the first store, which no load passes
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t token = t0 + wj * L::kWaveT + 16 * j + (lane & 15);
+    targets[j] = token < d.rows && d.targets ? d.targets[token] : -1;
+  }
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
     const int column = wj * L::kWaveT + 16 * j + (lane & 15);
-    const int64_t token = t0 + column;
-    const int64_t target = token < d.rows && d.targets ? d.targets[token] : -1;
+    const int64_t token = t0 + column, target = targets[j];
     float most = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < L::TI; ++i)
@@ -150,6 +155,8 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
   const int lane = threadIdx.x & 63;
   if (row >= d.rows) return;
   const float2* parts = a.parts + row * a.tiles_v;
+  const int64_t target = d.targets ? d.targets[row] : -1;       // asked for beside the parts
+  const float hit = a.hit[row];                                 // nothing that counts without a target
   const float by = d.scale * kLog2e;
   float most = -__builtin_inff(), sum = 0.f;
 #pragma unroll 4
@@ -164,9 +171,8 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
   if (lane) return;
   if (d.stats) { d.stats[2 * row] = top; d.stats[2 * row + 1] = sum; }
   if (!d.logp) return;
-  const int64_t target = d.targets ? d.targets[row] : -1;
   float logp = 0.f;
-  if (target >= 0 && target < d.vocab) logp = sum == 0.f ? -__builtin_inff() : (a.hit[row] - top) * d.scale - logf(sum);
+  if (target >= 0 && target < d.vocab) logp = sum == 0.f ? -__builtin_inff() : (hit - top) * d.scale - logf(sum);
   d.logp[row] = logp;
 }
 
@@ -228,13 +234,22 @@ __global__ void __launch_bounds__(kThreads, 2) head_grad_kernel(const HeadArgs a
   const float by = d.scale * kLog2e;
   const int mine = wi * L::kWaveV + 4 * (lane >> 4);
   const int there = (int)min((int64_t)BV, d.vocab - v0);
+  float gs[L::TJ], mosts[L::TJ], sums[L::TJ];            // all loads before the first store, which none passes
+  int32_t targets[L::TJ];
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
     const int64_t token = t0 + wj * L::kWaveT + 16 * j + (lane & 15);
-    if (token >= a.rows64) continue;
     const bool in = token < d.rows;
-    const float g = in ? a.row_grad[token] : 0.f, most = in ? d.stats[2 * token] : 0.f, sum = in ? d.stats[2 * token + 1] : 1.f;
-    const int64_t target = in && d.targets ? d.targets[token] : -1;
+    gs[j] = in ? a.row_grad[token] : 0.f;
+    mosts[j] = in ? d.stats[2 * token] : 0.f;
+    sums[j] = in ? d.stats[2 * token + 1] : 1.f;
+    targets[j] = in && d.targets ? d.targets[token] : -1;
+  }
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t token = t0 + wj * L::kWaveT + 16 * j + (lane & 15), target = targets[j];
+    if (token >= a.rows64) continue;
+    const float g = gs[j], most = mosts[j], sum = sums[j];
     const bool none = target < 0 || target >= d.vocab || sum == 0.f;
     const int hit = target >= v0 && target < v0 + there ? (int)(target - v0) - mine : -1;
     const float share = g / sum;
