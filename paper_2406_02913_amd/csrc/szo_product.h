@@ -9,7 +9,8 @@
 //   columns  [r][128 of i], four r to an instruction: 16-wide groups are exchanged by r mod 4 and (r / 8) mod 2, to the same end; a read forms its address
 // Fragments are read from LDS a few groups of products before they are used, across the one barrier of a step.
 //   256 x 256: a step takes 1.33 us, 1.28 to 1.41 PFLOP/s with the whole chip at work (4096 x 32000 x 4096; the card's own large product 1.45 there, 1.59 at 16384 cubed), bound by the matrix
-// cores and, a fifth, by what stands at a step's barrier: a CU holds one workgroup, whose sums take half of its registers.
+// cores and, a fifth, by what stands at a step's barrier: a CU holds one workgroup, whose sums take half of its registers.  Four waves with twice the sums each, which read
+// a third less from LDS: 801 -> 1119, and 300 rows in tiles of 128 x 320 90 -> 118; a wave alone on its SIMD issues too slowly.
 #pragma once
 #include "szo_internal.h"
 #include "szo_types.h"
