@@ -31,7 +31,7 @@ struct HeadArgs {
   int64_t rows64;                    // rows, rounded up to a multiple of 64
   uint16_t* grad;                    // d [rows64][pitch]
   const float* row_grad;             // [rows]: scale * gradient * lift, 0 where the target is ignored
-  const float* lift;                 // [2]: the power of two that d is multiplied by, and its inverse
+  const float* lift;                 // [2]: what d is multiplied by, and its inverse
   const uint16_t* x_copy;            // x [rows64][width], rows without a target 0
   float* sums;                       // x_grad in parts [splits][rows][width]
   int splits, steps, add;            // parts of a piece, 64-wide steps of it, whether to add to what is there
@@ -178,8 +178,9 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
 
-// The first workgroup: scale * gradient of each row, lifted for fp16 by the power of two that takes the largest to 2^13 .. 2^14: with |1 - p| <= 1 nothing overflows, and what is
-// 2^-27 of the largest still has all its bits.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
+// The first workgroup: scale * gradient of each row, times a factor that takes the largest to just below a power of two, where a rounding is smallest relative to the value: most losses have
+// one gradient for all rows, and d of an unlikely target is nearly that, so its rounding is the whole row's (1.004 in bf16 would be off by 2^-8, 1.98 is by half of it).  For fp16 the
+// power is 2^14: with |1 - p| <= 1 nothing overflows, and what is 2^-27 of the largest still has all its bits.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
 __global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* lift, int64_t rows64, uint16_t* x_copy) {
   if (blockIdx.x > 0) {
     const int per = d.width / 8;
@@ -197,21 +198,20 @@ __global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d
     const int64_t t = d.targets ? d.targets[i] : -1;
     return t >= 0 && t < d.vocab ? grad[i] * d.scale : 0.f;
   };
-  if (d.type == SZO_F16)
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
-      const float g = fabsf(of(i));
-      if (g < __builtin_inff()) most = fmaxf(most, g);
-    }
+  for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
+    const float g = fabsf(of(i));
+    if (g < __builtin_inff()) most = fmaxf(most, g);
+  }
   most = lanes_max<64>(most);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
   __syncthreads();
   for (int w = 0; w < 4; ++w) most = fmaxf(most, part[w]);
-  const int up = most > 0.f ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
-  const float by = __builtin_amdgcn_ldexpf(1.f, up);
+  const int up = most > 0.f && d.type == SZO_F16 ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
+  const float fill = most > 0.f ? 0.992f / __builtin_amdgcn_frexp_mantf(most) : 1.f, by = __builtin_amdgcn_ldexpf(fill, up);
 #pragma unroll 4
   for (int64_t i = threadIdx.x; i < d.rows; i += 256) row_grad[i] = of(i) * by;
-  if (threadIdx.x == 0) { lift[0] = by; lift[1] = __builtin_amdgcn_ldexpf(1.f, -up); }
+  if (threadIdx.x == 0) { lift[0] = by; lift[1] = __builtin_amdgcn_ldexpf(1.f / fill, -up); }
 }
 
 // Rows of nothing.

@@ -108,6 +108,27 @@ def test_backward(case):
     assert (gx[~torch.from_numpy(there[:, 0]).to(DEV)] == 0).all()
 
 
+@pytest.mark.parametrize("g", [1.0042, 1.0, 1.97, 0.502, 3.1e-5])
+def test_a_gradient_that_all_rows_share_is_rounded_well(g):
+    """Targets that are unlikely: d is nearly the gradient in every row, and its rounding the whole row's error."""
+    R, V, K = 64, 3000, 256
+    rng = np.random.default_rng(7)
+    x, w = (torch.from_numpy(a).bfloat16().to(DEV) for a in (rng.standard_normal((R, K)) * 0.1, rng.standard_normal((V, K)) * 0.1))
+    t = torch.from_numpy(rng.permutation(V)[:R].astype(np.int32)).to(DEV)
+    _, stats = forward(x, w, t)
+    d = szo.make_head_desc(x, w, t, stats=stats)
+    by_x, by_w = torch.empty_like(x), torch.empty_like(w)
+    szo.szo_head_logprobs_bwd(d, torch.full((R,), g, device=DEV), by_x, by_w, _room(szo.szo_head_bwd_workspace_bytes(d)))
+    p = np.exp(od.log_probs(_np(x) @ _np(w).T))
+    assert p.max() < 2.0 ** -6
+    d = -g * p
+    d[np.arange(R), t.cpu().numpy()] += g
+    # d lies between 1.95 and 1.99 times a power of two: off by 2^-8 / 1.95 of it at most; the result's own rounding is 2^-8 / sqrt(3) in the mean of squares, at most
+    bound = 2.0 ** -8 * np.sqrt(1 / 1.95 ** 2 + 1 / 3)
+    for got, want in ((by_x, d @ _np(w)), (by_w, d.T @ _np(x))):
+        assert np.linalg.norm(_np(got) - want) <= bound * np.linalg.norm(want), np.linalg.norm(_np(got) - want) / np.linalg.norm(want)
+
+
 def test_one_gradient_alone_and_no_targets():
     x, w, t, rng = _setup(70, 600, 128, "bf16")
     _, stats = forward(x, w, t)
