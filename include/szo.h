@@ -426,8 +426,9 @@ size_t szo_attn_workspace_bytes(const szo_attn_desc* desc /* host */);
 int szo_attn_plan(const szo_attn_desc* desc /* host */, int32_t* plan /* host, 4 */);
 
 /* The same attention for sequences that share prefixes: candidate answers behind one prompt, continuations of one, questions behind the same examples.
- * Sequences group_start[g] to group_start[g + 1] - 1 form a group, and the first shared[g] tokens of every one of them are the same, on the pages that the page
- * table names for them all (or on copies: those of one of them that has new tokens are read).  Tiles of 32 rows (tokens times query heads of a key head) of a group's sequences go
+ * Sequences group_start[g] to group_start[g + 1] - 1 form a group, and the first shared[g] tokens of every one of them are the same (of a shorter one those
+ * that it has), on the pages that the page table names for them all or on copies.  A shared block is read from the row of a sequence whose new tokens see it: pages behind a sequence's length, or
+ * that its window has left, need not be there.  Tiles of 32 rows (tokens times query heads of a key head) of a group's sequences go
  * over the shared blocks together and then over each one's own; the result is that of szo_attn_cached up to the order of sums.  Of
  * shared[g] whole blocks of 32 tokens count, max_shared tokens at most; tokens behind a sequence's length and masked ones have no influence here either.  Sequences
  * of no group share nothing. */

@@ -311,49 +311,6 @@ struct GroupTile {
   __device__ __forceinline__ bool empty() const { return first >= last || (uint32_t)first_row >= (uint32_t)rows; }           // starts that do not ascend: below 0
 };
 
-// What a tile goes over: the shared blocks (slot -1), then the own ones of each sequence that has rows in it; lane k has those of slot k.
-struct Segments {
-  int shared_first, shared_count, sequence;          // the shared ones, read by the page table's row of this sequence
-  int own_sequence, own_first, own_count, own_page;  // this lane's slot; where the first of its blocks lies, so that entering a segment waits for no page table
-  __device__ __forceinline__ int count(int slot) const { return slot < 0 ? shared_count : __builtin_amdgcn_readlane(own_count, slot); }
-};
-struct SegmentWalk {
-  int slot, left, block, page_at, sub, per_page;     // blocks of the segment from this one on, the block's number in its sequence and where it lies
-  int own_from;                                      // of all slots' blocks, the first one of this walk
-  bool entered;                                      // at a slot's first block
-  const int32_t* table;
-  // Shared blocks from `at` to `to`, then slots' ones.
-  __device__ __forceinline__ void begin(const Segments& g, int at, int to, const int32_t* page_table, int max_pages, const Divisor& by_page) {
-    slot = at < to ? -1 : 0;
-    enter(g, at < to ? at : own_from, page_table, max_pages, by_page);
-    if (at < to) left = to - at;
-  }
-  __device__ __forceinline__ void enter(const Segments& g, int at, const int32_t* page_table, int max_pages, const Divisor& by_page) {
-    int n = g.count(slot);
-    while (at >= n) { at -= n; n = g.count(++slot); }          // blocks asked for are there
-    left = n - at;
-    block = (slot < 0 ? g.shared_first : __builtin_amdgcn_readlane(g.own_first, slot)) + at;
-    table = page_table + (int64_t)(slot < 0 ? g.sequence : __builtin_amdgcn_readlane(g.own_sequence, slot)) * max_pages;
-    page_at = by_page.of(block);
-    sub = block - page_at * per_page;
-    entered = slot >= 0 && at == 0;
-  }
-  __device__ __forceinline__ void step(const Segments& g, const int32_t* page_table, int max_pages, const Divisor& by_page) {
-    entered = false;
-    if (--left > 0) {
-      ++block;
-      if (++sub == per_page) { sub = 0; ++page_at; }
-    } else {
-      ++slot;
-      enter(g, slot == 0 ? own_from : 0, page_table, max_pages, by_page);
-    }
-  }
-  __device__ __forceinline__ int at(const Segments& g, const szo_kv_cache& c, int head) const {
-    const int page = entered ? __builtin_amdgcn_readlane(g.own_page, slot) : table[page_at];
-    return (uint32_t)page >= (uint32_t)c.pages ? -1 : (page * c.kv_heads + head) * per_page + sub;
-  }
-};
-
 // A value of all lanes: largest, sum.
 template <int CTRL> __device__ __forceinline__ int lane_permuted(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false); }
 template <typename F>
@@ -372,6 +329,64 @@ __device__ __forceinline__ int wave_of(int v, F f) {
 }
 __device__ __forceinline__ int wave_max(int v) { return wave_of(v, [](int a, int b) { return max(a, b); }); }
 __device__ __forceinline__ int wave_add(int v) { return wave_of(v, [](int a, int b) { return a + b; }); }
+
+// What a tile goes over: the shared blocks (slot -1), then the own ones of each sequence that has rows in it; lane k has those of slot k.
+//   A shared block is looked up in the page table's row of a sequence whose rows see it.  Of the others' nothing need be there: a sequence may end inside the prefix, or its window have left
+// it.  Of those whose windows begin at the block or before it that is the one that sees furthest, so that a copy of a page that is not full for another one is not read for it.
+typedef __attribute__((address_space(3))) volatile int* sight_at;
+struct Segments {
+  int shared_first, shared_count;
+  sight_at sights;                                   // 64 pairs, each lane its own: first block that its slot's rows see, tokens up to which they do; read too seldom for registers
+  int reach;                                         // of all slots
+  int own_sequence, own_first, own_count, own_page;  // this lane's slot; where the first of its blocks lies, so that entering a segment waits for no page table
+  __device__ __forceinline__ int count(int slot) const { return slot < 0 ? shared_count : __builtin_amdgcn_readlane(own_count, slot); }
+};
+struct SegmentWalk {
+  int slot, left, block, page_at, sub, per_page;     // blocks of the segment from this one on, the block's number in its sequence and where it lies
+  int own_from;                                      // of all slots' blocks, the first one of this walk
+  bool entered;                                      // at a slot's first block
+  const int32_t* table;
+  int until;                                         // shared blocks before this one are looked up in the row that `table` is
+  // Shared blocks from `at` to `to`, then slots' ones.
+  __device__ __forceinline__ void begin(const Segments& g, int at, int to, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    slot = at < to ? -1 : 0;
+    enter(g, at < to ? at : own_from, page_table, max_pages, by_page);
+    if (at < to) left = to - at;
+  }
+  __device__ __forceinline__ void enter(const Segments& g, int at, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    int n = g.count(slot);
+    while (at >= n) { at -= n; n = g.count(++slot); }          // blocks asked for are there
+    left = n - at;
+    block = (slot < 0 ? g.shared_first : __builtin_amdgcn_readlane(g.own_first, slot)) + at;
+    if (slot < 0) look_up(g, page_table, max_pages);
+    else table = page_table + (int64_t)__builtin_amdgcn_readlane(g.own_sequence, slot) * max_pages;
+    page_at = by_page.of(block);
+    sub = block - page_at * per_page;
+    entered = slot >= 0 && at == 0;
+  }
+  // Without windows one row serves for all blocks, with them the next one takes over where the last one's sight ends.
+  __device__ __forceinline__ void look_up(const Segments& g, const int32_t* page_table, int max_pages) {
+    const sight_at mine = g.sights + 2 * (threadIdx.x % 64);
+    const int from = mine[0], to = mine[1], sight = from <= block ? to : 0, most = wave_max(sight), lane = __builtin_ctzll(__ballot(sight == most));
+    table = page_table + (int64_t)__builtin_amdgcn_readlane(g.own_sequence, lane) * max_pages;
+    until = most == g.reach ? 0x7FFFFFFF : max(most / kKvBlock, block + 1);
+  }
+  __device__ __forceinline__ void step(const Segments& g, const int32_t* page_table, int max_pages, const Divisor& by_page) {
+    entered = false;
+    if (--left > 0) {
+      ++block;
+      if (++sub == per_page) { sub = 0; ++page_at; }
+      if (slot < 0 && block >= until) look_up(g, page_table, max_pages);
+    } else {
+      ++slot;
+      enter(g, slot == 0 ? own_from : 0, page_table, max_pages, by_page);
+    }
+  }
+  __device__ __forceinline__ int at(const Segments& g, const szo_kv_cache& c, int head) const {
+    const int page = entered ? __builtin_amdgcn_readlane(g.own_page, slot) : table[page_at];
+    return (uint32_t)page >= (uint32_t)c.pages ? -1 : (page * c.kv_heads + head) * per_page + sub;
+  }
+};
 
 // WR waves side by side over rows, WK over the cache, every wave with what it reads straight from memory.
 //   A step computes the weights of block j and its share of the output beside the scores of block j + 1: matrix and vector instructions of
@@ -506,7 +521,13 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
     see_all = -wave_max(all_to);
     see_all_from = wave_max(all_from);
     segments.own_page = lane < slots && segments.own_count > 0 ? page_table[(int64_t)segments.own_sequence * max_pages + sh.by_page.of(segments.own_first)] : -1;
-    segments.sequence = __builtin_amdgcn_readlane(segments.own_sequence, 0);            // one that has new tokens: of others no pages need be there any more
+    const int slot_first = max(token_first - slot_start, 0);
+    const bool sees = lane < slots && slot_first <= slot_last;
+    __shared__ int sights[WR * WK][64][2];
+    segments.sights = (sight_at)&sights[wave][0][0];
+    segments.sights[2 * lane] = sees ? window_from(slot_behind + slot_first) / kKvBlock : 0;
+    segments.sights[2 * lane + 1] = !sees ? 0 : d.causal ? max(min(slot_length, slot_behind + slot_last + 1), 0) : slot_length;
+    segments.reach = reach;
     segments.shared_first = -wave_max(first_seen) / kKvBlock;
     segments.shared_count = max(min(g.blocks, (reach + kKvBlock - 1) / kKvBlock) - segments.shared_first, 0);
     // Every walker takes a run of the shared blocks and a run of the own ones, which are slower (masked, and from memory that no other tile reads: 4500 cycles beside 2600); the
@@ -529,7 +550,7 @@ __device__ __forceinline__ void attn_walk(const int32_t* q_start, const int32_t*
   if (j0 < j1) {
     // A block without a page is read as block 0 and masked as a whole; behind the last block the last one stands in, for nothing.
     Walk walk(SHARED ? 0 : j0, bpp);
-    SegmentWalk piece = {-1, 0, 0, 0, 0, bpp, own_from, false, nullptr};
+    SegmentWalk piece = {-1, 0, 0, 0, 0, bpp, own_from, false, nullptr, 0};
     int now, next, block_now = 0, slot_now = -1, block_next = 0, slot_next = -1;
     if constexpr (SHARED) {
       piece.begin(segments, shared_from, shared_to, page_table, max_pages, sh.by_page);
