@@ -340,7 +340,8 @@ def _gate(t, T, H):
 
 def make_block_desc(y, h, h_out=None, x_out=None, norm=NORM_RMS, post=None, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None,
                     eps=1e-6, y_scale=1.0, h_scale=1.0, x_type=None):
-    """y, h [tokens, width] (one may be None), rows any distance apart; weights and biases fp32 [width]; gate fp32 [width] or [tokens, width].  `post` is on where a
+    """y, h [tokens, width] (one may be None), rows any distance apart; weights and biases fp32 [width]; gate fp32 [width] or [tokens, width]; one
+    that is expanded over tokens is a row that they share.  `post` is on where a
     weight or bias of it is given, unless said otherwise.  Without outputs: for the backward (x_type: torch type of the gradient by x_out, fp32, bf16 or fp16)."""
     import torch
     some = h if h is not None else y
@@ -357,7 +358,7 @@ def make_block_desc(y, h, h_out=None, x_out=None, norm=NORM_RMS, post=None, post
     d.gate, d.gate_stride = _gate(gate, T, H)
     d.h_out, d.h_out_stride = _rows(h_out, h_of, T, H)
     d.x_out, d.x_out_stride = _rows(x_out, x_of, T, H)
-    d.gated = None if gate is None else gate.dim()
+    d.gated = None if gate is None else 1 if d.gate_stride == 0 and T != 1 else gate.dim()       # axes of its gradient
     d.x_given = x_out is not None or x_type is not None
     d.types = y_of, h_of, x_of
     d.keep = (y, h, h_out, x_out, post_weight, post_bias, gate, pre_weight, pre_bias)
@@ -366,7 +367,7 @@ def make_block_desc(y, h, h_out=None, x_out=None, norm=NORM_RMS, post=None, post
 
 def make_block_grads(desc, x_out_grad=None, h_out_grad=None, y_grad=None, h_grad=None, gate_grad=None, post_weight_grad=None, post_bias_grad=None,
                      pre_weight_grad=None, pre_bias_grad=None):
-    """Gradients of what make_block_desc() was given, of the same shapes and types; None: 0 for those by the outputs, not wanted for the others.  A descriptor without
+    """Gradients of what make_block_desc() was given, of the same shapes and types (by a gate that is expanded over tokens [width], the sum over them); None: 0 for those by the outputs, not wanted for the others.  A descriptor without
     x_out and x_type takes the type of x_out_grad."""
     import torch
     T, H = desc.tokens, desc.width
@@ -375,7 +376,7 @@ def make_block_grads(desc, x_out_grad=None, h_out_grad=None, y_grad=None, h_grad
         x_of = x_out_grad.dtype
         desc.x_type, desc.types = _type(x_out_grad), (y_of, h_of, x_of)
     if gate_grad is not None and gate_grad.dim() != desc.gated:
-        raise ValueError("a gradient of another shape than the gate")
+        raise ValueError("a gradient by the gate has the gate's shape, [width] where tokens share it")
     g = BlockGrads()
     g.x_out_grad, g.x_out_stride = _rows(x_out_grad, x_of, T, H)
     g.h_out_grad, g.h_out_stride = _rows(h_out_grad, h_of, T, H)
