@@ -30,8 +30,9 @@ struct HeadArgs {
   int64_t pitch;                     // columns of d in memory, a multiple of 256
   int64_t rows64;                    // rows, rounded up to a multiple of 64
   uint16_t* grad;                    // d [rows64][pitch]
-  const float* row_grad;             // [rows]: scale * gradient * lift, 0 where the target is ignored
-  const float* lift;                 // [2]: what d is multiplied by, and its inverse
+  const float* row_grad;             // [rows]: scale * gradient, times a factor, 0 where the target is ignored
+  const float* row_back;             // [rows]: what a row of d W is multiplied by, 0 where the target is ignored
+  const float* back;                 // what d^T x is
   const uint16_t* x_copy;            // x [rows64][width], rows without a target 0
   float* sums;                       // x_grad in parts [splits][rows][width]
   int splits, steps, add;            // parts of a piece, 64-wide steps of it, whether to add to what is there
@@ -57,6 +58,12 @@ __device__ __forceinline__ float groups_sum(float v) {
   v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
 #endif
   return v;
+}
+
+// A row's gradient by its scaled logits, 0 where the target is ignored.
+__device__ __forceinline__ float gradient_of(const szo_head_desc& d, const float* grad, int64_t row) {
+  const int64_t t = d.targets ? d.targets[row] : -1;
+  return t >= 0 && t < d.vocab ? grad[row] * d.scale : 0.f;
 }
 
 template <int TYPE>
@@ -180,8 +187,9 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
 
 // The first workgroup: scale * gradient of each row, times a factor that takes the largest to just below a power of two, where a rounding is smallest relative to the value: most losses have
 // one gradient for all rows, and d of an unlikely target is nearly that, so its rounding is the whole row's (1.004 in bf16 would be off by 2^-8, 1.98 is by half of it).  For fp16 the
-// power is 2^14: with |1 - p| <= 1 nothing overflows, and what is 2^-27 of the largest still has all its bits.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
-__global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* lift, int64_t rows64, uint16_t* x_copy) {
+// power is 2^14: with |1 - p| <= 1 nothing overflows, and what is 2^-27 of the largest still has all its bits.  Rows without a target have no gradient, whatever the weight holds: what 0
+// times infinity left of theirs is dropped where the row is stored.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
+__global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* row_back, float* back, int64_t rows64, uint16_t* x_copy) {
   if (blockIdx.x > 0) {
     const int per = d.width / 8;
     const int64_t i = (int64_t)(blockIdx.x - 1) * 256 + threadIdx.x, row = i / per, at = i % per * 8;
@@ -194,13 +202,9 @@ __global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d
   }
   __shared__ float part[4];
   float most = 0.f;
-  auto of = [&](int64_t i) {
-    const int64_t t = d.targets ? d.targets[i] : -1;
-    return t >= 0 && t < d.vocab ? grad[i] * d.scale : 0.f;
-  };
 #pragma unroll 4
   for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
-    const float g = fabsf(of(i));
+    const float g = fabsf(gradient_of(d, grad, i));
     if (g < __builtin_inff()) most = fmaxf(most, g);
   }
   most = lanes_max<64>(most);
@@ -208,10 +212,14 @@ __global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d
   __syncthreads();
   for (int w = 0; w < 4; ++w) most = fmaxf(most, part[w]);
   const int up = most > 0.f && d.type == SZO_F16 ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
-  const float fill = most > 0.f ? 0.992f / __builtin_amdgcn_frexp_mantf(most) : 1.f, by = __builtin_amdgcn_ldexpf(fill, up);
+  const float fill = most > 0.f ? 0.992f / __builtin_amdgcn_frexp_mantf(most) : 1.f, by = __builtin_amdgcn_ldexpf(fill, up), undo = __builtin_amdgcn_ldexpf(1.f / fill, -up);
 #pragma unroll 4
-  for (int64_t i = threadIdx.x; i < d.rows; i += 256) row_grad[i] = of(i) * by;
-  if (threadIdx.x == 0) { lift[0] = by; lift[1] = __builtin_amdgcn_ldexpf(1.f / fill, -up); }
+  for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
+    const int64_t t = d.targets ? d.targets[i] : -1;
+    row_grad[i] = gradient_of(d, grad, i) * by;
+    row_back[i] = t >= 0 && t < d.vocab ? undo : 0.f;
+  }
+  if (threadIdx.x == 0) *back = undo;
 }
 
 // Rows of nothing.
@@ -291,7 +299,12 @@ __global__ void __launch_bounds__(kThreads, 2) head_x_grad_kernel(const HeadArgs
 #pragma unroll
       for (int j = 0; j < L::TJ; ++j) tile.sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float by = a.lift[1];
+  float by[L::TJ];                                       // all loads before the first store
+#pragma unroll
+  for (int j = 0; j < L::TJ; ++j) {
+    const int64_t token = t0 + wj * (BT / 4) + 16 * j + (lane & 15);
+    by[j] = !a.sums && token < d.rows ? a.row_back[token] : 0.f;
+  }
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j) {
     const int64_t token = t0 + wj * (BT / 4) + 16 * j + (lane & 15);
@@ -310,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 2) head_x_grad_kernel(const HeadArgs
         *to = v;
       } else {
         uint16_t* const to = static_cast<uint16_t*>(a.out) + token * a.out_stride + k;
-        const uint2 v = rounded4<TYPE>(tile.sum[i][j], by);
+        const uint2 v = by[j] == 0.f ? make_uint2(0, 0) : rounded4<TYPE>(tile.sum[i][j], by[j]);
         if (a.out_vec) *reinterpret_cast<uint2*>(to) = v;
         else { to[0] = (uint16_t)v.x; to[1] = (uint16_t)(v.x >> 16); to[2] = (uint16_t)v.y; to[3] = (uint16_t)(v.y >> 16); }
       }
@@ -326,13 +339,14 @@ __global__ void __launch_bounds__(256) head_x_sum_kernel(const HeadArgs a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per, k = i % per * 4;
   if (row >= d.rows) return;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  const float by = a.row_back[row];
 #pragma unroll 4
   for (int p = 0; p < a.splits; ++p) {
     const float4 v = *reinterpret_cast<const float4*>(a.sums + ((int64_t)p * d.rows + row) * d.width + k);
     s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
   }
   uint16_t* const to = static_cast<uint16_t*>(a.out) + row * a.out_stride + k;
-  const uint2 v = rounded4<TYPE>(s, a.lift[1]);
+  const uint2 v = by == 0.f ? make_uint2(0, 0) : rounded4<TYPE>(s, by);
   if (a.out_vec) *reinterpret_cast<uint2*>(to) = v;
   else { to[0] = (uint16_t)v.x; to[1] = (uint16_t)(v.x >> 16); to[2] = (uint16_t)v.y; to[3] = (uint16_t)(v.y >> 16); }
 }
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 2) head_weight_grad_kernel(const Hea
   // Through LDS, so that a row's 16-byte pieces go to memory side by side: stored as they lie, 8 bytes a lane and 32 side by side, lines reach memory in parts.
   constexpr int kPitch = SIZE * 2 + 16, kPieces = SIZE / 8;
   static_assert(SIZE * kPitch <= L::kLds, "the operands' place");
-  const float by = a.lift[1];
+  const float by = *a.back;
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < L::TJ; ++j)
@@ -506,7 +520,7 @@ struct Plan {
   int64_t rows64, pitch;
   int pieces;
   GradPlan x;
-  size_t grad_at, copy_at, sums_at, rows_at, lift_at, bytes;
+  size_t grad_at, copy_at, sums_at, rows_at, row_back_at, back_at, bytes;
 };
 Plan plan_of(const szo_head_desc* d) {
   Plan p;
@@ -521,7 +535,8 @@ Plan plan_of(const szo_head_desc* d) {
   p.copy_at = take((size_t)p.rows64 * d->width * 2);
   p.sums_at = take(p.pieces > 1 || p.x.splits > 1 ? (size_t)p.x.splits * d->rows * d->width * sizeof(float) : 0);
   p.rows_at = take((size_t)d->rows * sizeof(float));
-  p.lift_at = take(2 * sizeof(float));
+  p.row_back_at = take((size_t)d->rows * sizeof(float));
+  p.back_at = take(sizeof(float));
   p.bytes = at;
   return p;
 }
@@ -530,13 +545,15 @@ template <int TYPE>
 int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad, int64_t weight_grad_stride, char* room, hipStream_t s) {
   const szo_head_desc& d = a.d;
   const int64_t copies = weight_grad ? tiles_of(p.rows64 * (d.width / 8), 256) : 0;
-  head_prepare_kernel<<<dim3((unsigned)(1 + copies)), 256, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.lift_at), p.rows64, (uint16_t*)(room + p.copy_at));
+  head_prepare_kernel<<<dim3((unsigned)(1 + copies)), 256, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.row_back_at),
+                                                                          (float*)(room + p.back_at), p.rows64, (uint16_t*)(room + p.copy_at));
   SZO_LAUNCH_CHECK();
   a.rows64 = p.rows64;
   a.pitch = p.pitch;
   a.grad = (uint16_t*)(room + p.grad_at);
   a.row_grad = (const float*)(room + p.rows_at);
-  a.lift = (const float*)(room + p.lift_at);
+  a.row_back = (const float*)(room + p.row_back_at);
+  a.back = (const float*)(room + p.back_at);
   a.x_copy = (const uint16_t*)(room + p.copy_at);
   a.splits = p.x.splits;
   float* const sums = p.pieces > 1 || p.x.splits > 1 ? (float*)(room + p.sums_at) : nullptr;
