@@ -503,7 +503,8 @@ int szo_head_logprobs(const szo_head_desc* desc /* host */, void* workspace, voi
 size_t szo_head_workspace_bytes(const szo_head_desc* desc /* host */);
 /* Gradients by x and by the weight of a scalar whose gradient by logp is grad_logp (device fp32 [rows]), from the forward's stats:
  *   d = scale grad_logp (1[v = target] - p),   x_grad = d weight,   weight_grad = d^T x
- * The logits are computed again, piece by piece of the vocabulary; d is rounded to the type, times a factor that the largest gradient sets.  x_grad and weight_grad (device,
+ * The logits are computed again, piece by piece of the vocabulary; d is rounded to the type, times a factor that the largest gradient sets and, in fp16,
+ * a power of two for each row: a row of x_grad has the bits of its own gradient.  x_grad and weight_grad (device,
  * of the type, rows x_grad_stride and weight_grad_stride apart, 2-byte aligned; either may be NULL) are overwritten and may be the buffers of x and weight, with their strides.  Rows whose target
  * is ignored have gradient 0 and no part in weight_grad, whatever they hold.  workspace: szo_head_bwd_workspace_bytes(desc): up to 256 MiB (or 256 entries) for a piece of d, as
  * much as x, and what sums of x_grad take.  SZO_EUNSUPPORTED also for rows times width from 2^34 on. */

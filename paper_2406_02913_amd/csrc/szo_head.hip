@@ -185,41 +185,104 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a) {
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
 
-// The first workgroup: scale * gradient of each row, times a factor that takes the largest to just below a power of two, where a rounding is smallest relative to the value: most losses have
-// one gradient for all rows, and d of an unlikely target is nearly that, so its rounding is the whole row's (1.004 in bf16 would be off by 2^-8, 1.98 is by half of it).  For fp16 the
-// power is 2^14: with |1 - p| <= 1 nothing overflows, and what is 2^-27 of the largest still has all its bits.  Rows without a target have no gradient, whatever the weight holds: what 0
-// times infinity left of theirs is dropped where the row is stored.  The others: x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
-__global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* row_back, float* back, int64_t rows64, uint16_t* x_copy) {
+// Factors of d.  A common one takes the largest gradient to just below a power of two, where a rounding is smallest relative to the value: most losses have one gradient for all rows, and
+// d of an unlikely target is nearly that, so its rounding is the whole row's (1.004 in bf16 would be off by 2^-8, 1.98 is by half of it).  In fp16 each row has a power of two of its own
+// beside it, which takes its gradient to between 2^13 and 2^14: with |1 - p| <= 1 nothing overflows, and entries of p from 2^-27 on have all their bits, however small the row's gradient is beside others.
+// x_grad's rows are divided by theirs.  weight_grad adds rows up, so the copy of x that it reads is multiplied by the inverse power, and by what takes the largest state of the
+// batch to below 2^15: exact but for states below 2^-28 of that, times what the row's gradient is smaller by than the largest.
+constexpr int kMostSizes = 256, kMostPlaces = 120;
+
+// Places that an fp16 row is shifted up by; `fill`: the common factor.
+__device__ __forceinline__ int places_of(float g, float fill) {
+  g = fabsf(g) * fill;
+  return g > 0.f && g < __builtin_inff() ? min(14 - __builtin_amdgcn_frexp_expf(g), kMostPlaces) : 0;
+}
+
+// Largest gradient and state of the rows that have a finite gradient other than 0, for each workgroup.
+__global__ void __launch_bounds__(1024) head_sizes_kernel(const szo_head_desc d, const float* grad, float2* sizes) {
+  const uint32_t per = (uint32_t)d.width / 8, all = (uint32_t)d.rows * per;            // below 2^31
+  float most = 0.f;
+  uint32_t state = 0;
+  for (uint32_t i = blockIdx.x * 1024 + threadIdx.x; i < all; i += gridDim.x * 1024) {
+    const uint32_t row = i / per;
+    const float g = fabsf(gradient_of(d, grad, row));
+    if (!(g > 0.f && g < __builtin_inff())) continue;
+    most = fmaxf(most, g);
+    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + (int64_t)row * d.x_stride + (i - row * per) * 8);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t size = w[k / 2] >> (k % 2 * 16) & 0x7FFFu;
+      state = max(state, size < 0x7C00u ? size : 0u);
+    }
+  }
+  __shared__ float2 part[16];
+  float x = (float)__builtin_bit_cast(_Float16, (uint16_t)state);
+  most = lanes_max<64>(most);
+  x = lanes_max<64>(x);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = make_float2(most, x);
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int w = 0; w < 16; ++w) { most = fmaxf(most, part[w].x); x = fmaxf(x, part[w].y); }
+  sizes[blockIdx.x] = make_float2(most, x);
+}
+
+// The first workgroup: scale * gradient of each row, times its factors, and what undoes them.  Rows without a target have no gradient, whatever the weight holds: what 0 times infinity left of
+// theirs is dropped where the row is stored.  The others: the copy of x with rows that have no target as 0, which may hold anything: 0 times infinity would reach the weight's gradient.
+// `count`: sizes that were found, fp16 and with weight_grad; else 0.
+__global__ void __launch_bounds__(256) head_prepare_kernel(const szo_head_desc d, const float* grad, float* row_grad, float* row_back, float* back, int64_t rows64, uint16_t* x_copy,
+                                                           const float2* sizes, int count) {
+  __shared__ float2 part[4];
+  const bool half = d.type == SZO_F16;
+  float most = 0.f, state = 0.f;
+  if (count > 0) {
+    if ((int)threadIdx.x < count) { most = sizes[threadIdx.x].x; state = sizes[threadIdx.x].y; }
+  } else if (blockIdx.x == 0) {
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
+      const float g = fabsf(gradient_of(d, grad, i));
+      if (g < __builtin_inff()) most = fmaxf(most, g);
+    }
+  }
+  if (half || blockIdx.x == 0) {                         // of the whole workgroup
+    most = lanes_max<64>(most);
+    state = lanes_max<64>(state);
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = make_float2(most, state);
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) { most = fmaxf(most, part[w].x); state = fmaxf(state, part[w].y); }
+  }
+  const float fill = most > 0.f ? 0.992f / __builtin_amdgcn_frexp_mantf(most) : 1.f;
+  // fp16: d times 2^places, states times 2^(sum - places)
+  const int sum = half && most > 0.f ? places_of(most, fill) + (state > 0.f ? 15 - __builtin_amdgcn_frexp_expf(state) : 0) : 0;
   if (blockIdx.x > 0) {
     const int per = d.width / 8;
     const int64_t i = (int64_t)(blockIdx.x - 1) * 256 + threadIdx.x, row = i / per, at = i % per * 8;
     if (row >= rows64) return;
     const int64_t target = row < d.rows && d.targets ? d.targets[row] : -1;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (target >= 0 && target < d.vocab) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + row * d.x_stride + at);
+    if (target >= 0 && target < d.vocab) {
+      v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + row * d.x_stride + at);
+      const float g = half ? fabsf(gradient_of(d, grad, row)) : 0.f;
+      if (g > 0.f && g < __builtin_inff()) {
+        const int by = sum - places_of(g, fill);
+        f16x8 h = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[k] = (_Float16)__builtin_amdgcn_ldexpf((float)h[k], by);
+        v = __builtin_bit_cast(uint4, h);
+      }
+    }
     *reinterpret_cast<uint4*>(x_copy + row * d.width + at) = v;
     return;
   }
-  __shared__ float part[4];
-  float most = 0.f;
-#pragma unroll 4
-  for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
-    const float g = fabsf(gradient_of(d, grad, i));
-    if (g < __builtin_inff()) most = fmaxf(most, g);
-  }
-  most = lanes_max<64>(most);
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
-  __syncthreads();
-  for (int w = 0; w < 4; ++w) most = fmaxf(most, part[w]);
-  const int up = most > 0.f && d.type == SZO_F16 ? min(max(14 - __builtin_amdgcn_frexp_expf(most), -100), 100) : 0;
-  const float fill = most > 0.f ? 0.992f / __builtin_amdgcn_frexp_mantf(most) : 1.f, by = __builtin_amdgcn_ldexpf(fill, up), undo = __builtin_amdgcn_ldexpf(1.f / fill, -up);
 #pragma unroll 4
   for (int64_t i = threadIdx.x; i < d.rows; i += 256) {
     const int64_t t = d.targets ? d.targets[i] : -1;
-    row_grad[i] = gradient_of(d, grad, i) * by;
-    row_back[i] = t >= 0 && t < d.vocab ? undo : 0.f;
+    const float g = gradient_of(d, grad, i);
+    const int by = half ? places_of(g, fill) : 0;
+    row_grad[i] = __builtin_amdgcn_ldexpf(g * fill, by);
+    row_back[i] = t >= 0 && t < d.vocab ? __builtin_amdgcn_ldexpf(1.f / fill, -by) : 0.f;
   }
-  if (threadIdx.x == 0) *back = undo;
+  if (threadIdx.x == 0) *back = __builtin_amdgcn_ldexpf(1.f / fill, -sum);
 }
 
 // Rows of nothing.
@@ -520,7 +583,7 @@ struct Plan {
   int64_t rows64, pitch;
   int pieces;
   GradPlan x;
-  size_t grad_at, copy_at, sums_at, rows_at, row_back_at, back_at, bytes;
+  size_t grad_at, copy_at, sums_at, rows_at, row_back_at, back_at, sizes_at, bytes;
 };
 Plan plan_of(const szo_head_desc* d) {
   Plan p;
@@ -537,6 +600,7 @@ Plan plan_of(const szo_head_desc* d) {
   p.rows_at = take((size_t)d->rows * sizeof(float));
   p.row_back_at = take((size_t)d->rows * sizeof(float));
   p.back_at = take(sizeof(float));
+  p.sizes_at = take(d->type == SZO_F16 ? kMostSizes * sizeof(float2) : 0);
   p.bytes = at;
   return p;
 }
@@ -545,8 +609,14 @@ template <int TYPE>
 int backward(HeadArgs a, const Plan& p, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad, int64_t weight_grad_stride, char* room, hipStream_t s) {
   const szo_head_desc& d = a.d;
   const int64_t copies = weight_grad ? tiles_of(p.rows64 * (d.width / 8), 256) : 0;
-  head_prepare_kernel<<<dim3((unsigned)(1 + copies)), 256, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.row_back_at),
-                                                                          (float*)(room + p.back_at), p.rows64, (uint16_t*)(room + p.copy_at));
+  float2* const sizes = (float2*)(room + p.sizes_at);
+  const int count = TYPE == SZO_F16 && weight_grad ? (int)std::min<int64_t>(kMostSizes, tiles_of(d.rows * (d.width / 8), 1024)) : 0;
+  if (count) {
+    head_sizes_kernel<<<dim3((unsigned)count), 1024, 0, s>>>(d, grad_logp, sizes);
+    SZO_LAUNCH_CHECK();
+  }
+  head_prepare_kernel<<<dim3((unsigned)(1 + copies)), 256, 0, s>>>(d, grad_logp, (float*)(room + p.rows_at), (float*)(room + p.row_back_at), (float*)(room + p.back_at), p.rows64,
+                                                                          (uint16_t*)(room + p.copy_at), sizes, count);
   SZO_LAUNCH_CHECK();
   a.rows64 = p.rows64;
   a.pitch = p.pitch;
