@@ -988,7 +988,7 @@ struct SharedPlan { int wr, wk, tiles, splits; };
 SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   SharedPlan p;
   const int64_t group = d->q_heads / d->cache.kv_heads, heads = d->cache.kv_heads, rows = d->tokens * group;
-  const int64_t held = std::max<int64_t>(1, rows / 32) * heads;            // tiles that hold something, about
+  const int64_t held = std::max<int64_t>({1, rows / 32, std::min(g->groups, d->cache.sequences)}) * heads;            // tiles that hold something, about: a group has one at least
   p.tiles = (int)(rows / 32 + g->groups + 2);
   // a tile's blocks: the shared ones, and half of the most of each sequence that is in it
   const int64_t each = std::max<int64_t>(1, rows / d->cache.sequences), sequences = std::max<int64_t>(1, std::min<int64_t>(32 / each, g->max_sequences));
@@ -1001,14 +1001,26 @@ SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   return p;
 }
 
-// Whether sequences go together: else each goes by itself, as szo_attn_cached has it.  They do where anything is shared and the chip's 2048 waves would have more than a block
-// each otherwise: below that nothing is waited for but the round trips that a wave begins with, of which groups have more (4 sequences behind 1024: 12.8 us together, 9.9 apart;
-// 16 behind 1024 12.9 and 14.0).
+// Whether sequences go together: else each goes by itself, as szo_attn_cached has it.  They do where
+//   - a tile of rows can be of more than one sequence: groups of one have nothing to share, and a sequence that fills eight tiles saves half a tile of them,
+//   - a window leaves a block of the prefix to see, behind half of the most that a sequence has of its own,
+//   - the chip's 2048 waves would have more than a block each otherwise: below that nothing is waited for but the round trips that a wave begins with, of which groups have more.
+// us together / apart, 32 query and 8 key heads of 128 in bf16, one token each: 4 sequences behind 1024 12.8 / 9.9; 64 groups of one behind 1024 83 / 28; 64 behind 8192 with up to 200 of
+// their own and a window of 100 17 / 8, of 1024 20 / 18, with 2000 of their own 34 / 26; 64 prompts of 500 behind 1000 842 / 760.
+//   It does not weigh the prefix against what sequences have of their own, whose blocks take 1.7 times as long together: 64 behind 64, 256, 1024, 2048 with 1000 each 33 / 25, 34 / 27, 34 / 34,
+// 35 / 43; 8 behind 2048 with 2000 each 25 / 15, 8 behind 8192 with 100 each 23 / 21, 2 of those 19 / 13; 32 answers of 30 tokens behind 64 17 / 9, behind 2000 54 / 49.
 bool together(const szo_attn_desc* d, const szo_attn_groups* g) {
-  if (g->groups == 0 || g->max_shared < kKvBlock) return false;
+  if (g->groups == 0 || g->max_shared < kKvBlock || g->max_sequences <= 1) return false;
   const int64_t group = d->q_heads / d->cache.kv_heads, rows = (int64_t)d->max_q * group;
+  if (rows > 256) return false;
   const int64_t tiles = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((rows + 31) / 32)) * d->cache.kv_heads;
-  return tiles * ((int64_t)d->max_len / kKvBlock + 1) > 2048;
+  int64_t seen = d->max_len;                                                // tokens of a sequence, at most
+  if (d->window > 0) {
+    const int64_t reach = (int64_t)d->window + d->max_q, own = std::max<int64_t>(0, (int64_t)d->max_len - g->max_shared);
+    if (reach - own / 2 < kKvBlock) return false;
+    seen = std::min(seen, reach);
+  }
+  return tiles * (seen / kKvBlock + 1) > 2048;
 }
 
 int check(const szo_attn_desc* d, const szo_attn_groups* g) {

@@ -45,20 +45,30 @@ def test_pages_of_several_blocks(monkeypatch, page):
     s.check(monkeypatch, lengths, new, 4, "bf16", window=150)
 
 
-# head_dim, key heads, group, sequences, new tokens, hint of lengths -> what the plan says
-WAYS = [(64, 8, 2, 70, 60, 200, (1, 4, 1, 1)), (128, 8, 4, 40, 10, 1 << 17, (1, 1, 4, 1)), (128, 4, 4, 64, 1, 1 << 17, (1, 1, 8, 8)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),
-        (256, 2, 2, 64, 1, 600, (1, 1, 4, 32))]
+@pytest.mark.parametrize("window,new", [(20, 40), (33, 1), (64, 1), (64, 7), (150, 1), (150, 40), (1000, 1)])
+def test_many_sequences_with_a_window(monkeypatch, window, new):
+    """Lengths from inside the prefix to far behind it, so that most tiles have sequences that see other pages than the next."""
+    lengths = [new + 1 + i * 37 % 230 for i in range(300)]
+    plan = []
+    s = Shared(lengths, [0, 300], [128], 8, 64, PAGE)
+    leave(s, lengths, [new] * 300, window)
+    s.check(monkeypatch, lengths, [new] * 300, 1, "bf16", window=window, max_len=max(lengths), max_shared=256, plan=plan)
+    assert plan[0][0] == 1
 
 
-@pytest.mark.parametrize("window", [0, 70])
+# head_dim, key heads, group, sequences, new tokens, hint of lengths and of the prefix -> what the plan says, with a window of 150 and without
+WAYS = [(64, 8, 2, 70, 60, 300, (1, 4, 1, 1)), (128, 8, 4, 40, 10, 300, (1, 1, 4, 1)), (128, 8, 4, 64, 1, 300, (1, 1, 4, 4)), (64, 8, 4, 256, 1, 3000, (1, 1, 8, 1)),
+        (128, 8, 4, 64, 1, 6000, (1, 1, 8, 4)), (256, 8, 2, 64, 1, 600, (1, 1, 4, 8))]
+
+
+@pytest.mark.parametrize("window", [0, 150])
 @pytest.mark.parametrize("D,heads,group,sequences,new,hint,want", WAYS)
 def test_every_way_that_sizes_choose(monkeypatch, D, heads, group, sequences, new, hint, want, window):
-    """Lengths from inside the prefix to far behind it, so that most tiles have sequences that see other pages than the next."""
     lengths = [new + 1 + i * 37 % 230 for i in range(sequences)]
     plan = []
     s = Shared(lengths, [0, sequences], [128], heads, D, PAGE)
     leave(s, lengths, [new] * sequences, window)
-    s.check(monkeypatch, lengths, [new] * sequences, group, "bf16", window=window, max_len=hint, plan=plan)
+    s.check(monkeypatch, lengths, [new] * sequences, group, "bf16", window=window, max_len=hint, max_shared=hint, plan=plan)
     assert plan == [want]
 
 
