@@ -1,4 +1,6 @@
 """Sequences that share a prefix and name its pages only where they see them: pages behind a sequence's length, or that its window has left, need not be there."""
+import functools
+
 import numpy as np
 import pytest
 import torch
@@ -45,14 +47,26 @@ def test_pages_of_several_blocks(monkeypatch, page):
     s.check(monkeypatch, lengths, new, 4, "bf16", window=150)
 
 
+@functools.lru_cache(maxsize=1)
+def _many(sequences, D, heads):
+    """Lengths from inside the prefix to far behind it, so that most tiles have sequences that see other pages than the next."""
+    lengths = [61 + i * 37 % 230 for i in range(sequences)]
+    return lengths, Shared(lengths, [0, sequences], [128], heads, D, PAGE)
+
+
+def many(monkeypatch, sequences, D, heads, new, window):
+    """One filling of a cache serves all tests of its size: only the tables are theirs."""
+    lengths, s = _many(sequences, D, heads)
+    monkeypatch.setattr(s.b, "table", s.b.table.copy())
+    leave(s, lengths, [new] * sequences, window)
+    return lengths, s
+
+
 @pytest.mark.parametrize("window,new", [(20, 40), (33, 1), (64, 1), (64, 7), (150, 1), (150, 40), (1000, 1)])
 def test_many_sequences_with_a_window(monkeypatch, window, new):
-    """Lengths from inside the prefix to far behind it, so that most tiles have sequences that see other pages than the next."""
-    lengths = [new + 1 + i * 37 % 230 for i in range(300)]
+    lengths, s = many(monkeypatch, 300, 64, 8, new, window)
     plan = []
-    s = Shared(lengths, [0, 300], [128], 8, 64, PAGE)
-    leave(s, lengths, [new] * 300, window)
-    s.check(monkeypatch, lengths, [new] * 300, 1, "bf16", window=window, max_len=max(lengths), max_shared=256, plan=plan)
+    s.check(monkeypatch, lengths, [new] * 300, 1, "bf16", window=window, max_len=max(lengths), max_shared=max(lengths), plan=plan)
     assert plan[0][0] == 1
 
 
@@ -64,10 +78,8 @@ WAYS = [(64, 8, 2, 70, 60, 300, (1, 4, 1, 1)), (128, 8, 4, 40, 10, 300, (1, 1, 4
 @pytest.mark.parametrize("window", [0, 150])
 @pytest.mark.parametrize("D,heads,group,sequences,new,hint,want", WAYS)
 def test_every_way_that_sizes_choose(monkeypatch, D, heads, group, sequences, new, hint, want, window):
-    lengths = [new + 1 + i * 37 % 230 for i in range(sequences)]
+    lengths, s = many(monkeypatch, sequences, D, heads, new, window)
     plan = []
-    s = Shared(lengths, [0, sequences], [128], heads, D, PAGE)
-    leave(s, lengths, [new] * sequences, window)
     s.check(monkeypatch, lengths, [new] * sequences, group, "bf16", window=window, max_len=hint, max_shared=hint, plan=plan)
     assert plan == [want]
 
