@@ -511,6 +511,10 @@ size_t szo_head_workspace_bytes(const szo_head_desc* desc /* host */);
 int szo_head_logprobs_bwd(const szo_head_desc* desc /* host */, const float* grad_logp, void* x_grad, int64_t x_grad_stride, void* weight_grad,
                           int64_t weight_grad_stride, void* workspace, void* stream);
 size_t szo_head_bwd_workspace_bytes(const szo_head_desc* desc /* host */);
+/* Inspection: how the calls go about this descriptor.  plan[0], plan[1]: vocabulary entries and rows of a forward tile; plan[2]: pieces of the vocabulary in the backward, plan[3], plan[4]: entries
+ * and rows of a tile of d in the first of them, plan[5], plan[6], plan[7]: features and rows of a tile of x_grad, parts of a piece; plan[8]: features and entries of a tile of weight_grad.
+ * All 0 where there is nothing to do. */
+int szo_head_plan(const szo_head_desc* desc /* host */, int32_t* plan /* host, 9 */);
 
 /* ---- one-time set-up on the host (no GPU needed; deterministic) ------------------------- */
 

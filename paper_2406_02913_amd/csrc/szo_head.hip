@@ -570,12 +570,12 @@ int weight_grad_launch(HeadArgs a, hipStream_t s) {
   a.tiles_v = (int)tiles_of(a.piece_v, SIZE);
   return launch(head_weight_grad_kernel<TYPE, SIZE>, raised, Tile<TYPE, true, true, SIZE, SIZE, 2, 4>::kLds, tiles_of(a.d.width, SIZE) * a.tiles_v, s, a);
 }
+// Small tiles of dW where large ones would not fill the chip twice, or have a single step: two workgroups share a CU then.  us of a backward, large / small: 16 rows of 32000 x 4096 218 / 216, 200 rows
+// 299 / 308, 2000 rows 1310 / 1384; 2000 x 512: 16 rows 26 / 24, 2000 rows 89 / 67.
+bool small_weight_tiles(int64_t rows64, int64_t width, int64_t piece_v) { return rows64 <= 64 || tiles_of(width, 256) * tiles_of(piece_v, 256) < 512; }
 template <int TYPE>
 int weight_grad_launch(const HeadArgs& a, hipStream_t s) {
-  // Small tiles where large ones would not fill the chip twice, or have a single step: two workgroups share a CU then.  us of a backward, large / small: 16 rows of 32000 x 4096 218 / 216, 200 rows
-  // 299 / 308, 2000 rows 1310 / 1384; 2000 x 512: 16 rows 26 / 24, 2000 rows 89 / 67.
-  const bool small = a.rows64 <= 64 || tiles_of(a.d.width, 256) * tiles_of(a.piece_v, 256) < 512;
-  return small ? weight_grad_launch<TYPE, 128>(a, s) : weight_grad_launch<TYPE, 256>(a, s);
+  return small_weight_tiles(a.rows64, a.d.width, a.piece_v) ? weight_grad_launch<TYPE, 128>(a, s) : weight_grad_launch<TYPE, 256>(a, s);
 }
 
 // A backward: columns of d that are in memory at a time, parts of dx, and where things lie in the workspace.
@@ -676,6 +676,21 @@ extern "C" {
 size_t szo_head_workspace_bytes(const szo_head_desc* d) {
   if (check(d) != SZO_OK || d->rows == 0) return 16;
   return parts_bytes(d) + up16((size_t)d->rows * sizeof(float));
+}
+
+int szo_head_plan(const szo_head_desc* d, int32_t* plan) {
+  const int rc = check(d);
+  if (rc != SZO_OK) return rc;
+  if (!plan) return SZO_EINVAL;
+  std::fill(plan, plan + 9, 0);
+  if (d->rows == 0 || d->vocab == 0) return SZO_OK;
+  const Plan p = plan_of(d);
+  const int64_t piece_v = std::min(p.pitch, d->vocab);
+  const LogitPlan forward = logit_plan(d->rows, d->vocab), grad = logit_plan(d->rows, piece_v);
+  const int32_t says[9] = {forward.entries, forward.rows, p.pieces, grad.entries, grad.rows, p.x.features, p.x.rows, p.x.splits,
+                           small_weight_tiles(p.rows64, d->width, piece_v) ? 128 : 256};
+  std::copy(says, says + 9, plan);
+  return SZO_OK;
 }
 
 int szo_head_logprobs(const szo_head_desc* d, void* workspace, void* stream) {

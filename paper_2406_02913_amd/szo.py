@@ -159,6 +159,7 @@ _SIGS = {
     "szo_head_workspace_bytes": (C.c_size_t, [_P(HeadDesc)]),
     "szo_head_logprobs_bwd": (C.c_int, [_P(HeadDesc), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "szo_head_bwd_workspace_bytes": (C.c_size_t, [_P(HeadDesc)]),
+    "szo_head_plan": (C.c_int, [_P(HeadDesc), C.c_void_p]),
     "szo_last_hip_error": (C.c_int, []),
     "szo_version": (C.c_int, []),
 }
@@ -647,6 +648,13 @@ def szo_head_logprobs_bwd(desc, grad_logp, x_grad=None, weight_grad=None, worksp
 
 def szo_head_bwd_workspace_bytes(desc):
     return int(lib.szo_head_bwd_workspace_bytes(C.byref(desc)))
+
+
+def szo_head_plan(desc):
+    """(entries, rows of a forward tile; pieces of the vocabulary, entries, rows of a tile of d; features, rows of a tile of x_grad, parts of a piece; size of a tile of weight_grad)"""
+    plan = (C.c_int32 * 9)()
+    _check("szo_head_plan", lib.szo_head_plan(C.byref(desc), plan))
+    return tuple(plan)
 
 
 # ---- host set-up -----------------------------------------------------------------------------
