@@ -439,7 +439,8 @@ typedef struct szo_attn_groups {
   const int32_t* shared;        /* device [groups]                                                       */
 } szo_attn_groups;
 /* workspace: device, szo_attn_shared_workspace_bytes(desc, groups) for this very pair, 16-byte aligned, for this call alone while it runs.  SZO_EUNSUPPORTED as for
- * szo_attn_cached, for more than 2^30 rows (tokens times query heads of a key head), and beyond 2^23 - 1 tiles times parts and key heads. */
+ * szo_attn_cached, for more than 2^30 rows (tokens times query heads of a key head), and beyond 2^23 - 1 tiles times parts and
+ * key heads, or 2^24 - 1 tiles times 32 features of a head where there are parts. */
 int szo_attn_shared(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */, void* workspace, void* stream);
 size_t szo_attn_shared_workspace_bytes(const szo_attn_desc* desc /* host */, const szo_attn_groups* groups /* host */);
 /* Inspection: plan[0]: 1 where sequences go together, 0 where each goes by itself as in szo_attn_cached (nothing shared, or so little to do that it is faster); then tiles side by

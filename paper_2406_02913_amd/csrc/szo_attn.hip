@@ -984,6 +984,7 @@ int launch_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
 // 13.2 / 13.5, 15.8, 12.9, 13.2; answers of 3 to 61 tokens, 32 of them behind 4 x 2500 (976 tiles) 60, 87 / 72, side by side 77; 8 behind 2000 (344 tiles) 28, 40 / 35; 64 behind 2 x 2000 (2100
 // tiles) 101 / 136, side by side 114; 256 behind 8 x 2000 (7440 tiles) 295 / 443, side by side 241.  szo_attn_cached takes 102, 31, 113, 9.9, 74, 27, -, 358 for these.
 struct SharedPlan { int wr, wk, tiles, splits; };
+constexpr int join_pieces(int head_dim, int lanes) { return (32 * (head_dim / 4) * lanes + kThreads - 1) / kThreads; }       // workgroups that join a tile's parts
 
 SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
   SharedPlan p;
@@ -1033,6 +1034,7 @@ int check(const szo_attn_desc* d, const szo_attn_groups* g) {
   if (d->tokens * (d->q_heads / c.kv_heads) > 0x3FFFFFFF || g->groups > 0x3FFFFFFF) return SZO_EUNSUPPORTED;
   const SharedPlan p = plan_of(d, g);
   if ((int64_t)p.tiles * p.splits * c.kv_heads > kMostGroups) return SZO_EUNSUPPORTED;
+  if (p.splits > 1 && (int64_t)p.tiles * join_pieces(c.head_dim, 1) > 0xFFFFFFFFll / kThreads) return SZO_EUNSUPPORTED;
   return SZO_OK;
 }
 
@@ -1053,7 +1055,7 @@ int launch_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
 
 template <int TYPE, int D, int G>
 int join_shared(const AttnArgs& a, const SharedArgs& sh, hipStream_t s) {
-  constexpr int pieces = (32 * (D / 4) * G + kThreads - 1) / kThreads;            // of a tile
+  constexpr int pieces = join_pieces(D, G);
   const dim3 grid((unsigned)(sh.tiles * pieces), (unsigned)a.d.cache.kv_heads);
   attn_shared_join_kernel<TYPE, D, G><<<grid, kThreads, 0, s>>>(sh.tiles, sh.splits, a);
   SZO_LAUNCH_CHECK();

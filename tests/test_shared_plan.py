@@ -1,4 +1,6 @@
 """Which batches go over a shared prefix together, and how their tiles are counted: on the host, no kernel is launched."""
+import ctypes as C
+
 import pytest
 
 from paper_2406_02913_amd import szo
@@ -38,3 +40,17 @@ def test_every_group_has_a_tile():
     """64 groups of four sequences are 512 tiles for eight key heads, which fill the chip's waves without parts: 256 rows alone would be 64 tiles."""
     for groups, sequences, parts in ((64, 256, 1), (32, 64, 1), (16, 64, 2), (8, 64, 4), (1, 64, 4)):
         assert plan(groups, sequences, 1024, 100)[3] == parts, groups
+
+
+def test_more_tiles_than_a_launch_that_joins_their_parts_can_count():
+    """Threads of a launch are counted in 32 bits: eight workgroups of 256 join a tile's parts at a head dimension of 256."""
+    def call(groups):
+        cache = szo.KvCache(pages=1000, page_tokens=32, kv_heads=1, head_dim=256, sequences=128, max_pages=1000, k=P, v=P, k_exp=P, v_exp=P, page_table=P, lengths=P)
+        d = szo.AttnDesc(cache=cache, q_heads=1, type=szo.BF16, causal=1, scale=1.0, max_q=1, max_len=1 << 20, tokens=128, q=P, out=P, q_start=P, q_token_stride=256, q_head_stride=256,
+                         out_token_stride=256, out_head_stride=256)
+        plan = (C.c_int32 * 4)()
+        return szo.lib.szo_attn_shared_plan(C.byref(d), C.byref(szo.AttnGroups(groups=groups, max_sequences=2, max_shared=64, group_start=P, shared=P)), plan), plan[3]
+
+    least = (1 << 32) // (256 * 8) - 128 // 32 - 2                           # tiles: of the rows, and two besides those of the groups
+    assert call(least - 1) == (szo.OK, 2)
+    assert call(least)[0] == szo.EUNSUPPORTED
