@@ -60,10 +60,11 @@ __device__ __forceinline__ float groups_sum(float v) {
   return v;
 }
 
-// A row's gradient by its scaled logits, 0 where the target is ignored.
+// A row's gradient by its scaled logits, 0 where the target is ignored.  Both loads are asked for at once.
 __device__ __forceinline__ float gradient_of(const szo_head_desc& d, const float* grad, int64_t row) {
   const int64_t t = d.targets ? d.targets[row] : -1;
-  return t >= 0 && t < d.vocab ? grad[row] * d.scale : 0.f;
+  const float g = grad[row] * d.scale;
+  return t >= 0 && t < d.vocab ? g : 0.f;
 }
 
 template <int TYPE>
@@ -205,10 +206,10 @@ __global__ void __launch_bounds__(1024) head_sizes_kernel(const szo_head_desc d,
   uint32_t state = 0;
   for (uint32_t i = blockIdx.x * 1024 + threadIdx.x; i < all; i += gridDim.x * 1024) {
     const uint32_t row = i / per;
+    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + (int64_t)row * d.x_stride + (i - row * per) * 8);       // beside the gradient
     const float g = fabsf(gradient_of(d, grad, row));
     if (!(g > 0.f && g < __builtin_inff())) continue;
     most = fmaxf(most, g);
-    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.x) + (int64_t)row * d.x_stride + (i - row * per) * 8);
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
