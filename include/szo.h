@@ -431,7 +431,7 @@ int szo_attn_plan(const szo_attn_desc* desc /* host */, int32_t* plan /* host, 4
  * that its window has left, need not be there.  Tiles of 32 rows (tokens times query heads of a key head) of a group's sequences go
  * over the shared blocks together and then over each one's own; the result is that of szo_attn_cached up to the order of sums.  Of
  * shared[g] whole blocks of 32 tokens count, max_shared tokens at most; tokens behind a sequence's length and masked ones have no influence here either.  Sequences
- * of no group share nothing. */
+ * of no group share nothing.  A prefix that is shorter than what its sequences have of their own is faster by szo_attn_cached: the call does not weigh them. */
 typedef struct szo_attn_groups {
   int32_t groups, max_sequences;/* most sequences of a group: a hint, for the split of the work          */
   int32_t max_shared, reserved; /* most shared tokens that count                                         */

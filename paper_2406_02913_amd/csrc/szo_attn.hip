@@ -983,6 +983,9 @@ int launch_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
 // (16 tiles) 81, 48, 31, 23 / 57, 37, 25, 21, 21; 256 behind 4 x 2048 (256 tiles, 104 blocks) 50, 42, 52 / 36, 49; 4 behind 1024 (8 tiles, 40 blocks) 14.6, 14.1, 13.7, 12.9,
 // 13.2 / 13.5, 15.8, 12.9, 13.2; answers of 3 to 61 tokens, 32 of them behind 4 x 2500 (976 tiles) 60, 87 / 72, side by side 77; 8 behind 2000 (344 tiles) 28, 40 / 35; 64 behind 2 x 2000 (2100
 // tiles) 101 / 136, side by side 114; 256 behind 8 x 2000 (7440 tiles) 295 / 443, side by side 241.  szo_attn_cached takes 102, 31, 113, 9.9, 74, 27, -, 358 for these.
+//   A group counts as one tile at least: 32 groups of two behind 1024 48 -> 20, 16 of four behind 4096 43 -> 33.  Other heads than 8 key heads of 128 have tests of every way and few times, together / apart: 64
+// of one token behind 1024 with 100 of their own 15 / 13 with heads of 64, 27 / 63 with 32 key heads; 32 of them with 1000 of their own, 4 key heads of 256, 30 / 34.
+//   A tile looks for its sequences from the group's first on, 64 at a time: that grows with the square of a group's sequences, and has not been measured for thousands of them.
 struct SharedPlan { int wr, wk, tiles, splits; };
 constexpr int join_pieces(int head_dim, int lanes) { return (32 * (head_dim / 4) * lanes + kThreads - 1) / kThreads; }       // workgroups that join a tile's parts
 

@@ -8,7 +8,12 @@
 // Bound by memory: a row is read once and written once, and everything between stays in registers.  A row belongs to 1 to 16 waves, eight neighbouring
 // features of it to a thread (16 above 8192 features), so that a wave's loads are whole lines and a row's statistics are one exchange through LDS: the
 // variance comes from each wave's own mean and squares about it, joined as sums of squares about means are, which loses nothing where the mean is large.
-//   8192 tokens of 4096, block's output and stream in fp32, post norm and gate: 87 us, 5.4 TB/s of what is read and written once.  16 tokens: 4.3, a launch.
+//   8192 tokens of 4096, block's output and stream in fp32, post norm and gate: 87 us, 5.4 TB/s of what is read and written once; all in bf16 46 (268 MB at 5.8 TB/s, part of it from the last-level
+// cache).  16 tokens: 4.3, a launch.
+//   Two kinds of rows keep less in registers, in the backward: above 8192 features 87 to 155 registers a thread are spilled (260 to 380 bytes of scratch), and rows whose eights are not at multiples of 16
+// bytes (odd widths, strides and addresses), which are read feature by feature, spill 175 to 383 above 4096 features (0.6 to 1.3 KB).  us of 16 M features in bf16, RMS norm before the block alone / layer norms on
+// both sides with biases and a shared gate: 4096 features 38 / 53, 5120 51 / 81, 8192 44 / 74, 11008 115 / 186, 16384 122 / 178; read feature by feature 4095 201 / -, 5001 600 / 949, 12345 681 / 933.  fp32 instead of
+// bf16 at 4096 features - / 112, fp32 in and bf16 out - / 99.
 #include <algorithm>
 #include "szo_internal.h"
 #include "szo_types.h"
@@ -550,7 +555,7 @@ __global__ void __launch_bounds__(1024) block_sums_kernel(const float* __restric
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 constexpr int64_t kMostGroups = 0xFFFFFFFFll / 1024;
 
-// Eight features a thread up to 512 threads, sixteen beyond: with 1024 threads a thread has 128 registers, and a backward's sums alone take 40 or 80.
+// Eight features a thread up to 512 threads, sixteen beyond: with 1024 threads a thread has 128 registers, and a backward's sums alone take 32 or 64.
 int chunks_of(int width) { return width <= 4096 ? 1 : 2; }
 int waves_of(int width) { return (width + 512 * chunks_of(width) - 1) / (512 * chunks_of(width)); }
 // Rows of a workgroup: it has 256 threads at least where rows have fewer.

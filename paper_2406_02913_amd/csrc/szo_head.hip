@@ -7,8 +7,10 @@
 // logit, where it has it), and a small kernel joins the tiles of a row.  The backward computes them again, turns them into d, rounded to 16 bits, and multiplies that
 // twice.  d is in memory for a piece of the vocabulary at a time.  Three products of the same size, bound by the matrix cores for many rows and by one pass
 // over the weight for few.
-//   A head of 32000 entries of width 4096 in bf16, forward: 16 rows 46 to 62 us (262 MB of weight, read at 5.7 to 4.2 TB/s), 300 rows 90, 4096 rows 800 to 830 (1.30 to 1.34 PFLOP/s).  Backward
-// of 4096 rows 2520: d 859 with 262 MB written, dx 759 (1.41 PFLOP/s), dW 845, the copy of x 21.  200 rows of width 2048 in fp16 157: 44, 48 and 6 for its parts, 56, 3.5.
+//   A head of 32000 entries of width 4096 in bf16, several cards, weight in the last-level cache to weight in memory alone: 16 rows 45 to 62 us (262 MB of weight, read at 5.8 to 4.2 TB/s), 300 rows
+// 82 to 96, 4096 rows 800 to 852 (1.26 to 1.34 PFLOP/s; fp16 860).  Backward of 4096 rows 2450 to 2600 (fp16 2670): d 824 to 877 with 262 MB written, dx 742 to 793 (1.35 to 1.45 PFLOP/s), dW 819 to 869, the
+// copy of x 21.  200 rows of width 2048 in fp16 149 to 166: 45, 50 and 6 for its parts, 57, 4.8 for sizes of rows, 4.1 for the copy.  A vocabulary that does not fill the chip is far from its
+// bytes: 16 rows of 8000 x 4096 26 (65 MB: 13), 4 of 4000 x 8192 45.
 #include <algorithm>
 #include "szo_product.h"
 
