@@ -1006,7 +1006,7 @@ SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
 }
 
 // Whether sequences go together: else each goes by itself, as szo_attn_cached has it.  They do where
-//   - a tile of rows can be of more than one sequence: groups of one have nothing to share, and a sequence that fills eight tiles saves half a tile of them,
+//   - a tile of rows can be of more than one sequence: groups of one have nothing to share, and sequences that fill eight tiles each save half a tile of them,
 //   - a window leaves a block of the prefix to see, behind half of the most that a sequence has of its own,
 //   - the chip's 2048 waves would have more than a block each otherwise: below that nothing is waited for but the round trips that a wave begins with, of which groups have more.
 // us together / apart, 32 query and 8 key heads of 128 in bf16, one token each: 4 sequences behind 1024 12.8 / 9.9; 64 groups of one behind 1024 83 / 28; 64 behind 8192 with up to 200 of
@@ -1016,7 +1016,7 @@ SharedPlan plan_of(const szo_attn_desc* d, const szo_attn_groups* g) {
 bool together(const szo_attn_desc* d, const szo_attn_groups* g) {
   if (g->groups == 0 || g->max_shared < kKvBlock || g->max_sequences <= 1) return false;
   const int64_t group = d->q_heads / d->cache.kv_heads, rows = (int64_t)d->max_q * group;
-  if (rows > 256) return false;
+  if (d->tokens * group > 256 * (int64_t)d->cache.sequences) return false;            // in the mean: one long prompt among continuations leaves these together
   const int64_t tiles = std::min<int64_t>(d->tokens * group / 32 + d->cache.sequences, (int64_t)d->cache.sequences * ((rows + 31) / 32)) * d->cache.kv_heads;
   int64_t seen = d->max_len;                                                // tokens of a sequence, at most
   if (d->window > 0) {

@@ -8,11 +8,11 @@ from paper_2406_02913_amd import szo
 P = 0x10000                                    # never dereferenced
 
 
-def plan(groups, sequences, prefix, own, new=1, window=0, heads=8, group=4, D=128, most=None):
+def plan(groups, sequences, prefix, own, new=1, window=0, heads=8, group=4, D=128, most=None, tokens=None):
     """Groups of equally many sequences; at most `own` tokens of a sequence's own."""
     cache = szo.KvCache(pages=1000, page_tokens=32, kv_heads=heads, head_dim=D, sequences=sequences, max_pages=1000, k=P, v=P, k_exp=P, v_exp=P, page_table=P, lengths=P)
-    d = szo.AttnDesc(cache=cache, q_heads=heads * group, type=szo.BF16, causal=1, window=window, scale=1.0, max_q=new, max_len=prefix + own, tokens=sequences * new, q=P, out=P, q_start=P,
-                     q_token_stride=heads * group * D, q_head_stride=D, out_token_stride=heads * group * D, out_head_stride=D)
+    d = szo.AttnDesc(cache=cache, q_heads=heads * group, type=szo.BF16, causal=1, window=window, scale=1.0, max_q=new, max_len=prefix + own, tokens=sequences * new if tokens is None else tokens, q=P, out=P,
+                     q_start=P, q_token_stride=heads * group * D, q_head_stride=D, out_token_stride=heads * group * D, out_head_stride=D)
     g = szo.AttnGroups(groups=groups, max_sequences=sequences // groups if most is None else most, max_shared=prefix, group_start=P, shared=P)
     return szo.szo_attn_shared_plan(d, g)
 
@@ -34,6 +34,7 @@ def test_a_window_that_has_left_the_prefix():
 def test_sequences_that_fill_tiles_by_themselves():
     assert plan(1, 64, 1000, 500, new=64)[0] == 1
     assert plan(1, 64, 1000, 500, new=65) == (0, 0, 0, 0) and plan(1, 64, 1000, 500, new=500) == (0, 0, 0, 0)
+    assert plan(1, 64, 1000, 500, new=500, tokens=563)[0] == 1               # one long prompt beside 63 continuations
 
 
 def test_every_group_has_a_tile():
